@@ -454,6 +454,103 @@ int rslm_rescore(const rslm_rescore_codec *codec, const float *q_rot,
                  int32_t *out_ids, void *stream);
 
 /* ------------------------------------------------------------------------
+ * Microscaled 4-bit rows (MX4): vectors in the 4-bit floating point that the
+ * matrix cores multiply as it is, for collections, or weights, that are scored
+ * whole.  Coordinate d of a row has an E2M1 code (bit 3 the sign, bits 0..2
+ * the magnitude 0, 0.5, 1, 1.5, 2, 3, 4 or 6), and every 32 coordinates an
+ * E8M0 scale s:
+ *   value = magnitude * 2^(s - 127);  s = 255: all 32 are NaN.
+ * A matrix of n rows of dim coordinates, with steps = ceil(dim / 128):
+ *   codes  : n x 64 steps bytes, coordinate d in byte d / 2 of its row, the low
+ *            nibble for even d; 16-byte aligned;
+ *   scales : n x 4 steps bytes, scale d / 32; 4-byte aligned.
+ * Past dim both are zero; the products below rely on it.  1 <= dim <= 65,536,
+ * n <= 2^31 - 256.  Float rows are float32, float16 or bfloat16 (RSLM_F32, ...),
+ * aligned to their element, row i at i * stride elements.
+ *
+ * rslm_mx4_quantize: rows of floats, or of floats rotated by the plan (its
+ * dim, passes > 0; the bits of rslm_fwht's rotation), to MX4 rows:
+ *   s    = floor(log2 max|x|) - 2 + 127, at least 0 (so for a block of zeros);
+ *          255 where the 32 hold an infinity or a NaN;
+ *   code = x / 2^(s - 127) to the nearest magnitude, ties to the even code,
+ *          at most 6; 0 for a zero of either sign.
+ *   plan: NULL, or a plan of dimension dim.  Rows of x may overlap (any
+ *   stride >= 0).
+ * rslm_mx4_dequantize: the values, rounded to the type asked for (float32 and
+ *   bfloat16 hold them exactly); stride >= dim.
+ * ------------------------------------------------------------------------ */
+#define RSLM_F32 0
+#define RSLM_F16 1
+#define RSLM_BF16 2
+int rslm_mx4_quantize(const rslm_plan *plan, const void *x, int32_t dtype, int64_t n, int32_t dim,
+                      int64_t stride, uint8_t *codes, uint8_t *scales, void *stream);
+int rslm_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t n, int32_t dim, void *out,
+                        int32_t dtype, int64_t stride, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Products of MX4 rows; sums in float32.
+ * rslm_mx4_matmul: both sides in 4 bits,
+ *   out[i][j] = sum_d a_i[d] b_j[d],  out: m rows of n, type dtype,
+ *   row i at i * stride elements (stride >= n).  m <= 4,194,240.
+ * rslm_mx4_score: float rows (queries, activations) against 4-bit ones,
+ *   out[i][j] = sum_d x_i[d] b_j[d],
+ *   x: m rows of dim, type dtype, stride >= 0; out: m rows of n, float32 or x's
+ *   type (else RSLM_ERR_UNSUPPORTED), out_stride >= n.  x is not rounded: a
+ *   float32 x has the result of a float32 product.
+ * rslm_mx4_score_backward: its gradient with respect to x,
+ *   dx[i][d] = sum_j dout[i][j] b_j[d],
+ *   dout: m rows of n, type dtype, stride >= 0; dx: m rows of dim, float32 or
+ *   dout's type, dx_stride >= dim.  The workspace holds partial sums (float32,
+ *   joined in a fixed order: results do not change from call to call).
+ * m <= 8,388,480 for the last two.  A row of b with a NaN scale makes its
+ * products NaN.
+ * ------------------------------------------------------------------------ */
+int rslm_mx4_matmul(const uint8_t *a_codes, const uint8_t *a_scales, int64_t m, const uint8_t *b_codes,
+                    const uint8_t *b_scales, int64_t n, int32_t dim, void *out, int32_t dtype, int64_t stride,
+                    void *stream);
+int rslm_mx4_score(const void *x, int32_t dtype, int64_t m, int64_t stride, const uint8_t *codes,
+                   const uint8_t *scales, int64_t n, int32_t dim, void *out, int32_t out_dtype, int64_t out_stride,
+                   void *stream);
+size_t rslm_mx4_score_backward_workspace(int64_t m, int64_t n, int32_t dim);
+int rslm_mx4_score_backward(const void *dout, int32_t dtype, int64_t m, int64_t stride, const uint8_t *codes,
+                            const uint8_t *scales, int64_t n, int32_t dim, void *dx, int32_t dx_dtype,
+                            int64_t dx_stride, void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Log probabilities over rows of scores.  With z_j = scale * scores[i][j]
+ * (scale: the inverse temperature, > 0), of each row i:
+ *   lse      = log sum_j e^{z_j}
+ *   logprob  = z_t - lse for the entry t = target[i]; 0 where target[i] is
+ *              outside [0, n) (no target)
+ *   entropy  = lse - sum_j p_j z_j,  p_j = e^{z_j - lse}
+ *   top_*    = the k largest entries by (score desc, index asc), as log
+ *              probabilities and indices, padded with (-inf, -1)
+ * An entry whose z is -infinity is masked: probability 0, log probability
+ * -infinity, no alternative.  A row of masked entries has lse -infinity and
+ * entropy 0; a NaN or +infinity makes lse and entropy NaN (a NaN is no
+ * alternative).
+ *   scores: m rows of n, type dtype, stride >= 0; target: m int64 (NULL with
+ *   logprob NULL); logprob, entropy, lse: m float32 or NULL; top_*:
+ *   m x k, 0 <= k <= 1024.  m <= 8,388,607, 1 <= n < 2^31.  stats: m x 2
+ *   float32, the row's largest score and log sum_j e^{z_j - z_max}, which the
+ *   gradient takes: z_j - lse to full precision however large the scores are.
+ *
+ * rslm_logprob_backward: the gradient of the scores from those of logprob and
+ * entropy (m float32 each; NULL: zero), given stats and entropy:
+ *   dscores[i][j] = scale (dlogprob_i (1[j = t] - p_j)
+ *                          - dentropy_i p_j (z_j - lse_i + entropy_i)),
+ *   0 for masked entries and without a target's first term; type dtype,
+ *   dstride >= n.  dscores may be scores (same stride).
+ * ------------------------------------------------------------------------ */
+size_t rslm_logprob_workspace(int64_t m, int64_t n, int32_t k);
+int rslm_logprob(const void *scores, int32_t dtype, int64_t m, int64_t n, int64_t stride, float scale,
+                 const int64_t *target, int32_t k, float *logprob, float *lse, float *entropy, float *stats,
+                 float *top_logprob, int32_t *top_ids, void *ws, size_t ws_bytes, void *stream);
+int rslm_logprob_backward(const void *scores, int32_t dtype, int64_t m, int64_t n, int64_t stride, float scale,
+                          const int64_t *target, const float *stats, const float *entropy, const float *dlogprob,
+                          const float *dentropy, void *dscores, int64_t dstride, void *stream);
+
+/* ------------------------------------------------------------------------
  * Profiling hook (not part of the method): in later rslm_scan_topk calls
  * made by the calling host thread, ev_begin / ev_end (hipEvent_t passed as
  * void*, created by the caller with timing enabled) take the start and end

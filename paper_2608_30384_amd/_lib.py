@@ -17,6 +17,9 @@ IVF_ASSIGN_L2 = 0
 IVF_PROBE_IP = 1
 RSLM_RESCORE_SQ8 = 0
 RSLM_RESCORE_RSLM = 1
+RSLM_F32 = 0
+RSLM_F16 = 1
+RSLM_BF16 = 2
 
 EXPORTS = [
     "rslm_status_string", "rslm_last_hip_error", "rslm_version",
@@ -29,6 +32,9 @@ EXPORTS = [
     "rslm_scan_topk_workspace", "rslm_scan_topk", "rslm_workspace_size",
     "rslm_sq8_fit", "rslm_sq8_encode", "rslm_rescore", "rslm_set_timer", "rslm_calibrate_read",
     "rslm_grid2_lists",
+    "rslm_mx4_quantize", "rslm_mx4_dequantize", "rslm_mx4_matmul", "rslm_mx4_score",
+    "rslm_mx4_score_backward_workspace", "rslm_mx4_score_backward",
+    "rslm_logprob_workspace", "rslm_logprob", "rslm_logprob_backward",
 ]
 
 
@@ -102,6 +108,18 @@ def _declare(lib):
         "rslm_set_timer": (C.c_int, [C.c_int, P, P]),
         "rslm_calibrate_read": (C.c_int, [P, I64, P, I32, C.c_int, P]),
         "rslm_grid2_lists": (C.c_int, [P, I32, C.c_float, P, P]),
+        "rslm_mx4_quantize": (C.c_int, [P, P, I32, I64, I32, I64, P, P, P]),
+        "rslm_mx4_dequantize": (C.c_int, [P, P, I64, I32, P, I32, I64, P]),
+        "rslm_mx4_matmul": (C.c_int, [P, P, I64, P, P, I64, I32, P, I32, I64, P]),
+        "rslm_mx4_score": (C.c_int, [P, I32, I64, I64, P, P, I64, I32, P, I32, I64, P]),
+        "rslm_mx4_score_backward_workspace": (SZ, [I64, I64, I32]),
+        "rslm_mx4_score_backward": (C.c_int, [P, I32, I64, I64, P, P, I64, I32, P, I32, I64, P,
+                                              SZ, P]),
+        "rslm_logprob_workspace": (SZ, [I64, I64, I32]),
+        "rslm_logprob": (C.c_int, [P, I32, I64, I64, I64, C.c_float, P, I32, P, P, P, P, P, P, P,
+                                   SZ, P]),
+        "rslm_logprob_backward": (C.c_int, [P, I32, I64, I64, I64, C.c_float, P, P, P, P, P, P,
+                                            I64, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)

@@ -440,3 +440,194 @@ def rslm_rescore_rslm(plan2, codes2, scales2, q_rot, cand_scores, cand_ids, k_ou
                                                  _ptr(out_scores), _ptr(out_ids),
                                                  _stream(stream)))
     return out_scores, out_ids
+
+
+# ------------------------------------------------------------------ 4-bit (MX4) rows
+_FLOATS = {torch.float32: L.RSLM_F32, torch.float16: L.RSLM_F16, torch.bfloat16: L.RSLM_BF16}
+
+
+def _float_type(dtype, name):
+    if dtype not in _FLOATS:
+        raise TypeError(f"{name} must be float32, float16 or bfloat16, got {dtype}")
+    return _FLOATS[dtype]
+
+
+def _need_rows(t, name, shape=None):
+    """A 2-D device tensor of floats whose rows are contiguous (any row stride);
+    its type code and row stride."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    code = _float_type(t.dtype, name)
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} must be {'two-dimensional' if shape is None else tuple(shape)}, got {tuple(t.shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    return code, t.stride(0)
+
+
+def _out_rows(out, shape, dtype, device, name="out"):
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=device)
+    elif out.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {out.dtype}")
+    code, stride = _need_rows(out, name, shape)
+    return out, code, stride
+
+
+def _same_device(a, b, name):
+    if a.device != b.device:
+        raise ValueError(f"{name} must be on {a.device}, got {b.device}")
+
+
+class Mx4Rows:
+    """A matrix of microscaled 4-bit rows: ``codes`` (n x 64 steps uint8) and
+    ``scales`` (n x 4 steps uint8) of ``dim`` coordinates, steps = ceil(dim / 128),
+    zero past dim (``rslm_mx4_quantize`` writes them so)."""
+
+    def __init__(self, codes, scales, dim):
+        _need(codes, torch.uint8, "codes")
+        _need(scales, torch.uint8, "scales")
+        if not 1 <= dim <= 65536:
+            raise ValueError("dim must be 1..65536")
+        steps = (dim + 127) // 128
+        if codes.dim() != 2 or codes.shape[1] != 64 * steps or tuple(scales.shape) != (codes.shape[0], 4 * steps):
+            raise ValueError(f"codes / scales must be n x {64 * steps} and n x {4 * steps}")
+        _same_device(codes, scales, "scales")
+        self.codes, self.scales, self.dim = codes, scales, int(dim)
+
+    @classmethod
+    def empty(cls, n, dim, device):
+        steps = (dim + 127) // 128
+        return cls(torch.empty((n, 64 * steps), dtype=torch.uint8, device=device),
+                   torch.empty((n, 4 * steps), dtype=torch.uint8, device=device), dim)
+
+    @property
+    def n(self):
+        return self.codes.shape[0]
+
+    @property
+    def device(self):
+        return self.codes.device
+
+
+def rslm_mx4_quantize(x, plan=None, rows=None, stream=None):
+    """MX4 rows of the rows of x (float32, float16 or bfloat16, any row stride),
+    rotated by the plan first if one is given."""
+    code, stride = _need_rows(x, "x")
+    n, dim = x.shape
+    if plan is not None and plan.dim != dim:
+        raise ValueError("x must have the plan's dimension")
+    if rows is None:
+        rows = Mx4Rows.empty(n, dim, x.device)
+    elif rows.n != n or rows.dim != dim:
+        raise ValueError("rows must have the shape of x")
+    _same_device(x, rows, "rows")
+    L.check("rslm_mx4_quantize", L.lib().rslm_mx4_quantize(
+        plan.handle if plan is not None else None, _ptr(x), code, n, dim, stride, _ptr(rows.codes),
+        _ptr(rows.scales), _stream(stream)))
+    return rows
+
+
+def rslm_mx4_dequantize(rows, dtype=torch.float32, out=None, stream=None):
+    """The values of MX4 rows."""
+    out, code, stride = _out_rows(out, (rows.n, rows.dim), dtype, rows.device)
+    _same_device(rows, out, "out")
+    L.check("rslm_mx4_dequantize", L.lib().rslm_mx4_dequantize(
+        _ptr(rows.codes), _ptr(rows.scales), rows.n, rows.dim, _ptr(out), code, stride,
+        _stream(stream)))
+    return out
+
+
+def rslm_mx4_matmul(a, b, dtype=torch.float32, out=None, stream=None):
+    """a b^T of two sets of MX4 rows (a.n x b.n)."""
+    if a.dim != b.dim:
+        raise ValueError("a and b must have the same dimension")
+    _same_device(a, b, "b")
+    out, code, stride = _out_rows(out, (a.n, b.n), dtype, a.device)
+    _same_device(a, out, "out")
+    L.check("rslm_mx4_matmul", L.lib().rslm_mx4_matmul(
+        _ptr(a.codes), _ptr(a.scales), a.n, _ptr(b.codes), _ptr(b.scales), b.n, a.dim, _ptr(out),
+        code, stride, _stream(stream)))
+    return out
+
+
+def rslm_mx4_score(x, b, dtype=torch.float32, out=None, stream=None):
+    """x b^T of float rows x and MX4 rows b; dtype: float32 or x's."""
+    code, stride = _need_rows(x, "x")
+    if x.shape[1] != b.dim:
+        raise ValueError("x must have b's dimension")
+    _same_device(x, b, "b")
+    out, ocode, ostride = _out_rows(out, (x.shape[0], b.n), dtype, x.device)
+    _same_device(x, out, "out")
+    L.check("rslm_mx4_score", L.lib().rslm_mx4_score(
+        _ptr(x), code, x.shape[0], stride, _ptr(b.codes), _ptr(b.scales), b.n, b.dim, _ptr(out),
+        ocode, ostride, _stream(stream)))
+    return out
+
+
+def rslm_mx4_score_backward(dout, b, dtype=None, out=None, stream=None):
+    """The gradient of ``rslm_mx4_score`` with respect to x: dout b (dout.shape[0] x
+    b.dim); dtype: dout's (default) or float32."""
+    code, stride = _need_rows(dout, "dout")
+    if dout.shape[1] != b.n:
+        raise ValueError("dout must have a column for every row of b")
+    _same_device(dout, b, "b")
+    m = dout.shape[0]
+    out, ocode, ostride = _out_rows(out, (m, b.dim), dout.dtype if dtype is None else dtype, dout.device)
+    _same_device(dout, out, "out")
+    nb = L.lib().rslm_mx4_score_backward_workspace(m, b.n, b.dim)
+    ws = _WS.get(nb, dout.device, "mx4_backward", stream)
+    L.check("rslm_mx4_score_backward", L.lib().rslm_mx4_score_backward(
+        _ptr(dout), code, m, stride, _ptr(b.codes), _ptr(b.scales), b.n, b.dim, _ptr(out), ocode,
+        ostride, _ptr(ws), ws.numel(), _stream(stream)))
+    return out
+
+
+# ------------------------------------------------------------------ log probabilities
+class LogProb:
+    """What ``rslm_logprob`` returns, float32 except top_ids (int32): logprob
+    (None without targets), lse and entropy (m), top_logprob and top_ids (m x k),
+    and stats (m x 2), which the gradient takes."""
+
+    def __init__(self, logprob, lse, entropy, stats, top_logprob, top_ids):
+        self.logprob, self.lse, self.entropy, self.stats = logprob, lse, entropy, stats
+        self.top_logprob, self.top_ids = top_logprob, top_ids
+
+
+def rslm_logprob(scores, target=None, k=0, scale=1.0, stream=None):
+    """Log probability of the entry target[i] (int64; outside the row: none) of
+    each row of scores, log-sum-exp, entropy, and the k most likely entries."""
+    code, stride = _need_rows(scores, "scores")
+    _need(target, torch.int64, "target")
+    m, n = scores.shape
+    if target is not None and target.shape != (m,):
+        raise ValueError("target must have an entry for every row of scores")
+    new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=scores.device)
+    r = LogProb(new(m) if target is not None else None, new(m), new(m), new(m, 2),
+                new(m, k), new(m, k, dtype=torch.int32))
+    nb = L.lib().rslm_logprob_workspace(m, n, k)
+    ws = _WS.get(nb, scores.device, "logprob", stream)
+    L.check("rslm_logprob", L.lib().rslm_logprob(
+        _ptr(scores), code, m, n, stride, scale, _ptr(target), k, _ptr(r.logprob), _ptr(r.lse),
+        _ptr(r.entropy), _ptr(r.stats), _ptr(r.top_logprob), _ptr(r.top_ids), _ptr(ws), ws.numel(),
+        _stream(stream)))
+    return r
+
+
+def rslm_logprob_backward(scores, target, result, dlogprob=None, dentropy=None, scale=1.0, out=None,
+                          stream=None):
+    """The gradient of scores from those of logprob and entropy (None: zero);
+    result: what ``rslm_logprob`` returned for these scores."""
+    code, stride = _need_rows(scores, "scores")
+    _need(target, torch.int64, "target")
+    _need(dlogprob, torch.float32, "dlogprob")
+    _need(dentropy, torch.float32, "dentropy")
+    m, n = scores.shape
+    for t, name in ((target, "target"), (dlogprob, "dlogprob"), (dentropy, "dentropy"), (result.lse, "result")):
+        if t is not None and t.shape != (m,):
+            raise ValueError(f"{name} must have an entry for every row of scores")
+    out, _, ostride = _out_rows(out, (m, n), scores.dtype, scores.device)
+    L.check("rslm_logprob_backward", L.lib().rslm_logprob_backward(
+        _ptr(scores), code, m, n, stride, scale, _ptr(target), _ptr(result.stats), _ptr(result.entropy),
+        _ptr(dlogprob), _ptr(dentropy), _ptr(out), ostride, _stream(stream)))
+    return out

@@ -1,0 +1,439 @@
+// Log probabilities over rows of scores, z = scale * score:
+//   lse = log sum_j e^{z_j},  log probability of an entry z_j - lse,
+//   entropy = lse - sum_j p_j z_j,  and the k largest entries;
+// and the gradient  dz_j = dlp (1[j = target] - p_j) - dH p_j (z_j - lse + H).
+//
+// Forward: one pass over a row.  A thread keeps a running maximum and two sums
+// of the entries it reads, Z = sum w and W = sum w y with y = (score - maximum)
+// scale log2(e) and w = 2^y, and rescales them when its maximum rises; the
+// threads' are joined at the end (lse = maximum scale + ln Z, entropy = ln Z - ln2 W / Z).
+// The k largest come from the same pass: entries at or above a threshold, the
+// k-th largest known so far, go to a buffer in LDS, which is cut back to its k
+// best when it fills.  The first threshold is the k-th largest of the threads'
+// own maxima, which at least k entries reach.  Few rows are cut into slices,
+// joined by a second kernel.
+//
+// An entry of -infinity (or one that scale makes so) is masked: probability 0,
+// no alternative, gradient 0.  A row of nothing else has lse -infinity and
+// entropy 0.  Bound by memory: one read forward, a read and a write backward.
+#include "mx4_dev.h"
+#include "select_dev.h"
+
+namespace rslm {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kLpThreads = 256;
+constexpr int kLpEach = 16;                          // entries of a thread in a piece
+constexpr int kLpPiece = kLpThreads * kLpEach;
+constexpr int kLpMaxSlices = 256;
+
+// Running maximum (of the scores) and sums of part of a row.
+struct SoftSum {
+  float m, z, w;
+};
+
+// The sums of a and b together.
+__device__ __forceinline__ SoftSum soft_join(const SoftSum &a, const SoftSum &b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  if (m == -__builtin_inff()) {
+    // nothing but masked entries, or NaN
+    return SoftSum{m, a.z + b.z, a.w + b.w};
+  }
+  SoftSum r{m, 0.f, 0.f};
+  const float da = (a.m - m) * c, db = (b.m - m) * c;
+  // a part that is empty keeps what it has (0, or NaN): e^-inf times it
+  const float ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
+  r.z = a.z * ea + b.z * eb;
+  r.w = ea * (a.w + fmaxf(da, -200.f) * a.z) + eb * (b.w + fmaxf(db, -200.f) * b.z);
+  return r;
+}
+
+__device__ __forceinline__ SoftSum soft_join_wave(SoftSum s, float c) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) {
+    const SoftSum o{__shfl_xor(s.m, off, 64), __shfl_xor(s.z, off, 64), __shfl_xor(s.w, off, 64)};
+    s = soft_join(s, o, c);
+  }
+  return s;
+}
+
+struct LogprobArgs {
+  const void *scores;
+  int64_t m, n, stride;
+  float scale;
+  const int64_t *target;
+  int k;
+  float *logprob, *lse, *entropy, *stats, *top_logprob;
+  int32_t *top_ids;
+  int slices;
+  int64_t per;          // entries of a slice, a multiple of kLpPiece
+  SoftSum *sums;        // m x slices
+  uint64_t *cands;      // m x slices x k, 0: none
+};
+
+// z - lse of a score, from the row's largest and ln Z: exact to the last places
+// where z itself is large, and -infinity for a masked entry.
+__device__ __forceinline__ float log_of(float v, float m, float lz, float scale) {
+  return v * scale == -__builtin_inff() ? -__builtin_inff() : fmaf(v - m, scale, -lz);
+}
+
+// The row's numbers from its sums, by one thread; ln Z.
+template <int T>
+__device__ __forceinline__ float emit_row(const LogprobArgs &a, int64_t row, const SoftSum &s) {
+  float lz = logf(s.z), lse = fmaf(s.m, a.scale, lz), h = fmaf(-kLn2, s.w / s.z, lz);
+  if (s.z != s.z) {
+    lz = lse = h = s.z;
+  } else if (s.m * a.scale == -__builtin_inff()) {
+    lse = -__builtin_inff();
+    h = 0.f;
+  }
+  if (a.lse) a.lse[row] = lse;
+  if (a.entropy) a.entropy[row] = h;
+  a.stats[2 * row] = s.m;
+  a.stats[2 * row + 1] = lz;
+  if (a.logprob) {
+    const int64_t t = a.target[row];
+    a.logprob[row] =
+        t >= 0 && t < a.n ? log_of(load_float<T>(a.scores, row * a.stride + t), s.m, lz, a.scale) : 0.f;
+  }
+  return lz;
+}
+
+// The k best of the cnt composites in sm.buf, in order, as log probabilities.
+__device__ __forceinline__ void emit_top(const LogprobArgs &a, int64_t row, SelectSmem &sm, int cnt, float m, float lz) {
+  const int t = threadIdx.x, k = a.k;
+  float *os = a.top_logprob + row * k;
+  int32_t *oi = a.top_ids + row * k;
+  auto put = [&](int r, uint64_t e) {
+    const float v = key_to_float(uint32_t(e >> 32));
+    os[r] = log_of(v, m, lz, a.scale);
+    oi[r] = v * a.scale == -__builtin_inff() ? -1 : int32_t(0xffffffffu - uint32_t(e & 0xffffffffu));
+  };
+  if (cnt <= kLpThreads) {
+    if (t < cnt) {
+      const uint64_t e = sm.buf[t];
+      int r = 0;
+      for (int j = 0; j < cnt; ++j) r += sm.buf[j] > e;   // ids differ, so no two are equal
+      if (r < k) put(r, e);
+    }
+  } else {
+    sort_desc(sm, cnt);
+    for (int j = t; j < min(cnt, k); j += kLpThreads) put(j, sm.buf[j]);
+  }
+  for (int j = cnt + t; j < k; j += kLpThreads) {
+    os[j] = -__builtin_inff();
+    oi[j] = -1;
+  }
+}
+
+template <int T, bool TOP>
+__global__ void __launch_bounds__(kLpThreads) k_logprob(LogprobArgs a) {
+  __shared__ SelectSmem sm;
+  __shared__ SoftSum parts[kLpThreads / 64];
+  __shared__ __align__(16) float tops[kLpThreads];
+  __shared__ float thr_s;
+  __shared__ float lz_s;
+  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+  const int64_t row = blockIdx.x / a.slices;
+  const int slice = int(blockIdx.x % a.slices);
+  const int64_t j0 = int64_t(slice) * a.per, j1 = min(a.n, j0 + a.per);
+  const typename FloatType<T>::type *x = static_cast<const typename FloatType<T>::type *>(a.scores) + row * a.stride;
+  const float c = a.scale * kLog2e;
+  const float ninf = -__builtin_inff();
+  SoftSum s{ninf, 0.f, 0.f};
+  int count = 0;        // entries in the buffer, the same in every thread
+  float thr = ninf;     // entries below it are not among the k largest
+  for (int64_t j = j0; j < j1; j += kLpPiece) {
+    float v[kLpEach];
+#pragma unroll
+    for (int u = 0; u < kLpEach / 8; ++u) {
+      float e[8];
+      const int64_t at = j + (u * kLpThreads + tid) * 8;
+      const int64_t left = j1 - at;
+      if (left >= 8) {
+        load_float8<T>(e, x + at, 0, 8);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = i < left ? load_float<T>(x, at + i) : ninf;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[8 * u + i] = e[i];
+    }
+    float top = v[0];
+#pragma unroll
+    for (int i = 1; i < kLpEach; ++i) top = fmaxf(top, v[i]);
+    top = top == top ? top : ninf;
+    if (top > s.m) {
+      if (s.m > ninf) {
+        const float d = (s.m - top) * c, e = __builtin_amdgcn_exp2f(d);
+        s.w = e * (s.w + fmaxf(d, -200.f) * s.z);
+        s.z *= e;
+      }
+      s.m = top;
+    }
+    const float ref = s.m == ninf ? 0.f : s.m;
+#pragma unroll
+    for (int i = 0; i < kLpEach; ++i) {
+      const float y = (v[i] - ref) * c;
+      const float w = __builtin_amdgcn_exp2f(y);
+      s.z += w;
+      s.w = fmaf(w, fmaxf(y, -200.f), s.w);   // masked: w = 0 times -200
+    }
+    if constexpr (TOP) {
+      const int k = a.k;
+      // entries at or above the threshold; the buffer takes them unless it
+      // would overflow, which every thread learns after the barrier
+      auto push = [&](int i0, int i1) {
+        if (top >= thr) {
+#pragma unroll
+          for (int i = 0; i < kLpEach; ++i) {
+            if (i >= i0 && i < i1 && v[i] >= thr && v[i] > ninf) {
+              const uint32_t pos = atomicAdd(&sm.count, 1u);
+              if (pos < uint32_t(kSelCap))
+                sm.buf[pos] = composite(order_key(v[i] + 0.f), int32_t(j + ((i >> 3) * kLpThreads + tid) * 8 + (i & 7)));
+            }
+          }
+        }
+      };
+      // the k best of the buffer, and the k-th of them as the threshold
+      bool full = false;   // the buffer holds these and nothing else
+      auto cut = [&]() {
+        __syncthreads();
+        sort_desc(sm, count);
+        full = count >= k;
+        if (full) {
+          thr = fmaxf(thr, key_to_float(uint32_t(sm.buf[k - 1] >> 32)));
+          count = k;
+        }
+      };
+      // raise the threshold to the k-th largest of the threads' maxima
+      auto raise = [&]() {
+        if (k > kLpThreads) return;
+        tops[tid] = top;
+        __syncthreads();
+        int r = 0;
+        for (int i = 0; i < kLpThreads; i += 4) {
+          const float4 o = *reinterpret_cast<const float4 *>(&tops[i]);
+          r += (o.x > top || (o.x == top && i < tid)) + (o.y > top || (o.y == top && i + 1 < tid)) +
+               (o.z > top || (o.z == top && i + 2 < tid)) + (o.w > top || (o.w == top && i + 3 < tid));
+        }
+        if (r == k - 1) thr_s = top;
+        __syncthreads();
+        thr = fmaxf(thr, thr_s);
+      };
+      if (j == j0) raise();
+      for (int attempt = 0; attempt < 2; ++attempt) {
+        if (tid == 0) sm.count = uint32_t(count);
+        __syncthreads();
+        push(0, kLpEach);
+        __syncthreads();
+        const uint32_t now = sm.count;
+        __syncthreads();
+        if (now <= uint32_t(kSelCap)) {
+          full = full && int(now) == count;
+          count = int(now);
+          break;
+        }
+        if (attempt == 0) {
+          if (count > k) cut();
+          raise();
+        } else {
+          // a few entries of each thread at a time, which always fit
+          if (count > k) cut();
+          for (int i = 0; i < kLpEach; i += 4) {
+            __syncthreads();
+            if (tid == 0) sm.count = uint32_t(count);
+            __syncthreads();
+            push(i, i + 4);
+            __syncthreads();
+            count = int(sm.count);
+            cut();
+            __syncthreads();
+          }
+        }
+      }
+      if (count > kSelCap / 2 && count > k) cut();
+      // later entries have higher indices and lose to equal ones: a row of
+      // equal entries does not fill the buffer again
+      if (full) thr = key_to_float(order_key(thr + 0.f) + 1u);
+    }
+  }
+  s = soft_join_wave(s, c);
+  if (lane == 0) parts[wid] = s;
+  __syncthreads();
+  s = parts[0];
+#pragma unroll
+  for (int i = 1; i < kLpThreads / 64; ++i) s = soft_join(s, parts[i], c);
+  if (a.slices == 1) {
+    if (tid == 0) lz_s = emit_row<T>(a, row, s);
+    __syncthreads();
+    if constexpr (TOP) emit_top(a, row, sm, count, s.m, lz_s);
+  } else {
+    if (tid == 0) a.sums[blockIdx.x] = s;
+    if constexpr (TOP) {
+      if (count > a.k) {
+        __syncthreads();
+        sort_desc(sm, count);
+      }
+      __syncthreads();
+      for (int i = tid; i < a.k; i += kLpThreads) a.cands[int64_t(blockIdx.x) * a.k + i] = i < count ? sm.buf[i] : 0ull;
+    }
+  }
+}
+
+// Joins the slices of a row.
+template <int T, bool TOP>
+__global__ void __launch_bounds__(kLpThreads) k_logprob_join(LogprobArgs a) {
+  __shared__ SelectSmem sm;
+  __shared__ SoftSum parts[kLpThreads / 64];
+  __shared__ float lz_s;
+  const int tid = threadIdx.x;
+  const int64_t row = blockIdx.x;
+  const float c = a.scale * kLog2e;
+  SoftSum s{-__builtin_inff(), 0.f, 0.f};
+  if (tid < a.slices) s = a.sums[row * a.slices + tid];
+  s = soft_join_wave(s, c);
+  if ((tid & 63) == 0) parts[tid >> 6] = s;
+  if (tid == 0) sm.count = 0u;
+  __syncthreads();
+  s = parts[0];
+#pragma unroll
+  for (int i = 1; i < kLpThreads / 64; ++i) s = soft_join(s, parts[i], c);
+  if (tid == 0) lz_s = emit_row<T>(a, row, s);
+  if constexpr (TOP) {
+    for (int i = tid; i < a.slices * a.k; i += kLpThreads) {
+      const uint64_t e = a.cands[row * a.slices * a.k + i];
+      if (e) sm.buf[atomicAdd(&sm.count, 1u)] = e;   // slices * k <= kSelCap
+    }
+    __syncthreads();
+    emit_top(a, row, sm, int(sm.count), s.m, lz_s);
+  }
+}
+
+template <int T>
+__global__ void __launch_bounds__(256) k_logprob_backward(const void *scores, int64_t rows, int64_t n, int64_t stride,
+                                                          float scale, const int64_t *__restrict__ target,
+                                                          const float *__restrict__ stats,
+                                                          const float *__restrict__ entropy,
+                                                          const float *__restrict__ dlogprob,
+                                                          const float *__restrict__ dentropy, void *out,
+                                                          int64_t ostride, int64_t pieces) {
+  for (int64_t at = blockIdx.x; at < rows * pieces; at += gridDim.x) {
+    const int64_t row = at / pieces;
+    const int64_t j0 = ((at - row * pieces) * 256 + threadIdx.x) * 8;
+    if (j0 >= n) continue;
+    const typename FloatType<T>::type *x = static_cast<const typename FloatType<T>::type *>(scores) + row * stride;
+    const int left = int(n - j0 < 8 ? n - j0 : 8);
+    float v[8];
+    load_float8<T>(v, x + j0, 0, left);
+    const int64_t t = target ? target[row] : -1;
+    const float m = stats[2 * row], lz = stats[2 * row + 1];
+    const float dl = dlogprob && t >= 0 && t < n ? dlogprob[row] : 0.f;
+    const float dh = dentropy ? dentropy[row] : 0.f, h = dentropy ? entropy[row] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      // 2^24 p, so that a p below float32's normal range keeps its digits
+      const float lp = fmaf(v[i] - m, scale, -lz);
+      const float p = __builtin_amdgcn_exp2f(fmaf(lp, kLog2e, 24.f));
+      const float q = p * ((dl + dh * (fmaxf(lp, -1e4f) + h)) * scale);
+      const float d = fmaf(q, -0x1p-24f, j0 + i == t ? dl * scale : 0.f);
+      v[i] = v[i] * scale == -__builtin_inff() ? 0.f : d;
+    }
+    store_float8<T>(v, static_cast<typename FloatType<T>::type *>(out) + row * ostride + j0, 0, left);
+  }
+}
+
+// Slices of a row: enough workgroups for the GPU where there are few rows, at
+// least two pieces each, and no more candidates than the join's buffer holds.
+static int logprob_slices(int64_t m, int64_t n, int k) {
+  int64_t s = (512 + m - 1) / m;
+  const int64_t most = (n + 2 * kLpPiece - 1) / (2 * kLpPiece);
+  if (s > most) s = most;
+  if (s > kLpMaxSlices) s = kLpMaxSlices;
+  if (k > 0 && s > kSelCap / k) s = kSelCap / k;
+  return int(s < 1 ? 1 : s);
+}
+static size_t logprob_sums_bytes(int64_t m, int slices) {
+  return (size_t(m) * slices * sizeof(SoftSum) + 255) / 256 * 256;
+}
+
+template <int T>
+static void launch_logprob(const LogprobArgs &a, hipStream_t s) {
+  const dim3 grid(unsigned(a.m * a.slices)), rows(unsigned(a.m)), threads(kLpThreads);
+  if (a.k > 0) {
+    hipLaunchKernelGGL((k_logprob<T, true>), grid, threads, 0, s, a);
+    if (a.slices > 1) hipLaunchKernelGGL((k_logprob_join<T, true>), rows, threads, 0, s, a);
+  } else {
+    hipLaunchKernelGGL((k_logprob<T, false>), grid, threads, 0, s, a);
+    if (a.slices > 1) hipLaunchKernelGGL((k_logprob_join<T, false>), rows, threads, 0, s, a);
+  }
+}
+
+static bool logprob_sizes_ok(int64_t m, int64_t n, int k) {
+  return m >= 0 && n >= 1 && m <= 0x7fffffff / kLpMaxSlices && n <= 0x7fffffff && k >= 0 && k <= kMaxK;
+}
+static bool scale_ok(float scale) { return scale > 0.f && scale < __builtin_inff(); }
+
+}  // namespace rslm
+
+using namespace rslm;
+
+extern "C" {
+
+size_t rslm_logprob_workspace(int64_t m, int64_t n, int32_t k) {
+  if (!logprob_sizes_ok(m, n, k) || m == 0) return 0;
+  const int s = logprob_slices(m, n, k);
+  return s > 1 ? logprob_sums_bytes(m, s) + size_t(m) * s * k * sizeof(uint64_t) : 0;
+}
+
+int rslm_logprob(const void *scores, int32_t dtype, int64_t m, int64_t n, int64_t stride, float scale,
+                 const int64_t *target, int32_t k, float *logprob, float *lse, float *entropy, float *stats,
+                 float *top_logprob, int32_t *top_ids, void *ws, size_t ws_bytes, void *stream) {
+  if (!logprob_sizes_ok(m, n, k) || !float_type_ok(dtype) || stride < 0 || !scale_ok(scale))
+    return RSLM_ERR_INVALID_ARG;
+  if (m == 0) return RSLM_OK;
+  if (!scores || !stats || (logprob && !target) || (k > 0 && (!top_logprob || !top_ids)) ||
+      !aligned_to(scores, float_bytes(dtype)) || !aligned_to(target, 8) || !aligned_to(logprob, 4) ||
+      !aligned_to(lse, 4) || !aligned_to(entropy, 4) || !aligned_to(stats, 4) || !aligned_to(top_logprob, 4) || !aligned_to(top_ids, 4))
+    return RSLM_ERR_INVALID_ARG;
+  LogprobArgs a{scores, m, n, stride, scale, target, k, logprob, lse, entropy, stats, top_logprob, top_ids};
+  a.slices = logprob_slices(m, n, k);
+  if (ws_bytes < rslm_logprob_workspace(m, n, k)) return RSLM_ERR_WORKSPACE;
+  if (a.slices > 1) {
+    if (!ws || !aligned_to(ws, 16)) return RSLM_ERR_INVALID_ARG;
+    a.sums = static_cast<SoftSum *>(ws);
+    a.cands = reinterpret_cast<uint64_t *>(static_cast<char *>(ws) + logprob_sums_bytes(m, a.slices));
+  }
+  a.per = (n + int64_t(a.slices) * kLpPiece - 1) / (int64_t(a.slices) * kLpPiece) * kLpPiece;
+  const hipStream_t s = as_stream(stream);
+  if (dtype == RSLM_F32) launch_logprob<RSLM_F32>(a, s);
+  else if (dtype == RSLM_F16) launch_logprob<RSLM_F16>(a, s);
+  else launch_logprob<RSLM_BF16>(a, s);
+  return check_launch();
+}
+
+int rslm_logprob_backward(const void *scores, int32_t dtype, int64_t m, int64_t n, int64_t stride, float scale,
+                          const int64_t *target, const float *stats, const float *entropy, const float *dlogprob,
+                          const float *dentropy, void *dscores, int64_t dstride, void *stream) {
+  if (!logprob_sizes_ok(m, n, 0) || !float_type_ok(dtype) || stride < 0 || (m > 1 && dstride < n) ||
+      !scale_ok(scale))
+    return RSLM_ERR_INVALID_ARG;
+  if (m == 0) return RSLM_OK;
+  if (!scores || !stats || !dscores || (dlogprob && !target) || (dentropy && !entropy) ||
+      !aligned_to(scores, float_bytes(dtype)) || !aligned_to(dscores, float_bytes(dtype)) || !aligned_to(target, 8) ||
+      !aligned_to(stats, 4) || !aligned_to(entropy, 4) || !aligned_to(dlogprob, 4) || !aligned_to(dentropy, 4))
+    return RSLM_ERR_INVALID_ARG;
+  const int64_t pieces = (n + 2047) / 2048;
+  const dim3 grid(unsigned(m * pieces < (1 << 22) ? m * pieces : (1 << 22)));
+  const hipStream_t s = as_stream(stream);
+#define RSLM_LOGPROB_BACKWARD(T)                                                                                  \
+  hipLaunchKernelGGL(k_logprob_backward<T>, grid, dim3(256), 0, s, scores, m, n, stride, scale, target, stats,    \
+                     entropy, dlogprob, dentropy, dscores, dstride, pieces)
+  if (dtype == RSLM_F32) RSLM_LOGPROB_BACKWARD(RSLM_F32);
+  else if (dtype == RSLM_F16) RSLM_LOGPROB_BACKWARD(RSLM_F16);
+  else RSLM_LOGPROB_BACKWARD(RSLM_BF16);
+#undef RSLM_LOGPROB_BACKWARD
+  return check_launch();
+}
+
+}  // extern "C"

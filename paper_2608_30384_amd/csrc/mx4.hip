@@ -1,0 +1,327 @@
+// Quantisation of float rows to MX4 rows (mx4_dev.h), with the rotation of
+// rotate.hip in the same pass where a plan asks for it, and back to floats.
+//
+// Both directions are bound by memory: a row of D float32 is read (4 D bytes)
+// and 0.53 D bytes are written, or the reverse.  16 lanes take 128
+// coordinates, 8 consecutive ones each: one 16- or 32-byte load, one 4-byte
+// word of codes, and the 32 coordinates of a scale are those of four adjacent
+// lanes, whose largest magnitude is found by two exchanges inside the quad.
+#include "mx4_dev.h"
+#include "rows_dev.h"
+
+namespace rslm {
+
+// The largest of the values of the four lanes of a quad.
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+  v = max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), kDppQuadXor1, 0xf, 0xf, true)));
+  return max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), kDppQuadXor2, 0xf, 0xf, true)));
+}
+
+// One group of 128 coordinates: lane r of 16 holds coordinates 8 r + i and
+// writes their codes; the first lane of each quad writes its scale.
+__device__ __forceinline__ void mx4_put8(const float (&x)[8], uint8_t *codes, uint8_t *scales, int r) {
+  uint32_t top = 0u;
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    v[i] = x[i] + 0.f;   // -0 to +0: the sign of a cancelled sum depends on its order
+    top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+  }
+  const uint32_t s = e8m0_code(quad_max(top));
+  *reinterpret_cast<uint32_t *>(codes + 4 * r) = mx4_codes8(v, s);
+  if ((r & 3) == 0) scales[r >> 2] = uint8_t(s);
+}
+
+// U groups of 128 coordinates of a row by each 16 lanes; blockIdx.y: which U.
+template <int T, int U>
+__global__ void __launch_bounds__(256) k_mx4_quantize(const void *__restrict__ x, int64_t n, int dim,
+                                                      int64_t stride, int steps,
+                                                      uint8_t *__restrict__ codes,
+                                                      uint8_t *__restrict__ scales) {
+  const int r = threadIdx.x & 15;
+  const int t0 = blockIdx.y * U;
+  // whole groups of 16 lanes leave together
+  for (int64_t row = int64_t(blockIdx.x) * 16 + (threadIdx.x >> 4); row < n; row += int64_t(gridDim.x) * 16) {
+    const typename FloatType<T>::type *xr = static_cast<const typename FloatType<T>::type *>(x) + row * stride;
+    float v[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_float8<T>(v[u], xr, 128 * (t0 + u) + 8 * r, dim);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (t0 + u < steps)
+        mx4_put8(v[u], codes + (row * steps + t0 + u) * 64, scales + (row * steps + t0 + u) * 4, r);
+  }
+}
+
+template <int T, int U>
+__global__ void __launch_bounds__(256) k_mx4_dequantize(const uint8_t *__restrict__ codes,
+                                                        const uint8_t *__restrict__ scales, int64_t n,
+                                                        int dim, int steps, void *__restrict__ out,
+                                                        int64_t stride) {
+  const int r = threadIdx.x & 15;
+  const int t0 = blockIdx.y * U;
+  for (int64_t row = int64_t(blockIdx.x) * 16 + (threadIdx.x >> 4); row < n; row += int64_t(gridDim.x) * 16) {
+    typename FloatType<T>::type *orow = static_cast<typename FloatType<T>::type *>(out) + row * stride;
+    uint32_t w[U], s[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t g = row * steps + min(t0 + u, steps - 1);
+      w[u] = *reinterpret_cast<const uint32_t *>(codes + g * 64 + 4 * r);
+      s[u] = scales[g * 4 + (r >> 2)];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float v[8];
+      mx4_values8(v, w[u], s[u]);
+      store_float8<T>(v, orow, 128 * (t0 + u) + 8 * r, dim);
+    }
+  }
+}
+
+__device__ __forceinline__ void load_float8_any(float (&v)[8], const void *row, int c, int dim, int dtype) {
+  if (dtype == RSLM_F32) load_float8<RSLM_F32>(v, row, c, dim);
+  else if (dtype == RSLM_F16) load_float8<RSLM_F16>(v, row, c, dim);
+  else load_float8<RSLM_BF16>(v, row, c, dim);
+}
+
+// Rotate and quantise, D >= 128: the rotation runs in registers on 16-lane
+// rows (rows_dev.h), whose lanes end with 8 consecutive coordinates of each of
+// their blocks, as the quantiser takes them.  Every pass is scaled as it ends,
+// so the coordinates, and with them the codes, have the bits of rslm_fwht's.
+template <int RPV, int NBR, bool FULL>
+__global__ void __launch_bounds__(256, NBR <= 4 ? 4 : 2) k_mx4_quantize_rot(
+    const void *__restrict__ x, int dtype, int64_t n, int64_t stride, uint8_t *__restrict__ codes,
+    uint8_t *__restrict__ scales, RotParams rp) {
+  constexpr int VPW = 4 / RPV;
+  extern __shared__ float4 lds4[];
+  __shared__ __align__(16) uint32_t s1[kSignWords];
+  const int D = rp.D, steps = mx4_steps(D);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int vstride = rows_stride(D);
+  float *lds = reinterpret_cast<float *>(lds4);
+  uint16_t *ts = reinterpret_cast<uint16_t *>(lds + 4 * VPW * vstride);
+  RowsTs<128 * RPV * NBR> tload;
+  tload.load(rp);
+  RowsSigns signs;
+  signs.load(rp);
+  tload.store(ts, rp, signs, false);
+  signs.fill(s1, rp);
+  __syncthreads();
+  const int64_t n_groups = (n + VPW - 1) / VPW;
+  for (int64_t grp = int64_t(blockIdx.x) * 4 + wid; grp < n_groups; grp += int64_t(gridDim.x) * 4) {
+    int olane = lane;   // opaque: nothing derived from it is kept across the loop
+    asm volatile("" : "+v"(olane));
+    const RowsLane<RPV> ln(olane);
+    const int64_t row = grp * VPW + ln.vslot;
+    if (row >= n) continue;   // the lanes of this vector sit out; no workgroup barrier follows
+    float *vb = lds + (wid * VPW + ln.vslot) * vstride;
+    const char *xr = static_cast<const char *>(x) + row * stride * float_bytes(dtype);
+    float z[8 * NBR];
+#pragma unroll
+    for (int j = 0; j < NBR; ++j) {
+      float v[8];
+      load_float8_any(v, xr, 128 * (j * RPV + ln.pv) + 8 * ln.r, D, dtype);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z[8 * j + i] = v[i];
+    }
+#pragma unroll
+    for (int j = 0; j < NBR; ++j) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = z[8 * j + i];
+      rows_flip(v, s1, j * RPV + ln.pv, ln.r);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z[8 * j + i] = v[i];
+    }
+    rows_forward<RPV, NBR, FULL>(z, rp, ts, vb, ln, true);
+#pragma unroll
+    for (int j = 0; j < NBR; ++j) {
+      const int b = j * RPV + ln.pv;
+      if (FULL || b < steps) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = z[8 * j + i];
+        mx4_put8(v, codes + (row * steps + b) * 64, scales + (row * steps + b) * 4, ln.r);
+      }
+    }
+  }
+}
+
+// Rotate and quantise, D < 128 (one group): the vector in LDS, 16 lanes to a
+// vector, one butterfly of a stage after another.  B is the largest power of
+// two up to D; the stages of all whole blocks run together, then those of the
+// block that ends at D.
+__global__ void __launch_bounds__(256) k_mx4_quantize_rot_small(const void *__restrict__ x, int dtype,
+                                                                int64_t n, int64_t stride,
+                                                                uint8_t *__restrict__ codes,
+                                                                uint8_t *__restrict__ scales,
+                                                                RotParams rp) {
+  __shared__ __align__(16) float buf[16][132];
+  const int D = rp.D, B = rp.B, r = threadIdx.x & 15;
+  float *b = buf[threadIdx.x >> 4];
+  for (int64_t row = int64_t(blockIdx.x) * 16 + (threadIdx.x >> 4); row - (threadIdx.x >> 4) < n;
+       row += int64_t(gridDim.x) * 16) {
+    const bool live = row < n;   // a wavefront's lanes stay together
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    if (live) load_float8_any(v, static_cast<const char *>(x) + row * stride * float_bytes(dtype), 8 * r, D, dtype);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b[8 * r + i] = v[i] * rp.s1[8 * r + i];
+    wave_sync_r();
+    for (int pass = 0; pass < rp.passes; ++pass) {
+      if (pass == 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int o = 8 * r + i;
+          v[i] = o < D ? b[rp.tsrc[o]] * rp.s1[(o + 127) & 255] : 0.f;
+        }
+        wave_sync_r();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[8 * r + i] = v[i];
+        wave_sync_r();
+      }
+      for (int part = 0; part <= rp.overlap; ++part) {
+        float *p = part ? b + D - B : b;
+        const int pairs = part ? B >> 1 : (rp.n_full * B) >> 1;
+        for (int h = 1; h < B; h <<= 1) {
+          const float scale = 2 * h == B ? rp.inv_sqrt_b : 1.f;
+          for (int t = r; t < pairs; t += 16) {
+            const int i = ((t & ~(h - 1)) << 1) | (t & (h - 1));
+            const float a = p[i], c = p[i + h];
+            p[i] = (a + c) * scale;
+            p[i + h] = (a - c) * scale;
+          }
+          wave_sync_r();
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 8 * r + i < D ? b[8 * r + i] : 0.f;
+    if (live) mx4_put8(v, codes + row * 64, scales + row * 4, r);
+    wave_sync_r();
+  }
+}
+
+// Groups of 128 coordinates that 16 lanes take: as many as divide a row with
+// the fewest left over, up to four.
+static int groups_each(int steps) {
+  int best = 1, waste = steps;
+  for (int u = 4; u >= 1; --u) {
+    const int over = (steps + u - 1) / u * u - steps;
+    if (over < waste) waste = over, best = u;
+  }
+  return best;
+}
+
+// Workgroups over n rows, 16 rows each; they stride over more rows than a grid
+// can count.
+static unsigned row_groups(int64_t n) {
+  const int64_t g = (n + 15) / 16;
+  return unsigned(g < (1 << 20) ? g : (1 << 20));
+}
+
+#define RSLM_MX4_TYPES(DTYPE, CALL) \
+  switch (DTYPE) {                  \
+    case RSLM_F32: CALL(RSLM_F32); break;   \
+    case RSLM_F16: CALL(RSLM_F16); break;   \
+    default: CALL(RSLM_BF16);               \
+  }
+#define RSLM_MX4_GROUPS(T, U, CALL) \
+  switch (U) {                      \
+    case 1: CALL(T, 1); break;      \
+    case 2: CALL(T, 2); break;      \
+    case 3: CALL(T, 3); break;      \
+    default: CALL(T, 4);            \
+  }
+
+struct QuantizeCall {
+  const void *x;
+  int dtype;
+  int64_t n, stride;
+  uint8_t *codes, *scales;
+  hipStream_t s;
+};
+
+template <int RPV, int NBR, bool FULL>
+static void launch_quantize_rot_one(const rslm_plan *p, const QuantizeCall &c) {
+  const size_t shm = size_t(16 / RPV) * rows_stride(p->rot.D) * 4 + 128 * RPV * NBR * 2;
+  constexpr auto kernel = k_mx4_quantize_rot<RPV, NBR, FULL>;
+  const int64_t groups = (c.n + 16 / RPV - 1) / (16 / RPV);
+  hipLaunchKernelGGL(kernel, dim3(rows_grid<kernel>(shm, groups)), dim3(256), shm, c.s, c.x, c.dtype,
+                     c.n, c.stride, c.codes, c.scales, p->rot);
+}
+
+static void launch_quantize_rot(const rslm_plan *p, const QuantizeCall &c) {
+  const int D = p->rot.D;
+  if (!rows_ok(p->rot)) {
+    hipLaunchKernelGGL(k_mx4_quantize_rot_small, dim3(row_groups(c.n)), dim3(256), 0, c.s, c.x,
+                       c.dtype, c.n, c.stride, c.codes, c.scales, p->rot);
+    return;
+  }
+#define RSLM_QUANT_ROWS(RPV, NBR)                                              \
+  {                                                                            \
+    if (rows_only_full(RPV, NBR) || D == 128 * RPV * NBR)                      \
+      launch_quantize_rot_one<RPV, NBR, true>(p, c);                           \
+    else                                                                       \
+      launch_quantize_rot_one<RPV, NBR, rows_only_full(RPV, NBR)>(p, c);       \
+  }
+  const int nbt = rows_blocks(p->rot);
+  RSLM_ROWS_SWITCH(nbt, D == 384, RSLM_QUANT_ROWS)
+#undef RSLM_QUANT_ROWS
+}
+
+}  // namespace rslm
+
+using namespace rslm;
+
+extern "C" {
+
+int rslm_mx4_quantize(const rslm_plan *plan, const void *x, int32_t dtype, int64_t n, int32_t dim,
+                      int64_t stride, uint8_t *codes, uint8_t *scales, void *stream) {
+  if (n < 0 || n > kMx4MaxRows || dim < 1 || dim > kMx4MaxDim || !float_type_ok(dtype) || stride < 0)
+    return RSLM_ERR_INVALID_ARG;
+  if (plan && plan->rot.D != dim) return RSLM_ERR_INVALID_ARG;
+  if (n == 0) return RSLM_OK;
+  if (!x || !codes || !scales || !aligned_to(x, float_bytes(dtype)) || !aligned_to(codes, 16) ||
+      !aligned_to(scales, 4))
+    return RSLM_ERR_INVALID_ARG;
+  const hipStream_t s = as_stream(stream);
+  if (plan && plan->rot.passes > 0) {
+    launch_quantize_rot(plan, QuantizeCall{x, dtype, n, stride, codes, scales, s});
+    return check_launch();
+  }
+  const int steps = mx4_steps(dim), u = groups_each(steps);
+  const dim3 grid(row_groups(n), unsigned((steps + u - 1) / u));
+#define RSLM_QUANT(T, U) \
+  hipLaunchKernelGGL((k_mx4_quantize<T, U>), grid, dim3(256), 0, s, x, n, dim, stride, steps, codes, scales)
+#define RSLM_QUANT_T(T) RSLM_MX4_GROUPS(T, u, RSLM_QUANT)
+  RSLM_MX4_TYPES(dtype, RSLM_QUANT_T)
+#undef RSLM_QUANT_T
+#undef RSLM_QUANT
+  return check_launch();
+}
+
+int rslm_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t n, int32_t dim, void *out,
+                        int32_t dtype, int64_t stride, void *stream) {
+  if (n < 0 || n > kMx4MaxRows || dim < 1 || dim > kMx4MaxDim || !float_type_ok(dtype) ||
+      (n > 1 && stride < dim))
+    return RSLM_ERR_INVALID_ARG;
+  if (n == 0) return RSLM_OK;
+  if (!out || !codes || !scales || !aligned_to(out, float_bytes(dtype)) || !aligned_to(codes, 16) ||
+      !aligned_to(scales, 4))
+    return RSLM_ERR_INVALID_ARG;
+  const hipStream_t s = as_stream(stream);
+  const int steps = mx4_steps(dim), u = groups_each(steps);
+  const dim3 grid(row_groups(n), unsigned((steps + u - 1) / u));
+#define RSLM_DEQUANT(T, U) \
+  hipLaunchKernelGGL((k_mx4_dequantize<T, U>), grid, dim3(256), 0, s, codes, scales, n, dim, steps, out, stride)
+#define RSLM_DEQUANT_T(T) RSLM_MX4_GROUPS(T, u, RSLM_DEQUANT)
+  RSLM_MX4_TYPES(dtype, RSLM_DEQUANT_T)
+#undef RSLM_DEQUANT_T
+#undef RSLM_DEQUANT
+  return check_launch();
+}
+
+}  // extern "C"
