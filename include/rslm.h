@@ -500,18 +500,23 @@ int rslm_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t n, 
  * rslm_mx4_score_backward: its gradient with respect to x,
  *   dx[i][d] = sum_j dout[i][j] b_j[d],
  *   dout: m rows of n, type dtype, stride >= 0; dx: m rows of dim, float32 or
- *   dout's type, dx_stride >= dim.  The workspace holds partial sums (float32,
- *   joined in a fixed order: results do not change from call to call).
+ *   dout's type, dx_stride >= dim.  Its sums are split and joined in a fixed
+ *   order: results do not change from call to call.
+ * The workspaces (16-byte aligned) hold x or dout as the kernels multiply them,
+ * and the partial sums.  Without a need for the former (few rows, and bfloat16
+ * rows aligned to 16 bytes of a multiple of 128 values, not overlapping) as much
+ * less is accepted.
  * m <= 8,388,480 for the last two.  A row of b with a NaN scale makes its
  * products NaN.
  * ------------------------------------------------------------------------ */
 int rslm_mx4_matmul(const uint8_t *a_codes, const uint8_t *a_scales, int64_t m, const uint8_t *b_codes,
                     const uint8_t *b_scales, int64_t n, int32_t dim, void *out, int32_t dtype, int64_t stride,
                     void *stream);
+size_t rslm_mx4_score_workspace(int64_t m, int64_t n, int32_t dim, int32_t dtype);
 int rslm_mx4_score(const void *x, int32_t dtype, int64_t m, int64_t stride, const uint8_t *codes,
                    const uint8_t *scales, int64_t n, int32_t dim, void *out, int32_t out_dtype, int64_t out_stride,
-                   void *stream);
-size_t rslm_mx4_score_backward_workspace(int64_t m, int64_t n, int32_t dim);
+                   void *ws, size_t ws_bytes, void *stream);
+size_t rslm_mx4_score_backward_workspace(int64_t m, int64_t n, int32_t dim, int32_t dtype);
 int rslm_mx4_score_backward(const void *dout, int32_t dtype, int64_t m, int64_t stride, const uint8_t *codes,
                             const uint8_t *scales, int64_t n, int32_t dim, void *dx, int32_t dx_dtype,
                             int64_t dx_stride, void *ws, size_t ws_bytes, void *stream);

@@ -32,7 +32,7 @@ EXPORTS = [
     "rslm_scan_topk_workspace", "rslm_scan_topk", "rslm_workspace_size",
     "rslm_sq8_fit", "rslm_sq8_encode", "rslm_rescore", "rslm_set_timer", "rslm_calibrate_read",
     "rslm_grid2_lists",
-    "rslm_mx4_quantize", "rslm_mx4_dequantize", "rslm_mx4_matmul", "rslm_mx4_score",
+    "rslm_mx4_quantize", "rslm_mx4_dequantize", "rslm_mx4_matmul", "rslm_mx4_score_workspace", "rslm_mx4_score",
     "rslm_mx4_score_backward_workspace", "rslm_mx4_score_backward",
     "rslm_logprob_workspace", "rslm_logprob", "rslm_logprob_backward",
 ]
@@ -111,8 +111,9 @@ def _declare(lib):
         "rslm_mx4_quantize": (C.c_int, [P, P, I32, I64, I32, I64, P, P, P]),
         "rslm_mx4_dequantize": (C.c_int, [P, P, I64, I32, P, I32, I64, P]),
         "rslm_mx4_matmul": (C.c_int, [P, P, I64, P, P, I64, I32, P, I32, I64, P]),
-        "rslm_mx4_score": (C.c_int, [P, I32, I64, I64, P, P, I64, I32, P, I32, I64, P]),
-        "rslm_mx4_score_backward_workspace": (SZ, [I64, I64, I32]),
+        "rslm_mx4_score_workspace": (SZ, [I64, I64, I32, I32]),
+        "rslm_mx4_score": (C.c_int, [P, I32, I64, I64, P, P, I64, I32, P, I32, I64, P, SZ, P]),
+        "rslm_mx4_score_backward_workspace": (SZ, [I64, I64, I32, I32]),
         "rslm_mx4_score_backward": (C.c_int, [P, I32, I64, I64, P, P, I64, I32, P, I32, I64, P,
                                               SZ, P]),
         "rslm_logprob_workspace": (SZ, [I64, I64, I32]),

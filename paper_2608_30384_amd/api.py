@@ -559,9 +559,11 @@ def rslm_mx4_score(x, b, dtype=torch.float32, out=None, stream=None):
     _same_device(x, b, "b")
     out, ocode, ostride = _out_rows(out, (x.shape[0], b.n), dtype, x.device)
     _same_device(x, out, "out")
+    nb = L.lib().rslm_mx4_score_workspace(x.shape[0], b.n, b.dim, code)
+    ws = _WS.get(nb, x.device, "mx4_score", stream)
     L.check("rslm_mx4_score", L.lib().rslm_mx4_score(
         _ptr(x), code, x.shape[0], stride, _ptr(b.codes), _ptr(b.scales), b.n, b.dim, _ptr(out),
-        ocode, ostride, _stream(stream)))
+        ocode, ostride, _ptr(ws), ws.numel(), _stream(stream)))
     return out
 
 
@@ -575,7 +577,7 @@ def rslm_mx4_score_backward(dout, b, dtype=None, out=None, stream=None):
     m = dout.shape[0]
     out, ocode, ostride = _out_rows(out, (m, b.dim), dout.dtype if dtype is None else dtype, dout.device)
     _same_device(dout, out, "out")
-    nb = L.lib().rslm_mx4_score_backward_workspace(m, b.n, b.dim)
+    nb = L.lib().rslm_mx4_score_backward_workspace(m, b.n, b.dim, code)
     ws = _WS.get(nb, dout.device, "mx4_backward", stream)
     L.check("rslm_mx4_score_backward", L.lib().rslm_mx4_score_backward(
         _ptr(dout), code, m, stride, _ptr(b.codes), _ptr(b.scales), b.n, b.dim, _ptr(out), ocode,

@@ -177,6 +177,41 @@ __device__ __forceinline__ uint4 mx4_bf16x8(uint32_t w, float a) {
                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, a, 3)));
 }
 
+// ---- loads from memory to LDS, which go past the registers
+
+__device__ __forceinline__ i32x4 buffer_of(const uint8_t *p, int64_t bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(p);
+  i32x4 r;
+  r[0] = __builtin_amdgcn_readfirstlane(int(a));
+  r[1] = __builtin_amdgcn_readfirstlane(int(a >> 32) & 0xffff);
+  r[2] = __builtin_amdgcn_readfirstlane(int(bytes > 0xffffffffll ? 0xffffffffll : bytes));
+  r[3] = 0x00020000;   // raw, 32-bit; reads past the end give 0
+  return r;
+}
+// 64 lanes x 16 bytes from the buffer to LDS, lane l's at lds + 16 l.
+// The whole offset is the lane's, which the end of the buffer is checked against.
+__device__ __forceinline__ void load_to_lds(i32x4 buf, uint32_t lds, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :
+               : "s"(lds), "v"(offset), "s"(buf)
+               : "memory");
+}
+// The same from 64 addresses, one of each lane.
+__device__ __forceinline__ void load_to_lds(const void *p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(p) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+  return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char *)p));
+}
+// At most N of the wavefront's loads are still out, and its LDS reads are done;
+// then every wavefront's.
+template <int N>
+__device__ __forceinline__ void arrive() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+// The wavefront's LDS writes and reads are done; then every wavefront's.
+__device__ __forceinline__ void arrive_lds() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 inline bool float_type_ok(int dtype) {
   return dtype == RSLM_F32 || dtype == RSLM_F16 || dtype == RSLM_BF16;
 }

@@ -119,15 +119,19 @@ def test_mx4_calls_validate_arguments_without_device():
                 (P, P, 4, P, Z, 4, 96, P, 0, 4), (P, P, 4, P, P, 4, 96, Z, 0, 4), (P, P, 1 << 23, P, P, 4, 96, P, 0, 4)]:
         assert mm(*bad, Z) == 1, bad
     sc = lib.rslm_mx4_score
-    assert sc(Z, 0, 0, 96, P, P, 4, 96, P, 0, 4, Z) == 0 and sc(P, 0, 4, 96, Z, Z, 0, 96, P, 0, 4, Z) == 0
-    assert sc(P, 1, 4, 96, P, P, 4, 96, P, 2, 4, Z) == 2 and sc(P, 0, 4, 96, P, P, 4, 96, P, 1, 4, Z) == 2
+    assert sc(Z, 0, 0, 96, P, P, 4, 96, P, 0, 4, Z, 0, Z) == 0 and sc(P, 0, 4, 96, Z, Z, 0, 96, P, 0, 4, Z, 0, Z) == 0
+    assert sc(P, 1, 4, 96, P, P, 4, 96, P, 2, 4, Z, 0, Z) == 2 and sc(P, 0, 4, 96, P, P, 4, 96, P, 1, 4, Z, 0, Z) == 2
+    need = lib.rslm_mx4_score_workspace(100, 1000, 96, 0)
+    assert need > 0 and lib.rslm_mx4_score_workspace(1, 1000, 96, 0) == 0 and lib.rslm_mx4_score_workspace(100, 1000, 96, 9) == 0
+    assert sc(P, 0, 100, 96, P, P, 1000, 96, P, 0, 1000, P, need - 1, Z) == 4
+    assert sc(P, 0, 100, 96, P, P, 1000, 96, P, 0, 1000, ODD, need, Z) == 1
     for bad in [(P, 7, 4, 96, P, P, 4, 96, P, 0, 4), (P, 0, 4, -96, P, P, 4, 96, P, 0, 4), (Z, 0, 4, 96, P, P, 4, 96, P, 0, 4),
                 (P, 0, 4, 96, P, P, 4, 96, P, 0, 3), (P, 0, 4, 96, ODD, P, 4, 96, P, 0, 4), (P, 0, 4, 96, P, P, 4, 70000, P, 0, 4)]:
-        assert sc(*bad, Z) == 1, bad
+        assert sc(*bad, P, 1 << 30, Z) == 1, bad
     bw = lib.rslm_mx4_score_backward
-    need = lib.rslm_mx4_score_backward_workspace(256, 131072, 768)
-    assert need > 0 and need % (256 * 768 * 4) == 0
-    assert lib.rslm_mx4_score_backward_workspace(0, 131072, 768) == 0
+    need = lib.rslm_mx4_score_backward_workspace(256, 131072, 768, 0)
+    assert need > 0
+    assert lib.rslm_mx4_score_backward_workspace(0, 131072, 768, 0) == 0
     assert bw(P, 0, 256, 131072, P, P, 131072, 768, P, 0, 768, P, need - 1, Z) == 4
     assert bw(P, 0, 256, 131072, P, P, 131072, 768, P, 0, 768, Z, need, Z) == 1
     assert bw(P, 0, 256, 131072, P, P, 131072, 768, P, 0, 767, P, need, Z) == 1
