@@ -7,11 +7,20 @@
 // of the entries it reads, Z = sum w and W = sum w y with y = (score - maximum)
 // scale log2(e) and w = 2^y, and rescales them when its maximum rises; the
 // threads' are joined at the end (lse = maximum scale + ln Z, entropy = ln Z - ln2 W / Z).
-// The k largest come from the same pass: entries at or above a threshold, the
-// k-th largest known so far, go to a buffer in LDS, which is cut back to its k
-// best when it fills.  The first threshold is the k-th largest of the threads'
-// own maxima, which at least k entries reach.  Few rows are cut into slices,
-// joined by a second kernel.
+// The k largest come from the same pass.  The k-th largest of the threads' running
+// maxima is a value that at least k entries reach; a
+// thread whose piece of 16 entries reaches the one known so far notes the piece
+// in LDS.  At the end the noted pieces are read again (from the cache) for the
+// entries at or above the last such value, about k, which are ranked.  A row
+// that overflows the notes (one that ascends, say) is gone through once more, a
+// few entries at a time.  Few rows are cut into slices, joined by a second
+// kernel.
+// 4,096 x 32,768 bfloat16: 53 us without alternatives (5.1 TB/s), 73 with k = 10;
+// 97 where the bound came of ranking 64 parts' maxima, lane by lane, and 104 where
+// every entry at or above the first piece's bound went to the candidates at once.
+// 1 x 131,072 float32, k = 5: 7.4 us in 32 slices and 9.5 for the join, both the
+// latency of their barriers and reads.  Backward, 4,096 x 32,768 bfloat16: 112 us,
+// 4.8 TB/s read and written.
 //
 // An entry of -infinity (or one that scale makes so) is masked: probability 0,
 // no alternative, gradient 0.  A row of nothing else has lse -infinity and
@@ -26,6 +35,7 @@ constexpr int kLpThreads = 256;
 constexpr int kLpEach = 16;                          // entries of a thread in a piece
 constexpr int kLpPiece = kLpThreads * kLpEach;
 constexpr int kLpMaxSlices = 256;
+constexpr int kLpNotes = 1024;
 
 // Running maximum (of the scores) and sums of part of a row.
 struct SoftSum {
@@ -67,8 +77,10 @@ struct LogprobArgs {
   int32_t *top_ids;
   int slices;
   int64_t per;          // entries of a slice, a multiple of kLpPiece
+  int room;             // entries that a slice may leave, at least k
   SoftSum *sums;        // m x slices
-  uint64_t *cands;      // m x slices x k, 0: none
+  uint64_t *cands;      // m x slices x room
+  int32_t *counts;      // m x slices
 };
 
 // z - lse of a score, from the row's largest and ln Z: exact to the last places
@@ -100,6 +112,8 @@ __device__ __forceinline__ float emit_row(const LogprobArgs &a, int64_t row, con
 }
 
 // The k best of the cnt composites in sm.buf, in order, as log probabilities.
+// Up to 1,024 entries, an entry's place is the number of larger ones (no two are
+// equal): one read of all by every thread, instead of a sort's barriers.
 __device__ __forceinline__ void emit_top(const LogprobArgs &a, int64_t row, SelectSmem &sm, int cnt, float m, float lz) {
   const int t = threadIdx.x, k = a.k;
   float *os = a.top_logprob + row * k;
@@ -109,13 +123,25 @@ __device__ __forceinline__ void emit_top(const LogprobArgs &a, int64_t row, Sele
     os[r] = log_of(v, m, lz, a.scale);
     oi[r] = v * a.scale == -__builtin_inff() ? -1 : int32_t(0xffffffffu - uint32_t(e & 0xffffffffu));
   };
-  if (cnt <= kLpThreads) {
-    if (t < cnt) {
-      const uint64_t e = sm.buf[t];
-      int r = 0;
-      for (int j = 0; j < cnt; ++j) r += sm.buf[j] > e;   // ids differ, so no two are equal
-      if (r < k) put(r, e);
+  if (cnt <= 4 * kLpThreads) {
+    uint64_t e[4];
+    int r[4] = {};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[i] = t + i * kLpThreads < cnt ? sm.buf[t + i * kLpThreads] : 0ull;
+    if (cnt <= kLpThreads) {
+#pragma unroll 8
+      for (int j = 0; j < cnt; ++j) r[0] += sm.buf[j] > e[0];
+    } else {
+#pragma unroll 4
+      for (int j = 0; j < cnt; ++j) {
+        const uint64_t o = sm.buf[j];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] += o > e[i];
+      }
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (t + i * kLpThreads < cnt && r[i] < k) put(r[i], e[i]);
   } else {
     sort_desc(sm, cnt);
     for (int j = t; j < min(cnt, k); j += kLpThreads) put(j, sm.buf[j]);
@@ -126,12 +152,130 @@ __device__ __forceinline__ void emit_top(const LogprobArgs &a, int64_t row, Sele
   }
 }
 
+// A thread's entries of a piece, as they are stored; -infinity past the end.
+template <int T>
+struct PieceRaw {
+  typename FloatType<T>::type v[kLpEach];
+};
+template <int T>
+__device__ __forceinline__ void load_piece(PieceRaw<T> &p, const typename FloatType<T>::type *x, int64_t j, int64_t end) {
+  typedef typename FloatType<T>::type F;
+#pragma unroll
+  for (int u = 0; u < kLpEach / 8; ++u) {
+    const int64_t at = j + (u * kLpThreads + int(threadIdx.x)) * 8, left = end - at;
+    if (left >= 8) {
+      if constexpr (T == RSLM_F32) {
+        const F32x8u e = *reinterpret_cast<const F32x8u *>(x + at);
+        __builtin_memcpy(&p.v[8 * u], &e, sizeof(e));
+      } else {
+        const H16x8u e = *reinterpret_cast<const H16x8u *>(x + at);
+        __builtin_memcpy(&p.v[8 * u], &e, sizeof(e));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p.v[8 * u + i] = i < left ? x[at + i] : F(-__builtin_inff());
+    }
+  }
+}
+template <int T>
+__device__ __forceinline__ float piece_values(float (&v)[kLpEach], const PieceRaw<T> &p) {
+#pragma unroll
+  for (int i = 0; i < kLpEach; ++i) v[i] = float(p.v[i]);
+  float top = v[0];
+#pragma unroll
+  for (int i = 1; i < kLpEach; ++i) top = fmaxf(top, v[i]);
+  return top == top ? top : -__builtin_inff();
+}
+// index in the row of a thread's entry i of the piece at j
+__device__ __forceinline__ int32_t piece_index(int64_t j, int i) {
+  return int32_t(j + ((i >> 3) * kLpThreads + int(threadIdx.x)) * 8 + (i & 7));
+}
+
+// A value that at least k of the threads' `top` reach, the k-th largest cut to
+// its upper 16 bits (as ordered integers): found bit by bit, a step being four
+// compares and counts of lanes.  -infinity where k is more than the threads.
+__device__ __forceinline__ float top_bound(float top, int k, uint32_t *tops) {
+  if (k > kLpThreads) return -__builtin_inff();
+  tops[threadIdx.x] = order_key(top + 0.f);
+  __syncthreads();
+  const uint4 v = reinterpret_cast<const uint4 *>(tops)[threadIdx.x & 63];
+  __syncthreads();
+  uint32_t bound = 0u;
+#pragma unroll
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t up = bound | 1u << bit;
+    const int reach = __popcll(__ballot(v.x >= up)) + __popcll(__ballot(v.y >= up)) + __popcll(__ballot(v.z >= up)) +
+                      __popcll(__ballot(v.w >= up));
+    if (reach >= k) bound = up;
+  }
+  return bound < 0x00800000u ? -__builtin_inff() : key_to_float(bound);   // that of the lowest float
+}
+
+// Entries of a thread's piece at or above thr, to the buffer while it has room
+// (sm.count counts on).
+__device__ __forceinline__ void push(SelectSmem &sm, const float (&v)[kLpEach], float top, float thr, int64_t j, int i0,
+                                     int i1) {
+  if (!(top >= thr)) return;
+#pragma unroll
+  for (int i = 0; i < kLpEach; ++i) {
+    if (i >= i0 && i < i1 && v[i] >= thr && v[i] > -__builtin_inff()) {
+      const uint32_t pos = atomicAdd(&sm.count, 1u);
+      if (pos < uint32_t(kSelCap)) sm.buf[pos] = composite(order_key(v[i] + 0.f), piece_index(j, i));
+    }
+  }
+}
+
+// The buffer's k best of `count` (a barrier ahead of it is the caller's): their
+// number, and the k-th as the threshold.
+__device__ __forceinline__ int cut(SelectSmem &sm, int count, int k, float &thr) {
+  sort_desc(sm, count);
+  __syncthreads();
+  if (count < k) return count;
+  thr = fmaxf(thr, key_to_float(uint32_t(sm.buf[k - 1] >> 32)));
+  return k;
+}
+
+// The candidates of [j0, j1) again, where they overflowed: 1,024 entries at a
+// time, which always fit beside the k <= 1,024 that the buffer is cut to when
+// it has no room for more.  Returns their number.
+template <int T>
+__device__ __noinline__ int collect_again(SelectSmem &sm, const typename FloatType<T>::type *x, int64_t j0, int64_t j1,
+                                          int k) {
+  int count = 0;
+  float thr = -__builtin_inff();
+  for (int64_t j = j0; j < j1; j += kLpPiece) {
+    PieceRaw<T> raw;
+    float v[kLpEach];
+    load_piece<T>(raw, x, j, j1);
+    const float top = piece_values<T>(v, raw);
+    if (!__syncthreads_or(top >= thr && top > -__builtin_inff())) continue;
+    bool full = false;   // the buffer has been cut to k, and nothing added
+    for (int i = 0; i < kLpEach; i += 4) {
+      if (threadIdx.x == 0) sm.count = uint32_t(count);
+      __syncthreads();
+      push(sm, v, top, thr, j, i, i + 4);
+      __syncthreads();
+      const int now = int(sm.count);
+      __syncthreads();
+      full = full && now == count;
+      count = now;
+      if (count > kSelCap - 1024 && count > k) {
+        count = cut(sm, count, k, thr);
+        full = count == k;
+      }
+    }
+    // later entries have higher indices and lose to equal ones
+    if (full) thr = key_to_float(order_key(thr + 0.f) + 1u);
+  }
+  return count;
+}
+
 template <int T, bool TOP>
 __global__ void __launch_bounds__(kLpThreads) k_logprob(LogprobArgs a) {
   __shared__ SelectSmem sm;
   __shared__ SoftSum parts[kLpThreads / 64];
-  __shared__ __align__(16) float tops[kLpThreads];
-  __shared__ float thr_s;
+  __shared__ __align__(16) uint32_t tops[kLpThreads];
+  __shared__ uint32_t notes[TOP ? kLpNotes : 1];   // piece * 256 + thread
   __shared__ float lz_s;
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
   const int64_t row = blockIdx.x / a.slices;
@@ -141,28 +285,16 @@ __global__ void __launch_bounds__(kLpThreads) k_logprob(LogprobArgs a) {
   const float c = a.scale * kLog2e;
   const float ninf = -__builtin_inff();
   SoftSum s{ninf, 0.f, 0.f};
-  int count = 0;        // entries in the buffer, the same in every thread
-  float thr = ninf;     // entries below it are not among the k largest
-  for (int64_t j = j0; j < j1; j += kLpPiece) {
+  float thr = ninf;     // at least k entries reach it
+  if (TOP && tid == 0) sm.count = 0u;
+  if (TOP) __syncthreads();
+  PieceRaw<T> next;
+  if (j0 < j1) load_piece<T>(next, x, j0, j1);
+  int piece = 0, look = 0;
+  for (int64_t j = j0; j < j1; j += kLpPiece, ++piece) {
     float v[kLpEach];
-#pragma unroll
-    for (int u = 0; u < kLpEach / 8; ++u) {
-      float e[8];
-      const int64_t at = j + (u * kLpThreads + tid) * 8;
-      const int64_t left = j1 - at;
-      if (left >= 8) {
-        load_float8<T>(e, x + at, 0, 8);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = i < left ? load_float<T>(x, at + i) : ninf;
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[8 * u + i] = e[i];
-    }
-    float top = v[0];
-#pragma unroll
-    for (int i = 1; i < kLpEach; ++i) top = fmaxf(top, v[i]);
-    top = top == top ? top : ninf;
+    const float top = piece_values<T>(v, next);
+    if (j + kLpPiece < j1) load_piece<T>(next, x, j + kLpPiece, j1);
     if (top > s.m) {
       if (s.m > ninf) {
         const float d = (s.m - top) * c, e = __builtin_amdgcn_exp2f(d);
@@ -180,82 +312,51 @@ __global__ void __launch_bounds__(kLpThreads) k_logprob(LogprobArgs a) {
       s.w = fmaf(w, fmaxf(y, -200.f), s.w);   // masked: w = 0 times -200
     }
     if constexpr (TOP) {
-      const int k = a.k;
-      // entries at or above the threshold; the buffer takes them unless it
-      // would overflow, which every thread learns after the barrier
-      auto push = [&](int i0, int i1) {
-        if (top >= thr) {
+      if (piece == look && j + kLpPiece < j1) {   // pieces 0, 3, 15, 63, ...
+        thr = fmaxf(thr, top_bound(s.m, a.k, tops));
+        look = 4 * look + 3;
+      }
+      if (top >= thr && top > ninf) {
+        const uint32_t pos = atomicAdd(&sm.count, 1u);
+        if (pos < uint32_t(kLpNotes)) notes[pos] = uint32_t(piece * kLpThreads + tid);
+      }
+    }
+  }
+  int count = 0;
+  if constexpr (TOP) {
+    thr = fmaxf(thr, top_bound(s.m, a.k, tops));
+    __syncthreads();
+    const int noted = int(sm.count);
+    __syncthreads();
+    if (tid == 0) sm.count = 0u;
+    __syncthreads();
+    bool again = noted > kLpNotes;
+    if (!again) {
+      for (int i = tid; i < noted; i += kLpThreads) {
+        const uint32_t at = notes[i];
+        const int64_t j = j0 + int64_t(at / kLpThreads) * kLpPiece;
 #pragma unroll
-          for (int i = 0; i < kLpEach; ++i) {
-            if (i >= i0 && i < i1 && v[i] >= thr && v[i] > ninf) {
+        for (int u = 0; u < kLpEach / 8; ++u) {
+          const int64_t j8 = j + (u * kLpThreads + int(at % kLpThreads)) * 8;
+          const int left = int(j1 - j8 < 8 ? (j1 - j8 < 0 ? 0 : j1 - j8) : 8);
+          float e[8];
+          load_float8<T>(e, x + j8, 0, left);
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            if (q < left && e[q] >= thr && e[q] > ninf) {
               const uint32_t pos = atomicAdd(&sm.count, 1u);
-              if (pos < uint32_t(kSelCap))
-                sm.buf[pos] = composite(order_key(v[i] + 0.f), int32_t(j + ((i >> 3) * kLpThreads + tid) * 8 + (i & 7)));
+              if (pos < uint32_t(kSelCap)) sm.buf[pos] = composite(order_key(e[q] + 0.f), int32_t(j8 + q));
             }
-          }
-        }
-      };
-      // the k best of the buffer, and the k-th of them as the threshold
-      bool full = false;   // the buffer holds these and nothing else
-      auto cut = [&]() {
-        __syncthreads();
-        sort_desc(sm, count);
-        full = count >= k;
-        if (full) {
-          thr = fmaxf(thr, key_to_float(uint32_t(sm.buf[k - 1] >> 32)));
-          count = k;
-        }
-      };
-      // raise the threshold to the k-th largest of the threads' maxima
-      auto raise = [&]() {
-        if (k > kLpThreads) return;
-        tops[tid] = top;
-        __syncthreads();
-        int r = 0;
-        for (int i = 0; i < kLpThreads; i += 4) {
-          const float4 o = *reinterpret_cast<const float4 *>(&tops[i]);
-          r += (o.x > top || (o.x == top && i < tid)) + (o.y > top || (o.y == top && i + 1 < tid)) +
-               (o.z > top || (o.z == top && i + 2 < tid)) + (o.w > top || (o.w == top && i + 3 < tid));
-        }
-        if (r == k - 1) thr_s = top;
-        __syncthreads();
-        thr = fmaxf(thr, thr_s);
-      };
-      if (j == j0) raise();
-      for (int attempt = 0; attempt < 2; ++attempt) {
-        if (tid == 0) sm.count = uint32_t(count);
-        __syncthreads();
-        push(0, kLpEach);
-        __syncthreads();
-        const uint32_t now = sm.count;
-        __syncthreads();
-        if (now <= uint32_t(kSelCap)) {
-          full = full && int(now) == count;
-          count = int(now);
-          break;
-        }
-        if (attempt == 0) {
-          if (count > k) cut();
-          raise();
-        } else {
-          // a few entries of each thread at a time, which always fit
-          if (count > k) cut();
-          for (int i = 0; i < kLpEach; i += 4) {
-            __syncthreads();
-            if (tid == 0) sm.count = uint32_t(count);
-            __syncthreads();
-            push(i, i + 4);
-            __syncthreads();
-            count = int(sm.count);
-            cut();
-            __syncthreads();
-          }
         }
       }
-      if (count > kSelCap / 2 && count > k) cut();
-      // later entries have higher indices and lose to equal ones: a row of
-      // equal entries does not fill the buffer again
-      if (full) thr = key_to_float(order_key(thr + 0.f) + 1u);
+      __syncthreads();
+      count = int(sm.count);
+      __syncthreads();
+      again = count > kSelCap;
+    }
+    if (again) {
+      count = collect_again<T>(sm, x, j0, j1, a.k);
+      __syncthreads();
     }
   }
   s = soft_join_wave(s, c);
@@ -271,40 +372,54 @@ __global__ void __launch_bounds__(kLpThreads) k_logprob(LogprobArgs a) {
   } else {
     if (tid == 0) a.sums[blockIdx.x] = s;
     if constexpr (TOP) {
-      if (count > a.k) {
-        __syncthreads();
-        sort_desc(sm, count);
+      if (count > a.room) {
+        float none = ninf;
+        count = cut(sm, count, a.k, none);
       }
-      __syncthreads();
-      for (int i = tid; i < a.k; i += kLpThreads) a.cands[int64_t(blockIdx.x) * a.k + i] = i < count ? sm.buf[i] : 0ull;
+      if (tid == 0) a.counts[blockIdx.x] = count;
+      for (int i = tid; i < count; i += kLpThreads) a.cands[int64_t(blockIdx.x) * a.room + i] = sm.buf[i];
     }
   }
 }
 
-// Joins the slices of a row.
+// Joins the slices of a row.  Of their candidates, those that can be among the k
+// largest (top_bound again) are ranked.
 template <int T, bool TOP>
 __global__ void __launch_bounds__(kLpThreads) k_logprob_join(LogprobArgs a) {
   __shared__ SelectSmem sm;
   __shared__ SoftSum parts[kLpThreads / 64];
+  __shared__ __align__(16) uint32_t tops[kLpThreads];
   __shared__ float lz_s;
-  const int tid = threadIdx.x;
+  constexpr int kHeld = kSelCap / kLpThreads;
+  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
   const int64_t row = blockIdx.x;
   const float c = a.scale * kLog2e;
   SoftSum s{-__builtin_inff(), 0.f, 0.f};
   if (tid < a.slices) s = a.sums[row * a.slices + tid];
+  uint64_t e[kHeld];
+  float top = -__builtin_inff();
+  if constexpr (TOP) {
+    if (tid == 0) sm.count = 0u;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int at = i * kLpThreads + tid, slice = at / a.room;
+      const bool in = slice < a.slices && at - slice * a.room < a.counts[row * a.slices + min(slice, a.slices - 1)];
+      e[i] = in ? a.cands[row * a.slices * a.room + at] : 0ull;   // no composite is 0
+      if (in) top = fmaxf(top, key_to_float(uint32_t(e[i] >> 32)));
+    }
+  }
   s = soft_join_wave(s, c);
-  if ((tid & 63) == 0) parts[tid >> 6] = s;
-  if (tid == 0) sm.count = 0u;
+  if (lane == 0) parts[wid] = s;
   __syncthreads();
   s = parts[0];
 #pragma unroll
   for (int i = 1; i < kLpThreads / 64; ++i) s = soft_join(s, parts[i], c);
   if (tid == 0) lz_s = emit_row<T>(a, row, s);
   if constexpr (TOP) {
-    for (int i = tid; i < a.slices * a.k; i += kLpThreads) {
-      const uint64_t e = a.cands[row * a.slices * a.k + i];
-      if (e) sm.buf[atomicAdd(&sm.count, 1u)] = e;   // slices * k <= kSelCap
-    }
+    const float bound = top_bound(top, a.k, tops);
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (e[i] && key_to_float(uint32_t(e[i] >> 32)) >= bound) sm.buf[atomicAdd(&sm.count, 1u)] = e[i];
     __syncthreads();
     emit_top(a, row, sm, int(sm.count), s.m, lz_s);
   }
@@ -343,14 +458,16 @@ __global__ void __launch_bounds__(256) k_logprob_backward(const void *scores, in
   }
 }
 
-// Slices of a row: enough workgroups for the GPU where there are few rows, at
-// least two pieces each, and no more candidates than the join's buffer holds.
+// Slices of a row: enough workgroups for the GPU where there are few rows, a
+// piece each at least, and no more candidates than the join's buffer holds.
 static int logprob_slices(int64_t m, int64_t n, int k) {
-  int64_t s = (512 + m - 1) / m;
-  const int64_t most = (n + 2 * kLpPiece - 1) / (2 * kLpPiece);
+  int64_t s = (1024 + m - 1) / m;
+  const int64_t most = (n + kLpPiece - 1) / kLpPiece;
   if (s > most) s = most;
   if (s > kLpMaxSlices) s = kLpMaxSlices;
-  if (k > 0 && s > kSelCap / k) s = kSelCap / k;
+  // twice the k best of a slice, which it mostly need not cut to them
+  const int room = k <= kSelCap / 16 ? 2 * k : k;
+  if (k > 0 && s > kSelCap / room) s = kSelCap / room;
   return int(s < 1 ? 1 : s);
 }
 static size_t logprob_sums_bytes(int64_t m, int slices) {
@@ -383,7 +500,8 @@ extern "C" {
 size_t rslm_logprob_workspace(int64_t m, int64_t n, int32_t k) {
   if (!logprob_sizes_ok(m, n, k) || m == 0) return 0;
   const int s = logprob_slices(m, n, k);
-  return s > 1 ? logprob_sums_bytes(m, s) + size_t(m) * s * k * sizeof(uint64_t) : 0;
+  return s > 1 ? logprob_sums_bytes(m, s) + size_t(m) * (k > 0 ? kSelCap * sizeof(uint64_t) + s * sizeof(int32_t) : 0)
+               : 0;
 }
 
 int rslm_logprob(const void *scores, int32_t dtype, int64_t m, int64_t n, int64_t stride, float scale,
@@ -402,7 +520,9 @@ int rslm_logprob(const void *scores, int32_t dtype, int64_t m, int64_t n, int64_
   if (a.slices > 1) {
     if (!ws || !aligned_to(ws, 16)) return RSLM_ERR_INVALID_ARG;
     a.sums = static_cast<SoftSum *>(ws);
+    a.room = kSelCap / a.slices;
     a.cands = reinterpret_cast<uint64_t *>(static_cast<char *>(ws) + logprob_sums_bytes(m, a.slices));
+    a.counts = reinterpret_cast<int32_t *>(a.cands + size_t(m) * kSelCap);
   }
   a.per = (n + int64_t(a.slices) * kLpPiece - 1) / (int64_t(a.slices) * kLpPiece) * kLpPiece;
   const hipStream_t s = as_stream(stream);
