@@ -348,3 +348,29 @@ def test_offsets_past_32_bits(R):
     d[79, n - 1] = d[78, n - 3] = 1
     g = R.rslm_mx4_score_backward(d, b)
     assert g[79, 0] == value[n - 1] and g[78, 0] == value[n - 3] and g[:78].abs().sum() == 0
+
+
+@pytest.mark.parametrize("m,n,dim,dt", [(66, 16300, 129, "f32"), (130, 8201, 257, "bf16"), (513, 4097, 640, "f16"),
+                                        (1030, 2051, 1000, "f32"), (4090, 4100, 130, "bf16"),
+                                        (4100, 4081, 384, "f32"), (4097, 4096, 70, "f16"), (1000, 17000, 300, "bf16")])
+def test_matmul_of_many_tiles(R, m, n, dim, dt):
+    """Products large enough for tiles: values, rows with NaN scales, and the places around them."""
+    a, va = rows_of(R, m, dim, 21)
+    b, vb = rows_of(R, n, dim, 22)
+    if dt == "f16":
+        a = R.Mx4Rows(a.codes, torch.where(a.scales > 0, a.scales - 6, a.scales), dim)
+        va = va / 64
+    buf = torch.full((m + 2, n + 9), 3.0, device="cuda", dtype=DT[dt])
+    out = R.rslm_mx4_matmul(a, b, dtype=DT[dt], out=buf[1:m + 1, 4:4 + n])
+    check_sums(out, va @ vb.T, np.abs(va) @ np.abs(vb).T, dim, dt)
+    plain = R.rslm_mx4_matmul(a, b, dtype=DT[dt])       # aligned or not
+    assert torch.equal(plain, out)
+    out.fill_(3.0)
+    assert (buf == 3).all()
+    a.scales[m - 1, 0] = 255
+    b.scales[n // 2, (dim - 1) // 32] = 255
+    got = R.rslm_mx4_matmul(a, b, dtype=DT[dt])
+    assert torch.isnan(got[m - 1]).all() and torch.isnan(got[:, n // 2]).all()
+    keep = torch.ones(n, dtype=torch.bool, device="cuda")
+    keep[n // 2] = False
+    assert torch.equal(got[:m - 1, keep], plain[:m - 1, keep])
