@@ -467,11 +467,18 @@ def _need_rows(t, name, shape=None):
 
 def _out_rows(out, shape, dtype, device, name="out"):
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=device)
-    elif out.dtype != dtype:
+        return torch.empty(shape, dtype=dtype, device=device), _float_type(dtype, name), shape[1]
+    if out.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {out.dtype}")
     code, stride = _need_rows(out, name, shape)
+    if out.device != device:
+        raise ValueError(f"{name} must be on {device}, got {out.device}")
     return out, code, stride
+
+
+def _at(t):
+    """The address of t (None: null), as the declared argument types take it."""
+    return t.data_ptr() if t is not None else None
 
 
 def _same_device(a, b, name):
@@ -497,9 +504,14 @@ class Mx4Rows:
 
     @classmethod
     def empty(cls, n, dim, device):
+        if not 1 <= dim <= 65536:
+            raise ValueError("dim must be 1..65536")
         steps = (dim + 127) // 128
-        return cls(torch.empty((n, 64 * steps), dtype=torch.uint8, device=device),
-                   torch.empty((n, 4 * steps), dtype=torch.uint8, device=device), dim)
+        rows = cls.__new__(cls)   # what __init__ checks holds
+        rows.codes = torch.empty((n, 64 * steps), dtype=torch.uint8, device=device)
+        rows.scales = torch.empty((n, 4 * steps), dtype=torch.uint8, device=device)
+        rows.dim = int(dim)
+        return rows
 
     @property
     def n(self):
@@ -521,20 +533,20 @@ def rslm_mx4_quantize(x, plan=None, rows=None, stream=None):
         rows = Mx4Rows.empty(n, dim, x.device)
     elif rows.n != n or rows.dim != dim:
         raise ValueError("rows must have the shape of x")
-    _same_device(x, rows, "rows")
+    else:
+        _same_device(x, rows, "rows")
     L.check("rslm_mx4_quantize", L.lib().rslm_mx4_quantize(
-        plan.handle if plan is not None else None, _ptr(x), code, n, dim, stride, _ptr(rows.codes),
-        _ptr(rows.scales), _stream(stream)))
+        plan.handle if plan is not None else None, _at(x), code, n, dim, stride, _at(rows.codes),
+        _at(rows.scales), _raw_stream(stream, x.device)))
     return rows
 
 
 def rslm_mx4_dequantize(rows, dtype=torch.float32, out=None, stream=None):
     """The values of MX4 rows."""
     out, code, stride = _out_rows(out, (rows.n, rows.dim), dtype, rows.device)
-    _same_device(rows, out, "out")
     L.check("rslm_mx4_dequantize", L.lib().rslm_mx4_dequantize(
-        _ptr(rows.codes), _ptr(rows.scales), rows.n, rows.dim, _ptr(out), code, stride,
-        _stream(stream)))
+        _at(rows.codes), _at(rows.scales), rows.n, rows.dim, _at(out), code, stride,
+        _raw_stream(stream, out.device)))
     return out
 
 
@@ -544,10 +556,9 @@ def rslm_mx4_matmul(a, b, dtype=torch.float32, out=None, stream=None):
         raise ValueError("a and b must have the same dimension")
     _same_device(a, b, "b")
     out, code, stride = _out_rows(out, (a.n, b.n), dtype, a.device)
-    _same_device(a, out, "out")
     L.check("rslm_mx4_matmul", L.lib().rslm_mx4_matmul(
-        _ptr(a.codes), _ptr(a.scales), a.n, _ptr(b.codes), _ptr(b.scales), b.n, a.dim, _ptr(out),
-        code, stride, _stream(stream)))
+        _at(a.codes), _at(a.scales), a.n, _at(b.codes), _at(b.scales), b.n, a.dim, _at(out),
+        code, stride, _raw_stream(stream, out.device)))
     return out
 
 
@@ -558,12 +569,11 @@ def rslm_mx4_score(x, b, dtype=torch.float32, out=None, stream=None):
         raise ValueError("x must have b's dimension")
     _same_device(x, b, "b")
     out, ocode, ostride = _out_rows(out, (x.shape[0], b.n), dtype, x.device)
-    _same_device(x, out, "out")
     nb = L.lib().rslm_mx4_score_workspace(x.shape[0], b.n, b.dim, code)
-    ws = _WS.get(nb, x.device, "mx4_score", stream)
+    ws = _WS.get(nb, x.device, "mx4_score", stream) if nb else None
     L.check("rslm_mx4_score", L.lib().rslm_mx4_score(
-        _ptr(x), code, x.shape[0], stride, _ptr(b.codes), _ptr(b.scales), b.n, b.dim, _ptr(out),
-        ocode, ostride, _ptr(ws), ws.numel(), _stream(stream)))
+        _at(x), code, x.shape[0], stride, _at(b.codes), _at(b.scales), b.n, b.dim, _at(out),
+        ocode, ostride, _at(ws), nb, _raw_stream(stream, out.device)))
     return out
 
 
@@ -576,12 +586,11 @@ def rslm_mx4_score_backward(dout, b, dtype=None, out=None, stream=None):
     _same_device(dout, b, "b")
     m = dout.shape[0]
     out, ocode, ostride = _out_rows(out, (m, b.dim), dout.dtype if dtype is None else dtype, dout.device)
-    _same_device(dout, out, "out")
     nb = L.lib().rslm_mx4_score_backward_workspace(m, b.n, b.dim, code)
-    ws = _WS.get(nb, dout.device, "mx4_backward", stream)
+    ws = _WS.get(nb, dout.device, "mx4_backward", stream) if nb else None
     L.check("rslm_mx4_score_backward", L.lib().rslm_mx4_score_backward(
-        _ptr(dout), code, m, stride, _ptr(b.codes), _ptr(b.scales), b.n, b.dim, _ptr(out), ocode,
-        ostride, _ptr(ws), ws.numel(), _stream(stream)))
+        _at(dout), code, m, stride, _at(b.codes), _at(b.scales), b.n, b.dim, _at(out), ocode,
+        ostride, _at(ws), nb, _raw_stream(stream, out.device)))
     return out
 
 
@@ -602,17 +611,23 @@ def rslm_logprob(scores, target=None, k=0, scale=1.0, stream=None):
     code, stride = _need_rows(scores, "scores")
     _need(target, torch.int64, "target")
     m, n = scores.shape
-    if target is not None and target.shape != (m,):
-        raise ValueError("target must have an entry for every row of scores")
-    new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=scores.device)
-    r = LogProb(new(m) if target is not None else None, new(m), new(m), new(m, 2),
-                new(m, k), new(m, k, dtype=torch.int32))
+    if k < 0:
+        raise ValueError("k must not be negative")
+    if target is not None:
+        if target.shape != (m,):
+            raise ValueError("target must have an entry for every row of scores")
+        _same_device(scores, target, "target")
+    # one allocation for the row numbers: these calls are short
+    logprob, lse, entropy, stats, top = torch.empty(
+        m * (5 + k), dtype=torch.float32, device=scores.device).split([m, m, m, 2 * m, k * m])
+    r = LogProb(logprob if target is not None else None, lse, entropy, stats.view(m, 2), top.view(m, k),
+                torch.empty((m, k), dtype=torch.int32, device=scores.device))
     nb = L.lib().rslm_logprob_workspace(m, n, k)
-    ws = _WS.get(nb, scores.device, "logprob", stream)
+    ws = _WS.get(nb, scores.device, "logprob", stream) if nb else None
     L.check("rslm_logprob", L.lib().rslm_logprob(
-        _ptr(scores), code, m, n, stride, scale, _ptr(target), k, _ptr(r.logprob), _ptr(r.lse),
-        _ptr(r.entropy), _ptr(r.stats), _ptr(r.top_logprob), _ptr(r.top_ids), _ptr(ws), ws.numel(),
-        _stream(stream)))
+        _at(scores), code, m, n, stride, scale, _at(target), k, _at(r.logprob), _at(r.lse),
+        _at(r.entropy), _at(r.stats), _at(r.top_logprob), _at(r.top_ids), _at(ws), nb,
+        _raw_stream(stream, scores.device)))
     return r
 
 
@@ -626,10 +641,12 @@ def rslm_logprob_backward(scores, target, result, dlogprob=None, dentropy=None, 
     _need(dentropy, torch.float32, "dentropy")
     m, n = scores.shape
     for t, name in ((target, "target"), (dlogprob, "dlogprob"), (dentropy, "dentropy"), (result.lse, "result")):
-        if t is not None and t.shape != (m,):
-            raise ValueError(f"{name} must have an entry for every row of scores")
+        if t is not None:
+            if t.shape != (m,):
+                raise ValueError(f"{name} must have an entry for every row of scores")
+            _same_device(scores, t, name)
     out, _, ostride = _out_rows(out, (m, n), scores.dtype, scores.device)
     L.check("rslm_logprob_backward", L.lib().rslm_logprob_backward(
-        _ptr(scores), code, m, n, stride, scale, _ptr(target), _ptr(result.stats), _ptr(result.entropy),
-        _ptr(dlogprob), _ptr(dentropy), _ptr(out), ostride, _stream(stream)))
+        _at(scores), code, m, n, stride, scale, _at(target), _at(result.stats), _at(result.entropy),
+        _at(dlogprob), _at(dentropy), _at(out), ostride, _raw_stream(stream, out.device)))
     return out
