@@ -18,7 +18,7 @@
 // 4,096 x 32,768 bfloat16: 53 us without alternatives (5.1 TB/s), 73 with k = 10;
 // 97 where the bound came of ranking 64 parts' maxima, lane by lane, and 104 where
 // every entry at or above the first piece's bound went to the candidates at once.
-// 1 x 131,072 float32, k = 5: 7.4 us in 32 slices and 9.5 for the join, both the
+// 1 x 131,072 float32, k = 5: 7.4 us in 32 slices and 6.5 for the join, both the
 // latency of their barriers and reads.  Backward, 4,096 x 32,768 bfloat16: 112 us,
 // 4.8 TB/s read and written.
 //
@@ -79,7 +79,7 @@ struct LogprobArgs {
   int64_t per;          // entries of a slice, a multiple of kLpPiece
   int room;             // entries that a slice may leave, at least k
   SoftSum *sums;        // m x slices
-  uint64_t *cands;      // m x slices x room
+  uint64_t *cands;      // m x kSelCap: slices x room of them used
   int32_t *counts;      // m x slices
 };
 
@@ -89,9 +89,21 @@ __device__ __forceinline__ float log_of(float v, float m, float lz, float scale)
   return v * scale == -__builtin_inff() ? -__builtin_inff() : fmaf(v - m, scale, -lz);
 }
 
-// The row's numbers from its sums, by one thread; ln Z.
+// The score of the row's target, asked for early: two reads, one after the other.
+struct Target {
+  bool in;
+  float score;
+};
 template <int T>
-__device__ __forceinline__ float emit_row(const LogprobArgs &a, int64_t row, const SoftSum &s) {
+__device__ __forceinline__ Target target_of(const LogprobArgs &a, int64_t row) {
+  const int64_t t = a.logprob ? a.target[row] : -1;
+  Target r{t >= 0 && t < a.n, 0.f};
+  if (r.in) r.score = load_float<T>(a.scores, row * a.stride + t);
+  return r;
+}
+
+// The row's numbers from its sums, by one thread; ln Z.
+__device__ __forceinline__ float emit_row(const LogprobArgs &a, int64_t row, const SoftSum &s, const Target &target) {
   float lz = logf(s.z), lse = fmaf(s.m, a.scale, lz), h = fmaf(-kLn2, s.w / s.z, lz);
   if (s.z != s.z) {
     lz = lse = h = s.z;
@@ -103,11 +115,7 @@ __device__ __forceinline__ float emit_row(const LogprobArgs &a, int64_t row, con
   if (a.entropy) a.entropy[row] = h;
   a.stats[2 * row] = s.m;
   a.stats[2 * row + 1] = lz;
-  if (a.logprob) {
-    const int64_t t = a.target[row];
-    a.logprob[row] =
-        t >= 0 && t < a.n ? log_of(load_float<T>(a.scores, row * a.stride + t), s.m, lz, a.scale) : 0.f;
-  }
+  if (a.logprob) a.logprob[row] = target.in ? log_of(target.score, s.m, lz, a.scale) : 0.f;
   return lz;
 }
 
@@ -290,6 +298,8 @@ __global__ void __launch_bounds__(kLpThreads) k_logprob(LogprobArgs a) {
   if (TOP) __syncthreads();
   PieceRaw<T> next;
   if (j0 < j1) load_piece<T>(next, x, j0, j1);
+  Target target{};
+  if (a.slices == 1 && tid == 0) target = target_of<T>(a, row);
   int piece = 0, look = 0;
   for (int64_t j = j0; j < j1; j += kLpPiece, ++piece) {
     float v[kLpEach];
@@ -366,7 +376,7 @@ __global__ void __launch_bounds__(kLpThreads) k_logprob(LogprobArgs a) {
 #pragma unroll
   for (int i = 1; i < kLpThreads / 64; ++i) s = soft_join(s, parts[i], c);
   if (a.slices == 1) {
-    if (tid == 0) lz_s = emit_row<T>(a, row, s);
+    if (tid == 0) lz_s = emit_row(a, row, s, target);
     __syncthreads();
     if constexpr (TOP) emit_top(a, row, sm, count, s.m, lz_s);
   } else {
@@ -377,7 +387,7 @@ __global__ void __launch_bounds__(kLpThreads) k_logprob(LogprobArgs a) {
         count = cut(sm, count, a.k, none);
       }
       if (tid == 0) a.counts[blockIdx.x] = count;
-      for (int i = tid; i < count; i += kLpThreads) a.cands[int64_t(blockIdx.x) * a.room + i] = sm.buf[i];
+      for (int i = tid; i < count; i += kLpThreads) a.cands[row * kSelCap + slice * a.room + i] = sm.buf[i];
     }
   }
 }
@@ -396,17 +406,29 @@ __global__ void __launch_bounds__(kLpThreads) k_logprob_join(LogprobArgs a) {
   const float c = a.scale * kLog2e;
   SoftSum s{-__builtin_inff(), 0.f, 0.f};
   if (tid < a.slices) s = a.sums[row * a.slices + tid];
+  Target target{};
   uint64_t e[kHeld];
   float top = -__builtin_inff();
   if constexpr (TOP) {
     if (tid == 0) sm.count = 0u;
+    // room for all is there: candidates and their numbers are read at once
+    int have[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int at = i * kLpThreads + tid;
+      e[i] = a.cands[row * kSelCap + at];
+      have[i] = a.counts[row * a.slices + min(at / a.room, a.slices - 1)];
+    }
+    if (tid == 0) target = target_of<T>(a, row);
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
       const int at = i * kLpThreads + tid, slice = at / a.room;
-      const bool in = slice < a.slices && at - slice * a.room < a.counts[row * a.slices + min(slice, a.slices - 1)];
-      e[i] = in ? a.cands[row * a.slices * a.room + at] : 0ull;   // no composite is 0
+      const bool in = slice < a.slices && at - slice * a.room < have[i];
+      if (!in) e[i] = 0ull;   // no composite is 0
       if (in) top = fmaxf(top, key_to_float(uint32_t(e[i] >> 32)));
     }
+  } else if (tid == 0) {
+    target = target_of<T>(a, row);
   }
   s = soft_join_wave(s, c);
   if (lane == 0) parts[wid] = s;
@@ -414,7 +436,7 @@ __global__ void __launch_bounds__(kLpThreads) k_logprob_join(LogprobArgs a) {
   s = parts[0];
 #pragma unroll
   for (int i = 1; i < kLpThreads / 64; ++i) s = soft_join(s, parts[i], c);
-  if (tid == 0) lz_s = emit_row<T>(a, row, s);
+  if (tid == 0) lz_s = emit_row(a, row, s, target);
   if constexpr (TOP) {
     const float bound = top_bound(top, a.k, tops);
 #pragma unroll
