@@ -353,7 +353,7 @@ __global__ void __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 1 : 2) k_mx4_gemm
 // values by a workgroup, of which eight groups of threads take every eighth
 // part, and the eight sums one after another.
 template <int T>
-__global__ void __launch_bounds__(256) k_mx4_join(const float *__restrict__ part, int splits, int64_t m, int cols,
+__global__ void __launch_bounds__(256) k_mx4_join(const float *__restrict__ part, int splits, int64_t m, int64_t cols,
                                                   void *__restrict__ out, int64_t stride) {
   __shared__ float sums[8][32];
   const int v = threadIdx.x & 31, k0 = threadIdx.x >> 5;
@@ -374,6 +374,41 @@ __global__ void __launch_bounds__(256) k_mx4_join(const float *__restrict__ part
     __syncthreads();
   }
 }
+
+// The same of few parts and many values: four adjacent ones by a thread.
+template <int T>
+__global__ void __launch_bounds__(256) k_mx4_join_many(const float *__restrict__ part, int splits, int64_t m, int64_t cols,
+                                                       void *__restrict__ out, int64_t stride) {
+  const int64_t all = m * cols;
+  for (int64_t at = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4; at < all; at += int64_t(gridDim.x) * 1024) {
+    float s[4] = {};
+#pragma unroll 4
+    for (int k = 0; k < splits; ++k) {
+      const float *p = part + k * all + at;
+      if (at + 4 <= all) {
+        const F32x4u v = *reinterpret_cast<const F32x4u *>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] += v.v[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (at + i < all) s[i] += p[i];
+      }
+    }
+    int64_t row = at / cols, c = at - row * cols;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (at + i < all) store_float<T>(out, row * stride + c, s[i]);
+      if (++c == cols) c = 0, ++row;
+    }
+  }
+}
+
+// Which of the two joins, us with the product: the gradient of 2,048 x 32,768 x
+// 4,096 bfloat16 (2 parts) 545 by the first, 471 by the second; of 64 x 51,200 x
+// 1,024 (100 parts) 37 and 87.
+constexpr int64_t kManyValues = 1 << 16;
+constexpr int kFewParts = 16;
 
 struct Mx4GemmCall {
   const void *x;
@@ -398,14 +433,26 @@ static int64_t groups_of(int64_t len) { return (len + 127) / 128; }
 // Rows of x in a workgroup's tile.
 static int tile_rows(int64_t m) { return m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : m <= 128 ? 128 : 256; }
 
-// Parts into which the gradient's sum over the rows of b is split: enough
-// workgroups for the GPU, at least two groups of 128 rows each.
-static int backward_splits(int64_t m, int64_t n, int dim) {
+// Parts into which the sums over `len` values are split where m x cols has too
+// few tiles for the GPU: at least two groups of 128 each.  The gradient has long
+// sums and small outputs; for scores, the parts (about 8 bytes written and read
+// for a value of each, at 5 TB/s) have to cost less than the groups that a
+// workgroup is spared (2 us each, for every part of a number).  us, whole and
+// split: 118 x 100 x 2,917 float16 80.0, 19.2; 100 x 8,192 x 4,096 float32 146,
+// 42; 300 x 2,000 x 1,024 bfloat16 32.9, 24.1; but 128 x 20,000 x 768 bfloat16 22.3,
+// 30.7, which stays whole.
+static int sum_splits(int type, int64_t m, int64_t cols, int64_t len, bool backward) {
   const int bm = tile_rows(m);
-  const int64_t tiles = (dim + 255) / 256 * ((m + bm - 1) / bm);
-  const int64_t want = ((bm <= 64 ? 1024 : 256) + tiles - 1) / tiles, most = (groups_of(n) + 1) / 2;
-  const int64_t s = want < most ? want : most;
+  const int64_t tiles = (cols + 255) / 256 * ((m + bm - 1) / bm), groups = groups_of(len);
+  const int64_t want = backward ? ((bm <= 64 ? 1024 : 256) + tiles - 1) / tiles : 256 / tiles;
+  const int64_t most = (groups + 1) / 2;
+  int64_t s = want < most ? want : most;
+  if (!backward)
+    while (s > 1 && m * cols * s > 1200000 * type_parts(type) * (groups - (groups + s - 1) / s)) --s;
   return int(s < 1 ? 1 : s);
+}
+static size_t parts_bytes(int64_t m, int64_t cols, int splits) {
+  return splits > 1 ? (size_t(splits) * size_t(m) * size_t(cols) * sizeof(float) + 255) & ~size_t(255) : 0;
 }
 
 // Bytes of x's planes, 0 where x can be used as it is.
@@ -425,9 +472,13 @@ static void launch_gemm(const Mx4GemmCall &c, const void *xp, int64_t pitch, int
   hipLaunchKernelGGL((k_mx4_gemm<TO, NS, MF, WM, NF, WN, AG, TRANS>), grid, dim3(64 * WM * WN), 0, c.s,
                      static_cast<const uint8_t *>(xp), c.m, pitch, plane, c.bc, c.bs, c.n, c.dim, mx4_steps(c.dim),
                      c.out, c.ostride, splits > 1 ? part : nullptr, groups, per, int(mt), int(tiles));
-  if (splits > 1)
-    hipLaunchKernelGGL((k_mx4_join<TO>), dim3(value_groups(8 * c.m * cols)), dim3(256), 0, c.s, part, splits, c.m,
-                       int(cols), c.out, c.ostride);
+  const int64_t values = c.m * cols;
+  if (splits > 1 && splits <= kFewParts && values >= kManyValues)
+    hipLaunchKernelGGL((k_mx4_join_many<TO>), dim3(value_groups((values + 3) / 4)), dim3(256), 0, c.s, part, splits,
+                       c.m, cols, c.out, c.ostride);
+  else if (splits > 1)
+    hipLaunchKernelGGL((k_mx4_join<TO>), dim3(value_groups(8 * values)), dim3(256), 0, c.s, part, splits, c.m,
+                       cols, c.out, c.ostride);
 }
 
 // ws: partial sums of the splits, then the planes.
@@ -439,7 +490,7 @@ static void launch_gemm_rows(const Mx4GemmCall &c, int splits, char *ws) {
   const void *xp = c.x;
   int64_t pitch = c.stride * 2, plane = 0;
   if (planes_needed(c.x, T, c.stride, len)) {
-    char *planes = ws + (splits > 1 ? (size_t(splits) * size_t(c.m) * size_t(c.dim) * 4 + 255) & ~size_t(255) : 0);
+    char *planes = ws + parts_bytes(c.m, TRANS ? c.dim : c.n, splits);
     pitch = groups_of(len) * 256;
     plane = c.m * pitch;
     hipLaunchKernelGGL(k_mx4_split<T>, dim3(value_groups(c.m * pitch / 16)), dim3(256), 0, c.s, c.x, c.m, c.stride, len,
@@ -518,7 +569,8 @@ extern "C" {
 size_t rslm_mx4_score_workspace(int64_t m, int64_t n, int32_t dim, int32_t dtype) {
   if (m < 1 || n < 1 || m > 65535 * 128ll || n > kMx4MaxRows || dim < 1 || dim > kMx4MaxDim || !float_type_ok(dtype))
     return 0;
-  return score_few_ok(dtype, m, dim) ? 0 : planes_bytes(dtype, m, dim);
+  if (score_few_ok(dtype, m, dim)) return 0;
+  return parts_bytes(m, n, sum_splits(dtype, m, n, dim, false)) + planes_bytes(dtype, m, dim);
 }
 
 int rslm_mx4_score(const void *x, int32_t dtype, int64_t m, int64_t stride, const uint8_t *codes,
@@ -531,23 +583,19 @@ int rslm_mx4_score(const void *x, int32_t dtype, int64_t m, int64_t stride, cons
     launch_score_few_types(c, dtype, out_dtype);
     return check_launch();
   }
-  if (planes_needed(x, dtype, stride, dim)) {
-    if (ws_bytes < planes_bytes(dtype, m, dim)) return RSLM_ERR_WORKSPACE;
-    if (!ws || !aligned_to(ws, 16)) return RSLM_ERR_INVALID_ARG;
-  }
-  launch_gemm_types<false>(c, dtype, out_dtype, 1, ws);
+  const int splits = sum_splits(dtype, m, n, dim, false);
+  const size_t need =
+      parts_bytes(m, n, splits) + (planes_needed(x, dtype, stride, dim) ? planes_bytes(dtype, m, dim) : 0);
+  if (ws_bytes < need) return RSLM_ERR_WORKSPACE;
+  if (need && (!ws || !aligned_to(ws, 16))) return RSLM_ERR_INVALID_ARG;
+  launch_gemm_types<false>(c, dtype, out_dtype, splits, ws);
   return check_launch();
-}
-
-static size_t backward_parts_bytes(int64_t m, int64_t n, int dim) {
-  const int splits = backward_splits(m, n, dim);
-  return splits > 1 ? (size_t(splits) * size_t(m) * size_t(dim) * sizeof(float) + 255) & ~size_t(255) : 0;
 }
 
 size_t rslm_mx4_score_backward_workspace(int64_t m, int64_t n, int32_t dim, int32_t dtype) {
   if (m < 1 || n < 1 || m > 65535 * 128ll || n > kMx4MaxRows || dim < 1 || dim > kMx4MaxDim || !float_type_ok(dtype))
     return 0;
-  return backward_parts_bytes(m, n, dim) + planes_bytes(dtype, m, n);
+  return parts_bytes(m, dim, sum_splits(dtype, m, dim, n, true)) + planes_bytes(dtype, m, n);
 }
 
 int rslm_mx4_score_backward(const void *dout, int32_t dtype, int64_t m, int64_t stride, const uint8_t *codes,
@@ -562,12 +610,13 @@ int rslm_mx4_score_backward(const void *dout, int32_t dtype, int64_t m, int64_t 
     else hipLaunchKernelGGL(k_mx4_zero<RSLM_F16>, grid, dim3(256), 0, s, m, dim, dx, dx_stride);
     return check_launch();
   }
-  const size_t need = backward_parts_bytes(m, n, dim) +
-                      (planes_needed(dout, dtype, stride, n) ? planes_bytes(dtype, m, n) : 0);
+  const int splits = sum_splits(dtype, m, dim, n, true);
+  const size_t need =
+      parts_bytes(m, dim, splits) + (planes_needed(dout, dtype, stride, n) ? planes_bytes(dtype, m, n) : 0);
   if (ws_bytes < need) return RSLM_ERR_WORKSPACE;
   if (need && (!ws || !aligned_to(ws, 16))) return RSLM_ERR_INVALID_ARG;
   launch_gemm_types<true>(Mx4GemmCall{dout, m, stride, codes, scales, n, dim, dx, dx_stride, s}, dtype, dx_dtype,
-                          backward_splits(m, n, dim), ws);
+                          splits, ws);
   return check_launch();
 }
 
