@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(256) k_mx4_matmul(const uint8_t *__restrict__ 
 constexpr int kMmN = 256;               // rows of b
 constexpr int kMmRow = 128;             // bytes of a row's two groups
 
-template <int T, int MF, bool WIDE>
+template <int T, int MF>
 __global__ void __launch_bounds__(256, 1) k_mx4_matmul_tile(
     const uint8_t *__restrict__ ac, const uint8_t *__restrict__ as, int64_t m, const uint8_t *__restrict__ bc,
     const uint8_t *__restrict__ bs, int64_t n, int steps, void *__restrict__ out, int64_t stride, int mtiles) {
@@ -220,6 +220,9 @@ __global__ void __launch_bounds__(256, 1) k_mx4_matmul_tile(
   // 512), a part of LDS for each wavefront.
   typedef typename FloatType<T>::type Out;
   constexpr int kEach = 16 / sizeof(Out);              // values of a piece
+  struct __attribute__((packed, aligned(alignof(Out)))) Wide {
+    uint32_t v[4];
+  };
   constexpr int kPieces = 128 / kEach;                 // pieces of a row
   constexpr int kOwn = MF == 8 ? 32768 : 16384;
   constexpr int kRows = kOwn / (128 * int(sizeof(Out)));   // rows at a time
@@ -256,8 +259,8 @@ __global__ void __launch_bounds__(256, 1) k_mx4_matmul_tile(
       const int64_t orow = m0 + wm + 16 * k0 + row, c = n0 + wn + piece * kEach;
       if (orow >= m) continue;
       Out *p = static_cast<Out *>(out) + orow * stride + c;
-      if (WIDE && c + kEach <= n) {
-        *reinterpret_cast<uint4 *>(p) = v;
+      if (c + kEach <= n) {   // rows may begin anywhere
+        *reinterpret_cast<Wide *>(p) = __builtin_bit_cast(Wide, v);
       } else {
         Out e[kEach];
         __builtin_memcpy(e, &v, 16);
@@ -285,13 +288,8 @@ template <int T, int MF>
 static void launch_matmul_tile(const Mx4MatmulCall &c) {
   const int64_t mt = (c.m + 32 * MF - 1) / (32 * MF), nt = (c.n + kMmN - 1) / kMmN;
   const dim3 grid(unsigned(mt * nt));
-  // 16-byte stores where every row of out allows them
-  if (aligned_to(c.out, 16) && c.stride * float_bytes(T) % 16 == 0)
-    hipLaunchKernelGGL((k_mx4_matmul_tile<T, MF, true>), grid, dim3(256), 0, c.s, c.ac, c.as, c.m, c.bc, c.bs, c.n,
-                       c.steps, c.out, c.stride, int(mt));
-  else
-    hipLaunchKernelGGL((k_mx4_matmul_tile<T, MF, false>), grid, dim3(256), 0, c.s, c.ac, c.as, c.m, c.bc, c.bs, c.n,
-                       c.steps, c.out, c.stride, int(mt));
+  hipLaunchKernelGGL((k_mx4_matmul_tile<T, MF>), grid, dim3(256), 0, c.s, c.ac, c.as, c.m, c.bc, c.bs, c.n, c.steps,
+                     c.out, c.stride, int(mt));
 }
 
 template <int T, int MT, int NT>
@@ -301,26 +299,30 @@ static void launch_matmul_direct(const Mx4MatmulCall &c) {
                      c.steps, c.out, c.stride);
 }
 
-// LDS tiles where 64 of 128 x 256 are there to be had, of 256 x 256 where those
-// fill the GPU's 256 CUs; else straight from memory, a wavefront taking 64 x 64
-// of out, or 32 x 32 or 16 x 16 where there would be less than four wavefronts
-// to a CU.  us, m x n x dim to float32:
-//                        tiles 256  128   direct 64   32    16
-//     256 x  4,096 x  768      13.7   9.1       10.9   6.1   9.0
-//     512 x  4,096 x  768      14.4   9.7       11.4  10.0  16.2
-//   1,024 x  1,024 x 1,024     15.0  10.0       18.5   9.8  16.3
-//     256 x  8,192 x 4,096     29.9  21.0       60.0  58.5 112.9
-//   1,024 x  4,096 x  768      15.6  10.9       13.1  17.6  30.9
-//   2,048 x  4,096 x  768      17.2  12.8       21.5  34.9  57.8
-//   4,096 x  4,096 x  128      15.2  16.7       15.4  15.9  18.8
-//      37 x 100,003 x  96      18.3  13.5        7.5   8.1   8.3
-//      64 x  4,096 x 4,096     26.8  19.3       58.3  30.0  16.1
-//       1 x 100,000 x 1,024                           19.0  16.7
+// LDS tiles where there are 64 of 128 x 256, and of 256 x 256 where those fill the
+// GPU's 256 CUs and no quarter of their rows is past the end; else straight from
+// memory, a wavefront taking 64 x 64 of out, or 32 x 32 or 16 x 16 where there
+// would be less than four wavefronts to a CU.  us, m x n x dim to float32 (three
+// as marked to bfloat16):
+//                                tiles 256   128  direct 64    32     16
+//     256 x   4,096 x   768           13.7   9.1       10.9   6.1    9.0
+//     512 x   4,096 x   768           14.4   9.7       11.4  10.0   16.2
+//   1,024 x   1,024 x 1,024           15.0  10.0       18.5   9.8   16.3
+//     256 x   8,192 x 4,096           29.9  21.0       60.0  58.5  112.9
+//   1,024 x   4,096 x   768           15.6  10.9       13.1  17.6   30.9
+//   2,048 x   4,096 x   768           17.2  12.8       21.5  34.9   57.8
+//   4,096 x   4,096 x   128           15.2  16.7       15.4  15.9   18.8
+//     300 x 100,000 x 1,024 bfloat16  59.1  43.2
+//     700 x 100,000 x   768 bfloat16  65.9  72.1
+//   8,192 x  32,768 x 4,096 bfloat16   607   850
+//      37 x 100,003 x    96           18.3  13.5        7.5   8.1    8.3
+//      64 x   4,096 x 4,096           26.8  19.3       58.3  30.0   16.1
+//       1 x 100,000 x 1,024                                  19.0   16.7
 template <int T>
 static void launch_matmul(const Mx4MatmulCall &c) {
   auto pieces = [&](int64_t rows, int64_t cols) { return ((c.m + rows - 1) / rows) * ((c.n + cols - 1) / cols); };
   if (c.m > 64 && c.n > 64 && pieces(128, kMmN) >= 64) {
-    if (pieces(256, kMmN) >= 256) launch_matmul_tile<T, 8>(c);
+    if (pieces(256, kMmN) >= 256 && 2 * pieces(128, kMmN) > 3 * pieces(256, kMmN)) launch_matmul_tile<T, 8>(c);
     else launch_matmul_tile<T, 4>(c);
   } else if (c.m > 32 && pieces(64, 64) >= 1024) {
     launch_matmul_direct<T, 4, 4>(c);
