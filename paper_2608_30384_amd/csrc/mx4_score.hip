@@ -285,9 +285,11 @@ __global__ void __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 1 : 2) k_mx4_gemm
   };
   f32x4 acc[MF][NF] = {};
   if (count > 0) {
-    // group grp, whose slabs of b are in places p .. p + 3 (the first one in LDS)
-    auto group = [&](int grp, auto p_) {
+    // group grp, whose slabs of b are in places p .. p + 3 (the first one in LDS);
+    // ahead: later groups of b are loaded
+    auto group = [&](int grp, auto p_, auto ahead_) {
       constexpr int p = decltype(p_)::value;
+      constexpr bool ahead = decltype(ahead_)::value;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int abuf = (AG < 4 ? j / AG : p / 4) & 1, next = (p + j + 1) & 7;
@@ -304,11 +306,11 @@ __global__ void __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 1 : 2) k_mx4_gemm
             for (int c = 0; c < NF; ++c) acc[i][c] = mfma_bf16(fb[c], fa, acc[i][c]);
           }
         put_b(4 * grp + j + 1, next, (j + 1) & 1);
-        if (TRANS) load_b(4 * grp + j + 9, next);
-        else if (j == 3) load_b4(grp + 2, p);
+        if (TRANS && ahead) load_b(4 * grp + j + 9, next);
+        else if (ahead && j == 3) load_b4(grp + 2, p);
         // b's next slab is written; and x's next slabs are there, after which
-        // only the loads of b were issued
-        constexpr int kAfter = TRANS ? 2 * AG : 5;
+        // only the loads of b, where there are any, were issued
+        constexpr int kAfter = !ahead ? 0 : TRANS ? 2 * AG : 5;
         if (j % AG != AG - 1) arrive_lds();
         else if (TRANS || j == 3) arrive<kAfter>();
         else arrive<0>();
@@ -329,10 +331,10 @@ __global__ void __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 1 : 2) k_mx4_gemm
     arrive<0>();
     int grp = 0;
     for (; grp + 1 < count; grp += 2) {
-      group(grp, std::integral_constant<int, 0>{});
-      group(grp + 1, std::integral_constant<int, 4>{});
+      group(grp, std::integral_constant<int, 0>{}, std::true_type{});
+      group(grp + 1, std::integral_constant<int, 4>{}, std::true_type{});
     }
-    if (grp < count) group(grp, std::integral_constant<int, 0>{});
+    if (grp < count) group(grp, std::integral_constant<int, 0>{}, std::false_type{});
   }
 #pragma unroll
   for (int i = 0; i < MF; ++i) {
