@@ -318,6 +318,8 @@ static void launch_matmul_direct(const Mx4MatmulCall &c) {
 //      37 x 100,003 x    96           18.3  13.5        7.5   8.1    8.3
 //      64 x   4,096 x 4,096           26.8  19.3       58.3  30.0   16.1
 //       1 x 100,000 x 1,024                                  19.0   16.7
+// A grid of the 16 x 16 form counts its threads in 32 bits up to 2^30 rows of b;
+// past that 32 x 32.
 template <int T>
 static void launch_matmul(const Mx4MatmulCall &c) {
   auto pieces = [&](int64_t rows, int64_t cols) { return ((c.m + rows - 1) / rows) * ((c.n + cols - 1) / cols); };
@@ -326,7 +328,7 @@ static void launch_matmul(const Mx4MatmulCall &c) {
     else launch_matmul_tile<T, 4>(c);
   } else if (c.m > 32 && pieces(64, 64) >= 1024) {
     launch_matmul_direct<T, 4, 4>(c);
-  } else if (c.m > 16 && pieces(32, 32) >= 1024) {
+  } else if ((c.m > 16 || c.n > (1ll << 30)) && pieces(32, 32) >= 1024) {
     launch_matmul_direct<T, 2, 2>(c);
   } else {
     launch_matmul_direct<T, 1, 1>(c);

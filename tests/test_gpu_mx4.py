@@ -374,3 +374,18 @@ def test_matmul_of_many_tiles(R, m, n, dim, dt):
     keep = torch.ones(n, dtype=torch.bool, device="cuda")
     keep[n // 2] = False
     assert torch.equal(got[:m - 1, keep], plain[:m - 1, keep])
+
+
+def test_one_row_against_more_rows_than_a_small_grid_counts(R):
+    """2^30 + 5 rows of 4-bit codes (73 GB) to one row."""
+    n = (1 << 30) + 5
+    b = R.Mx4Rows.empty(n, 32, "cuda")
+    b.codes.zero_()
+    b.scales.fill_(127)
+    at = torch.tensor([0, 63, 1 << 26, (1 << 30) - 1, 1 << 30, n - 1], device="cuda")
+    b.codes[at, 3] = torch.arange(1, 7, device="cuda", dtype=torch.uint8)
+    a = R.rslm_mx4_quantize(torch.full((1, 32), 2.0, device="cuda"))
+    out = R.rslm_mx4_matmul(a, b, dtype=torch.bfloat16)
+    value = 2.0 * torch.tensor(mx4.E2M1[1:7], device="cuda", dtype=torch.float32)
+    assert torch.equal(out[0, at].float(), value)
+    assert torch.count_nonzero(out) == 6
