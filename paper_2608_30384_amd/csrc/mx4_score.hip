@@ -436,7 +436,11 @@ static int64_t groups_of(int64_t len) { return (len + 127) / 128; }
 static int tile_rows(int64_t m) { return m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : m <= 128 ? 128 : 256; }
 
 // Parts into which the sums over `len` values are split where m x cols has too
-// few tiles for the GPU: at least two groups of 128 each.  The gradient has long
+// few tiles for the GPU: at least two groups of 128 each, none without any.  As
+// many workgroups as the GPU holds at once (one of 8 wavefronts to a CU, two of 4),
+// and not one more, which all others would be waiting for: gradients of 256 x
+// 131,072 x 768 bfloat16 with 255 workgroups 62 us, with 258 103; 100 x 100,000 x 768
+// 41 and 64; 64 x 51,200 x 1,024 with 512 24, with 1,024 34.  The gradient has long
 // sums and small outputs; for scores, the parts (about 8 bytes written and read
 // for a value of each, at 5 TB/s) have to cost less than the groups that a
 // workgroup is spared (2 us each, for every part of a number).  us, whole and
@@ -446,12 +450,14 @@ static int tile_rows(int64_t m) { return m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ?
 static int sum_splits(int type, int64_t m, int64_t cols, int64_t len, bool backward) {
   const int bm = tile_rows(m);
   const int64_t tiles = (cols + 255) / 256 * ((m + bm - 1) / bm), groups = groups_of(len);
-  const int64_t want = backward ? ((bm <= 64 ? 1024 : 256) + tiles - 1) / tiles : 256 / tiles;
+  const int64_t want = (backward && bm <= 64 ? 512 : 256) / tiles;
   const int64_t most = (groups + 1) / 2;
   int64_t s = want < most ? want : most;
   if (!backward)
     while (s > 1 && m * cols * s > 1200000 * type_parts(type) * (groups - (groups + s - 1) / s)) --s;
-  return int(s < 1 ? 1 : s);
+  if (s < 1) s = 1;
+  const int64_t per = (groups + s - 1) / s;
+  return int((groups + per - 1) / per);
 }
 static size_t parts_bytes(int64_t m, int64_t cols, int splits) {
   return splits > 1 ? (size_t(splits) * size_t(m) * size_t(cols) * sizeof(float) + 255) & ~size_t(255) : 0;
