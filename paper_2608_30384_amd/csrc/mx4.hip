@@ -48,13 +48,16 @@ __global__ void __launch_bounds__(256) k_mx4_quantize(const void *__restrict__ x
   for (int64_t row = int64_t(blockIdx.x) * 16 + (threadIdx.x >> 4); row < n; row += int64_t(gridDim.x) * 16) {
     const typename FloatType<T>::type *xr = static_cast<const typename FloatType<T>::type *>(x) + row * stride;
     for (int t = t0; t < t1; t += kFlight) {
-      float v[kFlight][8];
+      Raw8<T> raw[kFlight];
 #pragma unroll
-      for (int u = 0; u < kFlight; ++u) load_float8<T>(v[u], xr, 128 * (t + u) + 8 * r, t + u < t1 ? dim : 0);
+      for (int u = 0; u < kFlight; ++u) load_raw8<T>(raw[u], xr, 128 * (t + u) + 8 * r, t + u < t1 ? dim : 0);
 #pragma unroll
       for (int u = 0; u < kFlight; ++u)
-        if (t + u < t1)
-          mx4_put8(v[u], codes + (row * steps + t + u) * 64, scales + (row * steps + t + u) * 4, r);
+        if (t + u < t1) {
+          float v[8];
+          raw_values<T>(v, raw[u]);
+          mx4_put8(v, codes + (row * steps + t + u) * 64, scales + (row * steps + t + u) * 4, r);
+        }
     }
   }
 }

@@ -71,23 +71,47 @@ __device__ __forceinline__ void store_float(void *p, int64_t i, float f) {
   else static_cast<uint16_t *>(p)[i] = float_to_h16<T>(f);
 }
 
+// row[c .. c + 7] as they are stored, 0 at and past dim.  Kept so until every
+// load of a thread is out: a conversion beside its load would wait for it.
+template <int T>
+struct Raw8 {
+  typename FloatType<T>::type v[8];
+};
+template <int T>
+__device__ __forceinline__ void load_raw8(Raw8<T> &p, const void *row, int c, int dim) {
+  typedef typename FloatType<T>::type F;
+  const F *x = static_cast<const F *>(row) + c;
+  if (c + 8 <= dim) {
+    if constexpr (T == RSLM_F32) {
+      const F32x8u a = *reinterpret_cast<const F32x8u *>(x);
+      __builtin_memcpy(&p, &a, sizeof(a));
+    } else {
+      const H16x8u a = *reinterpret_cast<const H16x8u *>(x);
+      __builtin_memcpy(&p, &a, sizeof(a));
+    }
+  } else if (c < dim) {
+    F e[8];   // a branch for each would wait for each
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = x[min(i, dim - 1 - c)];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p.v[i] = c + i < dim ? e[i] : F(0.f);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p.v[i] = F(0.f);
+  }
+}
+template <int T>
+__device__ __forceinline__ void raw_values(float (&v)[8], const Raw8<T> &p) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = float(p.v[i]);
+}
+
 // v[i] = row[c + i], 0 at and past dim.
 template <int T>
 __device__ __forceinline__ void load_float8(float (&v)[8], const void *row, int c, int dim) {
-  if (c + 8 <= dim) {
-    if constexpr (T == RSLM_F32) {
-      const F32x8u a = *reinterpret_cast<const F32x8u *>(static_cast<const float *>(row) + c);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = a.v[i];
-    } else {
-      const H16x8u a = *reinterpret_cast<const H16x8u *>(static_cast<const uint16_t *>(row) + c);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = h16_to_float<T>(a.v[i]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i < dim ? load_float<T>(row, c + i) : 0.f;
-  }
+  Raw8<T> p;
+  load_raw8<T>(p, row, c, dim);
+  raw_values<T>(v, p);
 }
 template <int T>
 __device__ __forceinline__ void store_float8(const float (&v)[8], void *row, int c, int dim) {
