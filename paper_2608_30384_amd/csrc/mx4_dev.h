@@ -193,7 +193,14 @@ __device__ __forceinline__ void mx4_values8(float (&v)[8], uint32_t w, uint32_t 
   v[0] = p0.x, v[1] = p0.y, v[2] = p1.x, v[3] = p1.y;
   v[4] = p2.x, v[5] = p2.y, v[6] = p3.x, v[7] = p3.y;
 }
-// The same in bfloat16, which holds every such value exactly.
+// Of the 4 codes of w's lower half.
+__device__ __forceinline__ f32x4 mx4_values4(uint32_t w, uint32_t s) {
+  const float a = e8m0_arg(s);
+  const f32x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, a, 0);
+  const f32x2 p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, a, 1);
+  return f32x4{p0.x, p0.y, p1.x, p1.y};
+}
+// 8 codes' values in bfloat16, which holds every such value exactly.
 __device__ __forceinline__ uint4 mx4_bf16x8(uint32_t w, float a) {
   return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, a, 0)),
                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, a, 1)),
