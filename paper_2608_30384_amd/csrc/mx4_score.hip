@@ -432,8 +432,20 @@ static unsigned value_groups(int64_t n) {
 static int type_parts(int type) { return type == RSLM_BF16 ? 1 : type == RSLM_F16 ? 2 : 3; }
 static int64_t groups_of(int64_t len) { return (len + 127) / 128; }
 
-// Rows of x in a workgroup's tile.
-static int tile_rows(int64_t m) { return m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : m <= 128 ? 128 : 256; }
+// Rows of x in a workgroup's tile.  Of 128 and 256, of which a CU holds one
+// workgroup, what keeps the CU for less time: rounds of 256 workgroups times the
+// groups of each, a group of 256 rows taking 1.6 times that of 128 rows.  Scores, us
+// with tiles of 128 and 256: 300 x 100,000 x 768 bfloat16 90, 115; 257 x 20,000 x 1,024
+// float32 49, 74; 384 x 30,000 x 1,536 float16 93, 74.
+static int tile_rows(int64_t m, int64_t cols, int64_t len) {
+  if (m <= 128) return m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : 128;
+  auto time = [&](int64_t rows) {
+    const int64_t tiles = (cols + 255) / 256 * ((m + rows - 1) / rows), groups = groups_of(len);
+    const int64_t splits = tiles < 256 ? 256 / tiles : 1;
+    return (tiles * splits + 255) / 256 * ((groups + splits - 1) / splits);
+  };
+  return 5 * time(128) < 8 * time(256) ? 128 : 256;
+}
 
 // Parts into which the sums over `len` values are split where m x cols has too
 // few tiles for the GPU: at least two groups of 128 each, none without any.  As
@@ -448,7 +460,7 @@ static int tile_rows(int64_t m) { return m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ?
 // 42; 300 x 2,000 x 1,024 bfloat16 32.9, 24.1; but 128 x 20,000 x 768 bfloat16 22.3,
 // 30.7, which stays whole.
 static int sum_splits(int type, int64_t m, int64_t cols, int64_t len, bool backward) {
-  const int bm = tile_rows(m);
+  const int bm = tile_rows(m, cols, len);
   const int64_t tiles = (cols + 255) / 256 * ((m + bm - 1) / bm), groups = groups_of(len);
   const int64_t want = (backward && bm <= 64 ? 512 : 256) / tiles;
   const int64_t most = (groups + 1) / 2;
@@ -506,7 +518,7 @@ static void launch_gemm_rows(const Mx4GemmCall &c, int splits, char *ws) {
     xp = planes;
   }
   constexpr int kAG = NS == 1 ? 2 : 1, kSmall = NS == 1 ? 4 : NS == 2 ? 2 : 1;
-  switch (tile_rows(c.m)) {
+  switch (tile_rows(c.m, TRANS ? c.dim : c.n, len)) {
     case 16: launch_gemm<TO, NS, 1, 1, 4, 4, 4, TRANS>(c, xp, pitch, plane, splits, part); break;
     case 32: launch_gemm<TO, NS, 2, 1, 4, 4, 4, TRANS>(c, xp, pitch, plane, splits, part); break;
     case 64: launch_gemm<TO, NS, 4, 1, 4, 4, kSmall, TRANS>(c, xp, pitch, plane, splits, part); break;
