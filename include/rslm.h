@@ -523,7 +523,7 @@ int rslm_mx4_score_backward(const void *dout, int32_t dtype, int64_t m, int64_t 
 
 /* ------------------------------------------------------------------------
  * Log probabilities over rows of scores.  With z_j = scale * scores[i][j]
- * (scale: the inverse temperature, > 0), of each row i:
+ * (scale: the inverse temperature, above 0 and at most 2^127), of each row i:
  *   lse      = log sum_j e^{z_j}
  *   logprob  = z_t - lse for the entry t = target[i]; 0 where target[i] is
  *              outside [0, n) (no target)

@@ -607,7 +607,8 @@ class LogProb:
 
 def rslm_logprob(scores, target=None, k=0, scale=1.0, stream=None):
     """Log probability of the entry target[i] (int64; outside the row: none) of
-    each row of scores, log-sum-exp, entropy, and the k most likely entries."""
+    each row of scores, log-sum-exp, entropy, and the k most likely entries.
+    scale: above 0, at most 2^127."""
     code, stride = _need_rows(scores, "scores")
     _need(target, torch.int64, "target")
     m, n = scores.shape

@@ -511,7 +511,8 @@ static void launch_logprob(const LogprobArgs &a, hipStream_t s) {
 static bool logprob_sizes_ok(int64_t m, int64_t n, int k) {
   return m >= 0 && n >= 1 && m <= 0x7fffffff / kLpMaxSlices && n <= 0x7fffffff && k >= 0 && k <= kMaxK;
 }
-static bool scale_ok(float scale) { return scale > 0.f && scale < __builtin_inff(); }
+// Up to 2^127: times log2(e) it has to stay within float32.
+static bool scale_ok(float scale) { return scale > 0.f && scale <= 0x1p127f; }
 
 }  // namespace rslm
 

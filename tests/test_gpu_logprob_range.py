@@ -1,0 +1,64 @@
+"""Log probabilities at the ends of float32's range, against float64.
+
+Tolerances, in units of U = 2^-24: z is known to 3 of them and a row of few entries
+has a log-sum-exp good to 8 (log n + 4); what is compared is at most 100 in
+magnitude, so 4 (100 + 8 (log n + 4)) U = 4e-5 covers values and, relative to the
+largest entry, gradients.
+"""
+
+import numpy as np
+import pytest
+
+from oracle import mx4
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+TOL = 4e-5
+
+
+@pytest.fixture(scope="module")
+def R():
+    import paper_2608_30384_amd as R
+
+    return R
+
+
+def check(R, x, scale, target, dl=None, dh=None, k=3):
+    """x: float32 array of scores whose z is within float32."""
+    t = torch.from_numpy(x).cuda()
+    tt = torch.tensor(target, device="cuda")
+    r = R.rslm_logprob(t, tt, k, scale=scale)
+    s32 = float(np.float32(scale))
+    want = mx4.logprob(x, s32, target, k)
+    room = lambda w: TOL * np.maximum(1.0, np.abs(np.where(np.isfinite(w), w, 0.0)))
+    for name, got in (("lse", r.lse), ("entropy", r.entropy), ("logprob", r.logprob), ("top", r.top_logprob)):
+        g, w = got.double().cpu().numpy(), want[name]
+        with np.errstate(invalid="ignore"):
+            assert ((g == w) | (np.abs(g - w) <= room(w))).all(), (name, g, w)
+    assert np.array_equal(r.top_ids.cpu().numpy(), want["ids"])
+    if dl is not None:
+        d = [torch.tensor(v, dtype=torch.float32, device="cuda") for v in (dl, dh)]
+        g = R.rslm_logprob_backward(t, tt, r, d[0], d[1], scale=scale).double().cpu().numpy()
+        w = mx4.logprob_grad(x, s32, target, d[0].double().cpu().numpy(), d[1].double().cpu().numpy())
+        assert np.isfinite(g).all() and (np.abs(g - w) <= TOL * np.abs(w).max(1, keepdims=True)).all(), (g, w)
+    return r
+
+
+@pytest.mark.parametrize("n", [5, 9000])
+def test_largest_scale(R, n):
+    """2^127 is taken, and anything above it refused: its product with log2(e) is no float32."""
+    scale = 2.0 ** 127
+    x = np.full((3, n), -1.9, dtype=np.float32)
+    x[0, :3] = 0.25, 0.5, 0.5                        # z of 2^125 and 2^126: two equal ones
+    x[1, :4] = np.float32(np.array([0.0, -1.0, -2.0, -50.0]) / scale)
+    x[2, :2] = 0.0
+    check(R, x, scale, [1, 1, 0])
+    t = torch.from_numpy(x).cuda()
+    r = R.rslm_logprob(t, k=2, scale=scale)
+    for bad in (float(np.nextafter(np.float32(scale), np.float32(np.inf))), 3e38, float("inf"), 0.0, -1.0, float("nan")):
+        with pytest.raises(R.RslmError):
+            R.rslm_logprob(t, k=2, scale=bad)
+        with pytest.raises(R.RslmError):
+            R.rslm_logprob_backward(t, None, r, scale=bad)
