@@ -37,20 +37,31 @@ constexpr int kLpPiece = kLpThreads * kLpEach;
 constexpr int kLpMaxSlices = 256;
 constexpr int kLpNotes = 1024;
 
+// A difference of scores times scale, as (v part - m part) times rest, part a power
+// of two and the first of them one fused step: two scores may lie further apart than
+// float32's largest value, which at scales up to 1 is still a z of interest and
+// takes halves.  At larger ones such a z - lse is below float32's range anyway.
+struct ScoreStep {
+  float part, rest, c;   // c: rest log2(e)
+  __device__ __forceinline__ explicit ScoreStep(float scale)
+      : part(scale <= 1.f ? 0.5f : 1.f), rest(scale <= 1.f ? 2.f * scale : scale), c(rest * kLog2e) {}
+  __device__ __forceinline__ float apart(float v, float m) const { return fmaf(v, part, -(m * part)); }
+};
+
 // Running maximum (of the scores) and sums of part of a row.
 struct SoftSum {
   float m, z, w;
 };
 
 // The sums of a and b together.
-__device__ __forceinline__ SoftSum soft_join(const SoftSum &a, const SoftSum &b, float c) {
+__device__ __forceinline__ SoftSum soft_join(const SoftSum &a, const SoftSum &b, const ScoreStep &u) {
   const float m = fmaxf(a.m, b.m);
   if (m == -__builtin_inff()) {
     // nothing but masked entries, or NaN
     return SoftSum{m, a.z + b.z, a.w + b.w};
   }
   SoftSum r{m, 0.f, 0.f};
-  const float da = (a.m - m) * c, db = (b.m - m) * c;
+  const float da = u.apart(a.m, m) * u.c, db = u.apart(b.m, m) * u.c;
   // a part that is empty keeps what it has (0, or NaN): e^-inf times it
   const float ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
   r.z = a.z * ea + b.z * eb;
@@ -58,11 +69,11 @@ __device__ __forceinline__ SoftSum soft_join(const SoftSum &a, const SoftSum &b,
   return r;
 }
 
-__device__ __forceinline__ SoftSum soft_join_wave(SoftSum s, float c) {
+__device__ __forceinline__ SoftSum soft_join_wave(SoftSum s, const ScoreStep &u) {
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) {
     const SoftSum o{__shfl_xor(s.m, off, 64), __shfl_xor(s.z, off, 64), __shfl_xor(s.w, off, 64)};
-    s = soft_join(s, o, c);
+    s = soft_join(s, o, u);
   }
   return s;
 }
@@ -86,7 +97,8 @@ struct LogprobArgs {
 // z - lse of a score, from the row's largest and ln Z: exact to the last places
 // where z itself is large, and -infinity for a masked entry.
 __device__ __forceinline__ float log_of(float v, float m, float lz, float scale) {
-  return v * scale == -__builtin_inff() ? -__builtin_inff() : fmaf(v - m, scale, -lz);
+  const ScoreStep u(scale);
+  return v * scale == -__builtin_inff() ? -__builtin_inff() : fmaf(u.apart(v, m), u.rest, -lz);
 }
 
 // The score of the row's target, asked for early: two reads, one after the other.
@@ -290,7 +302,7 @@ __global__ void __launch_bounds__(kLpThreads) k_logprob(LogprobArgs a) {
   const int slice = int(blockIdx.x % a.slices);
   const int64_t j0 = int64_t(slice) * a.per, j1 = min(a.n, j0 + a.per);
   const typename FloatType<T>::type *x = static_cast<const typename FloatType<T>::type *>(a.scores) + row * a.stride;
-  const float c = a.scale * kLog2e;
+  const ScoreStep step(a.scale);
   const float ninf = -__builtin_inff();
   SoftSum s{ninf, 0.f, 0.f};
   float thr = ninf;     // at least k entries reach it
@@ -307,7 +319,7 @@ __global__ void __launch_bounds__(kLpThreads) k_logprob(LogprobArgs a) {
     if (j + kLpPiece < j1) load_piece<T>(next, x, j + kLpPiece, j1);
     if (top > s.m) {
       if (s.m > ninf) {
-        const float d = (s.m - top) * c, e = __builtin_amdgcn_exp2f(d);
+        const float d = step.apart(s.m, top) * step.c, e = __builtin_amdgcn_exp2f(d);
         s.w = e * (s.w + fmaxf(d, -200.f) * s.z);
         s.z *= e;
       }
@@ -316,7 +328,7 @@ __global__ void __launch_bounds__(kLpThreads) k_logprob(LogprobArgs a) {
     const float ref = s.m == ninf ? 0.f : s.m;
 #pragma unroll
     for (int i = 0; i < kLpEach; ++i) {
-      const float y = (v[i] - ref) * c;
+      const float y = step.apart(v[i], ref) * step.c;
       const float w = __builtin_amdgcn_exp2f(y);
       s.z += w;
       s.w = fmaf(w, fmaxf(y, -200.f), s.w);   // masked: w = 0 times -200
@@ -369,12 +381,12 @@ __global__ void __launch_bounds__(kLpThreads) k_logprob(LogprobArgs a) {
       __syncthreads();
     }
   }
-  s = soft_join_wave(s, c);
+  s = soft_join_wave(s, step);
   if (lane == 0) parts[wid] = s;
   __syncthreads();
   s = parts[0];
 #pragma unroll
-  for (int i = 1; i < kLpThreads / 64; ++i) s = soft_join(s, parts[i], c);
+  for (int i = 1; i < kLpThreads / 64; ++i) s = soft_join(s, parts[i], step);
   if (a.slices == 1) {
     if (tid == 0) lz_s = emit_row(a, row, s, target);
     __syncthreads();
@@ -403,7 +415,7 @@ __global__ void __launch_bounds__(kLpThreads) k_logprob_join(LogprobArgs a) {
   constexpr int kHeld = kSelCap / kLpThreads;
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
   const int64_t row = blockIdx.x;
-  const float c = a.scale * kLog2e;
+  const ScoreStep step(a.scale);
   SoftSum s{-__builtin_inff(), 0.f, 0.f};
   if (tid < a.slices) s = a.sums[row * a.slices + tid];
   Target target{};
@@ -430,12 +442,12 @@ __global__ void __launch_bounds__(kLpThreads) k_logprob_join(LogprobArgs a) {
   } else if (tid == 0) {
     target = target_of<T>(a, row);
   }
-  s = soft_join_wave(s, c);
+  s = soft_join_wave(s, step);
   if (lane == 0) parts[wid] = s;
   __syncthreads();
   s = parts[0];
 #pragma unroll
-  for (int i = 1; i < kLpThreads / 64; ++i) s = soft_join(s, parts[i], c);
+  for (int i = 1; i < kLpThreads / 64; ++i) s = soft_join(s, parts[i], step);
   if (tid == 0) lz_s = emit_row(a, row, s, target);
   if constexpr (TOP) {
     const float bound = top_bound(top, a.k, tops);
@@ -467,10 +479,11 @@ __global__ void __launch_bounds__(256) k_logprob_backward(const void *scores, in
     const float m = stats[2 * row], lz = stats[2 * row + 1];
     const float dl = dlogprob && t >= 0 && t < n ? dlogprob[row] : 0.f;
     const float dh = dentropy ? dentropy[row] : 0.f, h = dentropy ? entropy[row] : 0.f;
+    const ScoreStep u(scale);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       // 2^24 p, so that a p below float32's normal range keeps its digits
-      const float lp = fmaf(v[i] - m, scale, -lz);
+      const float lp = fmaf(u.apart(v[i], m), u.rest, -lz);
       const float p = __builtin_amdgcn_exp2f(fmaf(lp, kLog2e, 24.f));
       const float q = p * ((dl + dh * (fmaxf(lp, -1e4f) + h)) * scale);
       const float d = fmaf(q, -0x1p-24f, j0 + i == t ? dl * scale : 0.f);

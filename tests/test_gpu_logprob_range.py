@@ -34,8 +34,8 @@ def check(R, x, scale, target, dl=None, dh=None, k=3):
     want = mx4.logprob(x, s32, target, k)
     room = lambda w: TOL * np.maximum(1.0, np.abs(np.where(np.isfinite(w), w, 0.0)))
     for name, got in (("lse", r.lse), ("entropy", r.entropy), ("logprob", r.logprob), ("top", r.top_logprob)):
-        g, w = got.double().cpu().numpy(), want[name]
-        with np.errstate(invalid="ignore"):
+        with np.errstate(invalid="ignore", over="ignore"):
+            g, w = got.double().cpu().numpy(), want[name].astype(np.float32).astype(np.float64)
             assert ((g == w) | (np.abs(g - w) <= room(w))).all(), (name, g, w)
     assert np.array_equal(r.top_ids.cpu().numpy(), want["ids"])
     if dl is not None:
@@ -62,3 +62,15 @@ def test_largest_scale(R, n):
             R.rslm_logprob(t, k=2, scale=bad)
         with pytest.raises(R.RslmError):
             R.rslm_logprob_backward(t, None, r, scale=bad)
+
+
+@pytest.mark.parametrize("n", [5, 9000, 70001])
+@pytest.mark.parametrize("scale", [1e-38, 2e-38, 0.5, 1.0, 1.5])
+def test_scores_further_apart_than_the_largest_float(R, n, scale):
+    """z stays within float32 although differences of the scores do not."""
+    rng = np.random.default_rng(n)
+    x = rng.uniform(-3.3e38, 3.3e38, (4, n)).astype(np.float32) / np.float32(max(1.0, scale))
+    x[1] = np.where(np.arange(n) % 2, x.min(), x.max())
+    x[2, 0], x[2, n - 1] = x.max(), x.min()
+    x[3, 1:] = -np.inf
+    check(R, x, scale, [0, 1, n - 1, 0], [1e10, -1e10, 0.0, 1e10], [0.0, 1e10, 1e10, 0.0])
