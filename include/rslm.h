@@ -545,7 +545,7 @@ int rslm_mx4_score_backward(const void *dout, int32_t dtype, int64_t m, int64_t 
  *   dscores[i][j] = scale (dlogprob_i (1[j = t] - p_j)
  *                          - dentropy_i p_j (z_j - lse_i + entropy_i)),
  *   0 for masked entries and without a target's first term; type dtype,
- *   dstride >= n.  dscores may be scores (same stride).
+ *   dstride >= n.  scale dlogprob and scale dentropy have to be within float32.  dscores may be scores (same stride).
  * ------------------------------------------------------------------------ */
 size_t rslm_logprob_workspace(int64_t m, int64_t n, int32_t k);
 int rslm_logprob(const void *scores, int32_t dtype, int64_t m, int64_t n, int64_t stride, float scale,

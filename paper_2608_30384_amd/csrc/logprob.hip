@@ -479,14 +479,17 @@ __global__ void __launch_bounds__(256) k_logprob_backward(const void *scores, in
     const float m = stats[2 * row], lz = stats[2 * row + 1];
     const float dl = dlogprob && t >= 0 && t < n ? dlogprob[row] : 0.f;
     const float dh = dentropy ? dentropy[row] : 0.f, h = dentropy ? entropy[row] : 0.f;
+    const float a = dl * scale, b = dh * scale;   // here: a use beside its load would wait for it
+    // Of 2^24 p, so that a p below float32's normal range keeps its digits, the
+    // 2^-24 is taken off a and b, or where these are small themselves off the product.
+    const bool small = fmaxf(fabsf(a), fabsf(b)) < 0x1p-60f;
+    const float as = small ? a : a * 0x1p-24f, bs = small ? b : b * 0x1p-24f, rest = small ? -0x1p-24f : -1.f;
     const ScoreStep u(scale);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      // 2^24 p, so that a p below float32's normal range keeps its digits
       const float lp = fmaf(u.apart(v[i], m), u.rest, -lz);
       const float p = __builtin_amdgcn_exp2f(fmaf(lp, kLog2e, 24.f));
-      const float q = p * ((dl + dh * (fmaxf(lp, -1e4f) + h)) * scale);
-      const float d = fmaf(q, -0x1p-24f, j0 + i == t ? dl * scale : 0.f);
+      const float d = fmaf(p * fmaf(bs, fmaxf(lp, -1e4f) + h, as), rest, j0 + i == t ? a : 0.f);
       v[i] = v[i] * scale == -__builtin_inff() ? 0.f : d;
     }
     store_float8<T>(v, static_cast<typename FloatType<T>::type *>(out) + row * ostride + j0, 0, left);

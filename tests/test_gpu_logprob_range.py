@@ -74,3 +74,34 @@ def test_scores_further_apart_than_the_largest_float(R, n, scale):
     x[2, 0], x[2, n - 1] = x.max(), x.min()
     x[3, 1:] = -np.inf
     check(R, x, scale, [0, 1, n - 1, 0], [1e10, -1e10, 0.0, 1e10], [0.0, 1e10, 1e10, 0.0])
+
+
+@pytest.mark.parametrize("n", [5, 9000])
+@pytest.mark.parametrize("size,scale", [(1e33, 1.0), (3e37, 4.0), (1.0, 1e37), (1e-20, 1e36), (1e-33, 1.0), (1e-10, 1e-20),
+                                        (1e20, 1e-20)])
+def test_gradients_as_large_and_as_small_as_a_float(R, n, size, scale):
+    """Entry by entry: probabilities below float32's normal range too, where the
+    product with a large gradient is a normal number again.  An entry is off by the
+    error of z - lse (at most 150: 3 (150 + 8 (log n + 4)) U) relative to its terms'
+    magnitudes, and by float32's least normal number."""
+    rng = np.random.default_rng(n)
+    z = rng.uniform(-90.0, 0.0, (4, n))
+    x = (z / scale).astype(np.float32)
+    x[0, 1] = 0.0
+    t = [1, n - 1, 0, 2]
+    dl, dh = np.array([1.0, -1.0, 0.0, 0.5]) * size, np.array([0.0, 0.01, -0.01, 0.0]) * size
+    tt = torch.tensor(t, device="cuda")
+    xt = torch.from_numpy(x).cuda()
+    d = [torch.tensor(v, dtype=torch.float32, device="cuda") for v in (dl, dh)]
+    r = R.rslm_logprob(xt, tt, scale=scale)
+    g = R.rslm_logprob_backward(xt, tt, r, d[0], d[1], scale=scale).double().cpu().numpy()
+    s32 = float(np.float32(scale))
+    d = [v.double().cpu().numpy() for v in d]
+    want = mx4.logprob_grad(x, s32, t, d[0], d[1])
+    ref = mx4.logprob(x, s32, t)
+    hit = np.zeros((4, n))
+    hit[np.arange(4), t] = 1.0
+    terms = s32 * (np.abs(d[0])[:, None] * (hit + ref["p"]) + np.abs(d[1])[:, None] * ref["p"] * (np.abs(ref["logs"]) + ref["entropy"][:, None] + 1))
+    tol = 2.0 ** -24 * 3 * (150 + 8 * (np.log(n) + 4)) * terms + 2.0 ** -126
+    assert np.isfinite(g).all()
+    assert (np.abs(g - want) <= tol).all(), (g, want, tol)
