@@ -6,6 +6,7 @@
 // .. + 31 of a group of 128: 16 consecutive bytes of codes and one scale, as
 // the rows are stored.  The rows of b are the instruction's first operand, so
 // that a lane ends with four consecutive columns of one row of the output.
+#include "mx4_choice.h"
 #include "mx4_dev.h"
 
 #include <type_traits>
@@ -77,7 +78,6 @@ __global__ void __launch_bounds__(256) k_mx4_matmul(const uint8_t *__restrict__ 
 // fall on different banks; the exchange is in the address that a lane of the
 // load gives.  Rows of b are dealt to the fragments so that 16 lanes x 4 write
 // 64 consecutive bytes of each row of out.
-constexpr int kMmN = 256;               // rows of b
 constexpr int kMmRow = 128;             // bytes of a row's two groups
 
 template <int T, int MF>
@@ -292,46 +292,21 @@ static void launch_matmul_tile(const Mx4MatmulCall &c) {
                      c.out, c.stride, int(mt));
 }
 
-template <int T, int MT, int NT>
+template <int T, int F>
 static void launch_matmul_direct(const Mx4MatmulCall &c) {
-  const dim3 grid(unsigned((c.n + 64 * NT - 1) / (64 * NT)), unsigned((c.m + 16 * MT - 1) / (16 * MT)));
-  hipLaunchKernelGGL((k_mx4_matmul<T, MT, NT>), grid, dim3(256), 0, c.s, c.ac, c.as, c.m, c.bc, c.bs, c.n,
-                     c.steps, c.out, c.stride);
+  const Mx4DirectGrid g = matmul_direct_grid(c.m, c.n, 16 * F);
+  hipLaunchKernelGGL((k_mx4_matmul<T, F, F>), dim3(unsigned(g.x), unsigned(g.y)), dim3(256), 0, c.s, c.ac, c.as, c.m,
+                     c.bc, c.bs, c.n, c.steps, c.out, c.stride);
 }
 
-// LDS tiles where there are 64 of 128 x 256, and of 256 x 256 where those fill the
-// GPU's 256 CUs and no quarter of their rows is past the end; else straight from
-// memory, a wavefront taking 64 x 64 of out, or 32 x 32 or 16 x 16 where there
-// would be less than four wavefronts to a CU.  us, m x n x dim to float32 (three
-// as marked to bfloat16):
-//                                tiles 256   128  direct 64    32     16
-//     256 x   4,096 x   768           13.7   9.1       10.9   6.1    9.0
-//     512 x   4,096 x   768           14.4   9.7       11.4  10.0   16.2
-//   1,024 x   1,024 x 1,024           15.0  10.0       18.5   9.8   16.3
-//     256 x   8,192 x 4,096           29.9  21.0       60.0  58.5  112.9
-//   1,024 x   4,096 x   768           15.6  10.9       13.1  17.6   30.9
-//   2,048 x   4,096 x   768           17.2  12.8       21.5  34.9   57.8
-//   4,096 x   4,096 x   128           15.2  16.7       15.4  15.9   18.8
-//     300 x 100,000 x 1,024 bfloat16  59.1  43.2
-//     700 x 100,000 x   768 bfloat16  65.9  72.1
-//   8,192 x  32,768 x 4,096 bfloat16   607   850
-//      37 x 100,003 x    96           18.3  13.5        7.5   8.1    8.3
-//      64 x   4,096 x 4,096           26.8  19.3       58.3  30.0   16.1
-//       1 x 100,000 x 1,024                                  19.0   16.7
-// A grid of the 16 x 16 form counts its threads in 32 bits up to 2^30 rows of b;
-// past that 32 x 32.
 template <int T>
 static void launch_matmul(const Mx4MatmulCall &c) {
-  auto pieces = [&](int64_t rows, int64_t cols) { return ((c.m + rows - 1) / rows) * ((c.n + cols - 1) / cols); };
-  if (c.m > 64 && c.n > 64 && pieces(128, kMmN) >= 64) {
-    if (pieces(256, kMmN) >= 256 && 2 * pieces(128, kMmN) > 3 * pieces(256, kMmN)) launch_matmul_tile<T, 8>(c);
-    else launch_matmul_tile<T, 4>(c);
-  } else if (c.m > 32 && pieces(64, 64) >= 1024) {
-    launch_matmul_direct<T, 4, 4>(c);
-  } else if ((c.m > 16 || c.n > (1ll << 30)) && pieces(32, 32) >= 1024) {
-    launch_matmul_direct<T, 2, 2>(c);
-  } else {
-    launch_matmul_direct<T, 1, 1>(c);
+  switch (matmul_form(c.m, c.n)) {
+    case kMmTile256: launch_matmul_tile<T, 8>(c); break;
+    case kMmTile128: launch_matmul_tile<T, 4>(c); break;
+    case kMmDirect64: launch_matmul_direct<T, 4>(c); break;
+    case kMmDirect32: launch_matmul_direct<T, 2>(c); break;
+    default: launch_matmul_direct<T, 1>(c);
   }
 }
 
