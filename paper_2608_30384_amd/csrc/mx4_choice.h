@@ -54,4 +54,12 @@ inline Mx4MatmulForm matmul_form(int64_t m, int64_t n) {
   return kMmDirect16;
 }
 
+// ---- float by 4-bit (mx4_score.hip)
+
+// The gradient's row of b, from the first of its part of the sum, whose code a thread
+// takes in a slab of 32 rows, `own` its place among them; at and past the part's end
+// too.  Unsigned: slabs ahead of the last group pass 2^31 where one part has all of
+// 2^31 - 256 rows.
+constexpr uint32_t slab_row(int own, int slab) { return uint32_t(own) + 32u * uint32_t(slab); }
+
 }  // namespace rslm

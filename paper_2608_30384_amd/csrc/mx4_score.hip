@@ -6,6 +6,7 @@
 // 2 (float16) or 3 (float32) bfloat16 parts, cut off the top of its significand
 // one after the other.  The products of the parts are exact in the matrix
 // cores' float32, so the result has the error of a float32 sum.
+#include "mx4_choice.h"
 #include "mx4_dev.h"
 
 #include <type_traits>
@@ -226,9 +227,9 @@ __global__ void __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 1 : 2) k_mx4_gemm
   const int block = TRANS ? min(int(c0 / 32) + (own & 7), 4 * steps - 1) : 0;
   const uint8_t *pc = bc + (TRANS ? (row0 * steps * 4 + block) * 16 : (row0 * steps + g0) * 64) + in_block;
   const uint8_t *ps = bs + (TRANS ? row0 * steps * 4 + block : (row0 * steps + g0) * 4);
-  const int last = TRANS ? int(min(n - g0 * 128, int64_t(count) * 128)) - 1 : 0;   // row of b, from row0
+  const uint32_t last = TRANS ? uint32_t(min(n - g0 * 128, int64_t(count) * 128)) - 1u : 0u;   // row of b, from row0
   auto load_b = [&](int slab, int place) {   // TRANS
-    const uint32_t row = min((own >> 3) + 32 * slab, last);   // past the end: the last one, and zeros (put_b)
+    const uint32_t row = min(slab_row(own >> 3, slab), last);   // past the end: the last one, and zeros (put_b)
     q[place] = *reinterpret_cast<const words *>(pc + uint64_t(row) * uint32_t(64 * steps));
     sc[place] = ps[uint64_t(row) * uint32_t(4 * steps)];
   };
@@ -250,7 +251,7 @@ __global__ void __launch_bounds__(64 * WM * WN, WM * WN == 8 ? 1 : 2) k_mx4_gemm
     // the loads are waited for here: the compiler would do the selections and
     // shifts below, of all places, where the loads were just issued
     asm volatile("" : "+v"(q[place]), "+v"(sc[place]));
-    const int in = TRANS ? -int((own >> 3) + 32 * slab <= last) : -1;
+    const int in = TRANS ? -int(slab_row(own >> 3, slab) <= last) : -1;
     const float a = e8m0_arg((TRANS ? sc[place] : sc[place] >> (8 * (place & 3)) & 255u) & uint32_t(in));
 #pragma unroll
     for (int i = 0; i < kWords; ++i) {

@@ -13,6 +13,8 @@ int main() {
       const int side = f == rslm::kMmDirect64 ? 64 : f == rslm::kMmDirect32 ? 32 : f == rslm::kMmDirect16 ? 16 : 0;
       const rslm::Mx4DirectGrid g = side ? rslm::matmul_direct_grid(a, b, side) : rslm::Mx4DirectGrid{0, 0};
       std::printf("%d %lld %lld\n", side ? side : f == rslm::kMmTile256 ? 256 : 128, (long long)g.x, (long long)g.y);
+    } else if (!std::strcmp(what, "slab_row")) {   // own slab
+      std::printf("%lld\n", (long long)rslm::slab_row(int(a), int(b)));
     } else {
       return 1;
     }

@@ -41,3 +41,14 @@ def test_direct_grids_hold_their_threads(ask):
             if side < 128:
                 assert x * 256 < 1 << 32 and y <= 65535, (m, n, side, x, y)
                 assert x * 4 * side >= n and y * side >= m
+
+
+def test_rows_of_the_longest_sums(ask):
+    """The slabs that the gradient asks for run up to eight past its last group: none
+    comes out as a row inside the sum (nor, as a 32-bit number that has wrapped, below it)."""
+    for rows in (1, 128, 129, MOST_ROWS // 2, MOST_ROWS - 511, MOST_ROWS - 1, MOST_ROWS):
+        groups = -(-rows // 128)
+        slabs = range(max(0, 4 * groups - 9), 4 * groups + 9)
+        for own in (0, 31):
+            for slab, (row,) in zip(slabs, ask("slab_row", [(own, s) for s in slabs])):
+                assert row == own + 32 * slab
