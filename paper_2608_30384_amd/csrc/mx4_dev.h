@@ -219,17 +219,19 @@ __device__ __forceinline__ i32x4 buffer_of(const uint8_t *p, int64_t bytes) {
   r[3] = 0x00020000;   // raw, 32-bit; reads past the end give 0
   return r;
 }
-// 64 lanes x 16 bytes from the buffer to LDS, lane l's at lds + 16 l.
+// 64 lanes x 16 bytes from the buffer to LDS, lane l's at lds + 16 l.  The LDS
+// address goes in m0, which the compiler writes, as it may hold a value of its own
+// there; one instruction has to come between (it may be the s_nop).
 // The whole offset is the lane's, which the end of the buffer is checked against.
 __device__ __forceinline__ void load_to_lds(i32x4 buf, uint32_t lds, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
-               : "s"(lds), "v"(offset), "s"(buf)
+               : "{m0}"(lds), "v"(offset), "s"(buf)
                : "memory");
 }
 // The same from 64 addresses, one of each lane.
 __device__ __forceinline__ void load_to_lds(const void *p, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(p) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "{m0}"(lds), "v"(p) : "memory");
 }
 __device__ __forceinline__ uint32_t lds_address(const void *p) {
   return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char *)p));

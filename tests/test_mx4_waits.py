@@ -104,3 +104,30 @@ def test_the_count_itself():
     assert counted_waits([load, lds, load, wait, "s_barrier"]) == [(2, 1)]
     assert counted_waits([lds, load, load, "<L3>:", wait, "s_barrier"]) == [(2, None)]
     assert counted_waits([lds, load, load, "s_waitcnt vmcnt(0)", "s_barrier"]) == []
+
+
+def asm_statements(text):
+    """Every inline assembly statement, from its parenthesis to the matching one."""
+    for m in re.finditer(r"\basm\s*(?:volatile)?\s*\(", text):
+        depth, quoted, i = 1, False, m.end()
+        while depth:
+            c = text[i]
+            if c == '"' and text[i - 1] != "\\":
+                quoted = not quoted
+            elif not quoted:
+                depth += (c == "(") - (c == ")")
+            i += 1
+        yield text[m.end():i - 1]
+
+
+def test_inline_assembly_leaves_m0_to_the_compiler():
+    """Loads to LDS take their address in m0, where the compiler may keep values of its
+    own: it is an operand of the statement, and no statement writes it."""
+    seen = 0
+    for f in sorted(os.listdir(B.CSRC)):
+        for s in asm_statements(open(os.path.join(B.CSRC, f)).read()):
+            assert not re.search(r"\b[sv]_\w+ m0\b", s), (f, s)
+            if re.search(r"load_lds|offen lds", s):
+                seen += 1
+                assert re.search(r'"\{m0\}"', s), (f, s)
+    assert seen == 2
