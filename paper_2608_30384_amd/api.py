@@ -598,11 +598,12 @@ def rslm_mx4_score_backward(dout, b, dtype=None, out=None, stream=None):
 class LogProb:
     """What ``rslm_logprob`` returns, float32 except top_ids (int32): logprob
     (None without targets), lse and entropy (m), top_logprob and top_ids (m x k),
-    and stats (m x 2), which the gradient takes."""
+    and stats (m x 2) and scale (a number), which the gradient takes."""
 
-    def __init__(self, logprob, lse, entropy, stats, top_logprob, top_ids):
+    def __init__(self, logprob, lse, entropy, stats, top_logprob, top_ids, scale=1.0):
         self.logprob, self.lse, self.entropy, self.stats = logprob, lse, entropy, stats
         self.top_logprob, self.top_ids = top_logprob, top_ids
+        self.scale = scale
 
 
 def rslm_logprob(scores, target=None, k=0, scale=1.0, stream=None):
@@ -622,7 +623,7 @@ def rslm_logprob(scores, target=None, k=0, scale=1.0, stream=None):
     logprob, lse, entropy, stats, top = torch.empty(
         m * (5 + k), dtype=torch.float32, device=scores.device).split([m, m, m, 2 * m, k * m])
     r = LogProb(logprob if target is not None else None, lse, entropy, stats.view(m, 2), top.view(m, k),
-                torch.empty((m, k), dtype=torch.int32, device=scores.device))
+                torch.empty((m, k), dtype=torch.int32, device=scores.device), scale)
     nb = L.lib().rslm_logprob_workspace(m, n, k)
     ws = _WS.get(nb, scores.device, "logprob", stream) if nb else None
     L.check("rslm_logprob", L.lib().rslm_logprob(
@@ -632,10 +633,13 @@ def rslm_logprob(scores, target=None, k=0, scale=1.0, stream=None):
     return r
 
 
-def rslm_logprob_backward(scores, target, result, dlogprob=None, dentropy=None, scale=1.0, out=None,
+def rslm_logprob_backward(scores, target, result, dlogprob=None, dentropy=None, scale=None, out=None,
                           stream=None):
     """The gradient of scores from those of logprob and entropy (None: zero);
-    result: what ``rslm_logprob`` returned for these scores."""
+    result: what ``rslm_logprob`` returned for these scores, whose scale it is (another
+    one is refused)."""
+    if scale is not None and C.c_float(scale).value != C.c_float(result.scale).value:
+        raise ValueError(f"scale must be that of the result ({result.scale}), got {scale}")
     code, stride = _need_rows(scores, "scores")
     _need(target, torch.int64, "target")
     _need(dlogprob, torch.float32, "dlogprob")
@@ -648,6 +652,6 @@ def rslm_logprob_backward(scores, target, result, dlogprob=None, dentropy=None, 
             _same_device(scores, t, name)
     out, _, ostride = _out_rows(out, (m, n), scores.dtype, scores.device)
     L.check("rslm_logprob_backward", L.lib().rslm_logprob_backward(
-        _at(scores), code, m, n, stride, scale, _at(target), _at(result.stats), _at(result.entropy),
+        _at(scores), code, m, n, stride, result.scale, _at(target), _at(result.stats), _at(result.entropy),
         _at(dlogprob), _at(dentropy), _at(out), ostride, _raw_stream(stream, out.device)))
     return out

@@ -60,8 +60,9 @@ def test_largest_scale(R, n):
     for bad in (float(np.nextafter(np.float32(scale), np.float32(np.inf))), 3e38, float("inf"), 0.0, -1.0, float("nan")):
         with pytest.raises(R.RslmError):
             R.rslm_logprob(t, k=2, scale=bad)
+        r.scale = bad
         with pytest.raises(R.RslmError):
-            R.rslm_logprob_backward(t, None, r, scale=bad)
+            R.rslm_logprob_backward(t, None, r)
 
 
 @pytest.mark.parametrize("n", [5, 9000, 70001])
