@@ -465,6 +465,15 @@ def _need_rows(t, name, shape=None):
     return code, t.stride(0)
 
 
+def _no_history(**inputs):
+    """Refuses tensors that autograd would follow: the results have no history, and a
+    gradient through them would be lost without an error."""
+    for name, t in inputs.items():
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name} requires a gradient, which these calls do not record: take it from the "
+                             f"_backward function, and call under torch.no_grad() or pass {name}.detach()")
+
+
 def _out_rows(out, shape, dtype, device, name="out"):
     if out is None:
         return torch.empty(shape, dtype=dtype, device=device), _float_type(dtype, name), shape[1]
@@ -563,7 +572,9 @@ def rslm_mx4_matmul(a, b, dtype=torch.float32, out=None, stream=None):
 
 
 def rslm_mx4_score(x, b, dtype=torch.float32, out=None, stream=None):
-    """x b^T of float rows x and MX4 rows b; dtype: float32 or x's."""
+    """x b^T of float rows x and MX4 rows b; dtype: float32 or x's.  The gradient is
+    ``rslm_mx4_score_backward``'s: autograd does not follow the call."""
+    _no_history(x=x)
     code, stride = _need_rows(x, "x")
     if x.shape[1] != b.dim:
         raise ValueError("x must have b's dimension")
@@ -580,6 +591,7 @@ def rslm_mx4_score(x, b, dtype=torch.float32, out=None, stream=None):
 def rslm_mx4_score_backward(dout, b, dtype=None, out=None, stream=None):
     """The gradient of ``rslm_mx4_score`` with respect to x: dout b (dout.shape[0] x
     b.dim); dtype: dout's (default) or float32."""
+    _no_history(dout=dout)
     code, stride = _need_rows(dout, "dout")
     if dout.shape[1] != b.n:
         raise ValueError("dout must have a column for every row of b")
@@ -609,7 +621,9 @@ class LogProb:
 def rslm_logprob(scores, target=None, k=0, scale=1.0, stream=None):
     """Log probability of the entry target[i] (int64; outside the row: none) of
     each row of scores, log-sum-exp, entropy, and the k most likely entries.
-    scale: above 0, at most 2^127."""
+    scale: above 0, at most 2^127.  The gradient is ``rslm_logprob_backward``'s: autograd
+    does not follow the call."""
+    _no_history(scores=scores)
     code, stride = _need_rows(scores, "scores")
     _need(target, torch.int64, "target")
     m, n = scores.shape
@@ -638,6 +652,7 @@ def rslm_logprob_backward(scores, target, result, dlogprob=None, dentropy=None, 
     """The gradient of scores from those of logprob and entropy (None: zero);
     result: what ``rslm_logprob`` returned for these scores, whose scale it is (another
     one is refused)."""
+    _no_history(scores=scores, dlogprob=dlogprob, dentropy=dentropy)
     if scale is not None and C.c_float(scale).value != C.c_float(result.scale).value:
         raise ValueError(f"scale must be that of the result ({result.scale}), got {scale}")
     code, stride = _need_rows(scores, "scores")

@@ -35,3 +35,50 @@ def test_gradient_has_the_scale_of_its_result(R):
             R.rslm_logprob_backward(x, t, r, one, scale=bad)
     third = R.rslm_logprob(x, t, scale=1.0 / 3.0)     # the same number in float32
     R.rslm_logprob_backward(x, t, third, one, scale=float(np.float32(1.0 / 3.0)))
+
+
+def test_inputs_that_autograd_follows_are_refused(R):
+    x = torch.randn(4, 96, device="cuda")
+    b = R.rslm_mx4_quantize(torch.randn(50, 96, device="cuda", requires_grad=True))     # codes have no gradient
+    t = torch.zeros(4, dtype=torch.int64, device="cuda")
+    s, one = R.rslm_mx4_score(x, b), torch.ones(4, device="cuda")
+    r = R.rslm_logprob(s, t)
+    want = [R.rslm_mx4_score_backward(s, b), R.rslm_logprob_backward(s, t, r, one, one)]
+    xg, sg, og = (v.clone().requires_grad_() for v in (x, s, one))
+    calls = [lambda: R.rslm_mx4_score(xg, b), lambda: R.rslm_mx4_score_backward(sg, b), lambda: R.rslm_logprob(sg, t),
+             lambda: R.rslm_logprob_backward(sg, t, r, one), lambda: R.rslm_logprob_backward(s, t, r, og),
+             lambda: R.rslm_logprob_backward(s, t, r, one, og), lambda: R.rslm_mx4_score(xg * 2, b)]
+    for call in calls:
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call()
+        with torch.no_grad():
+            call()
+    with torch.no_grad():
+        assert torch.equal(R.rslm_mx4_score(xg, b), s)
+        assert torch.equal(R.rslm_mx4_score_backward(sg, b), want[0])
+        assert torch.equal(R.rslm_logprob_backward(sg, t, r, og, og), want[1])
+
+
+def test_as_functions_of_autograd(R):
+    """Wrapped by a user: autograd's own rules call them without history.  Against
+    float64, relative to the norm: 1e-5, above the error of sums of 96 and 50 terms."""
+    b = R.rslm_mx4_quantize(torch.randn(50, 96, device="cuda"))
+    t = torch.tensor([3, 0, 49, 7], device="cuda")
+
+    class Loss(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x):
+            ctx.scores = R.rslm_mx4_score(x, b)
+            ctx.result = R.rslm_logprob(ctx.scores, t, scale=0.5)
+            return ctx.result.logprob.clone()
+
+        @staticmethod
+        def backward(ctx, d):
+            return R.rslm_mx4_score_backward(R.rslm_logprob_backward(ctx.scores, t, ctx.result, d.contiguous()), b)
+
+    x = torch.randn(4, 96, device="cuda", requires_grad=True)
+    (Loss.apply(x) * torch.tensor([1.0, 2.0, -1.0, 0.5], device="cuda")).sum().backward()
+    y = x.detach().double().cpu().requires_grad_()
+    z = torch.log_softmax(0.5 * (y @ R.rslm_mx4_dequantize(b).double().cpu().t()), 1)
+    (z[torch.arange(4), t.cpu()] * torch.tensor([1.0, 2.0, -1.0, 0.5], dtype=torch.float64)).sum().backward()
+    assert (x.grad.double().cpu() - y.grad).norm() <= 1e-5 * y.grad.norm()
