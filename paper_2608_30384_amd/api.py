@@ -474,9 +474,21 @@ def _no_history(**inputs):
                              f"_backward function, and call under torch.no_grad() or pass {name}.detach()")
 
 
-def _out_rows(out, shape, dtype, device, name="out"):
+def _empty(shape, dtype, device, stream):
+    """Memory for a result that `stream` (None: the current one) will write.  It is that
+    stream's own: a block of the current stream's may still be in use there.  And it
+    is not handed out again before the current stream is done with it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _out_rows(out, shape, dtype, device, stream, name="out"):
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device), _float_type(dtype, name), shape[1]
+        return _empty(shape, dtype, device, stream), _float_type(dtype, name), shape[1]
     if out.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {out.dtype}")
     code, stride = _need_rows(out, name, shape)
@@ -512,13 +524,13 @@ class Mx4Rows:
         self.codes, self.scales, self.dim = codes, scales, int(dim)
 
     @classmethod
-    def empty(cls, n, dim, device):
+    def empty(cls, n, dim, device, stream=None):
         if not 1 <= dim <= 65536:
             raise ValueError("dim must be 1..65536")
         steps = (dim + 127) // 128
         rows = cls.__new__(cls)   # what __init__ checks holds
-        rows.codes = torch.empty((n, 64 * steps), dtype=torch.uint8, device=device)
-        rows.scales = torch.empty((n, 4 * steps), dtype=torch.uint8, device=device)
+        rows.codes = _empty((n, 64 * steps), torch.uint8, device, stream)
+        rows.scales = _empty((n, 4 * steps), torch.uint8, device, stream)
         rows.dim = int(dim)
         return rows
 
@@ -539,7 +551,7 @@ def rslm_mx4_quantize(x, plan=None, rows=None, stream=None):
     if plan is not None and plan.dim != dim:
         raise ValueError("x must have the plan's dimension")
     if rows is None:
-        rows = Mx4Rows.empty(n, dim, x.device)
+        rows = Mx4Rows.empty(n, dim, x.device, stream)
     elif rows.n != n or rows.dim != dim:
         raise ValueError("rows must have the shape of x")
     else:
@@ -552,7 +564,7 @@ def rslm_mx4_quantize(x, plan=None, rows=None, stream=None):
 
 def rslm_mx4_dequantize(rows, dtype=torch.float32, out=None, stream=None):
     """The values of MX4 rows."""
-    out, code, stride = _out_rows(out, (rows.n, rows.dim), dtype, rows.device)
+    out, code, stride = _out_rows(out, (rows.n, rows.dim), dtype, rows.device, stream)
     L.check("rslm_mx4_dequantize", L.lib().rslm_mx4_dequantize(
         _at(rows.codes), _at(rows.scales), rows.n, rows.dim, _at(out), code, stride,
         _raw_stream(stream, out.device)))
@@ -564,7 +576,7 @@ def rslm_mx4_matmul(a, b, dtype=torch.float32, out=None, stream=None):
     if a.dim != b.dim:
         raise ValueError("a and b must have the same dimension")
     _same_device(a, b, "b")
-    out, code, stride = _out_rows(out, (a.n, b.n), dtype, a.device)
+    out, code, stride = _out_rows(out, (a.n, b.n), dtype, a.device, stream)
     L.check("rslm_mx4_matmul", L.lib().rslm_mx4_matmul(
         _at(a.codes), _at(a.scales), a.n, _at(b.codes), _at(b.scales), b.n, a.dim, _at(out),
         code, stride, _raw_stream(stream, out.device)))
@@ -579,7 +591,7 @@ def rslm_mx4_score(x, b, dtype=torch.float32, out=None, stream=None):
     if x.shape[1] != b.dim:
         raise ValueError("x must have b's dimension")
     _same_device(x, b, "b")
-    out, ocode, ostride = _out_rows(out, (x.shape[0], b.n), dtype, x.device)
+    out, ocode, ostride = _out_rows(out, (x.shape[0], b.n), dtype, x.device, stream)
     nb = L.lib().rslm_mx4_score_workspace(x.shape[0], b.n, b.dim, code)
     ws = _WS.get(nb, x.device, "mx4_score", stream) if nb else None
     L.check("rslm_mx4_score", L.lib().rslm_mx4_score(
@@ -597,7 +609,7 @@ def rslm_mx4_score_backward(dout, b, dtype=None, out=None, stream=None):
         raise ValueError("dout must have a column for every row of b")
     _same_device(dout, b, "b")
     m = dout.shape[0]
-    out, ocode, ostride = _out_rows(out, (m, b.dim), dout.dtype if dtype is None else dtype, dout.device)
+    out, ocode, ostride = _out_rows(out, (m, b.dim), dout.dtype if dtype is None else dtype, dout.device, stream)
     nb = L.lib().rslm_mx4_score_backward_workspace(m, b.n, b.dim, code)
     ws = _WS.get(nb, dout.device, "mx4_backward", stream) if nb else None
     L.check("rslm_mx4_score_backward", L.lib().rslm_mx4_score_backward(
@@ -634,10 +646,10 @@ def rslm_logprob(scores, target=None, k=0, scale=1.0, stream=None):
             raise ValueError("target must have an entry for every row of scores")
         _same_device(scores, target, "target")
     # one allocation for the row numbers: these calls are short
-    logprob, lse, entropy, stats, top = torch.empty(
-        m * (5 + k), dtype=torch.float32, device=scores.device).split([m, m, m, 2 * m, k * m])
+    logprob, lse, entropy, stats, top = _empty(
+        m * (5 + k), torch.float32, scores.device, stream).split([m, m, m, 2 * m, k * m])
     r = LogProb(logprob if target is not None else None, lse, entropy, stats.view(m, 2), top.view(m, k),
-                torch.empty((m, k), dtype=torch.int32, device=scores.device), scale)
+                _empty((m, k), torch.int32, scores.device, stream), scale)
     nb = L.lib().rslm_logprob_workspace(m, n, k)
     ws = _WS.get(nb, scores.device, "logprob", stream) if nb else None
     L.check("rslm_logprob", L.lib().rslm_logprob(
@@ -665,7 +677,7 @@ def rslm_logprob_backward(scores, target, result, dlogprob=None, dentropy=None, 
             if t.shape != (m,):
                 raise ValueError(f"{name} must have an entry for every row of scores")
             _same_device(scores, t, name)
-    out, _, ostride = _out_rows(out, (m, n), scores.dtype, scores.device)
+    out, _, ostride = _out_rows(out, (m, n), scores.dtype, scores.device, stream)
     L.check("rslm_logprob_backward", L.lib().rslm_logprob_backward(
         _at(scores), code, m, n, stride, result.scale, _at(target), _at(result.stats), _at(result.entropy),
         _at(dlogprob), _at(dentropy), _at(out), ostride, _raw_stream(stream, out.device)))

@@ -82,3 +82,88 @@ def test_as_functions_of_autograd(R):
     z = torch.log_softmax(0.5 * (y @ R.rslm_mx4_dequantize(b).double().cpu().t()), 1)
     (z[torch.arange(4), t.cpu()] * torch.tensor([1.0, 2.0, -1.0, 0.5], dtype=torch.float64)).sum().backward()
     assert (x.grad.double().cpu() - y.grad).norm() <= 1e-5 * y.grad.norm()
+
+
+def calls_on(R, x, b, t, plan):
+    """Every call, by name, as a function of stream; what it returns as a list of tensors."""
+    s = R.rslm_mx4_score(x, b)
+    r = R.rslm_logprob(s, t, 5)
+    one = torch.ones(x.shape[0], device="cuda")
+    return dict(
+        quantize=lambda st: [v for q in [R.rslm_mx4_quantize(x, stream=st)] for v in (q.codes, q.scales)],
+        rotated=lambda st: [v for q in [R.rslm_mx4_quantize(x, plan, stream=st)] for v in (q.codes, q.scales)],
+        dequantize=lambda st: [R.rslm_mx4_dequantize(b, stream=st)],
+        matmul=lambda st: [R.rslm_mx4_matmul(b, b, stream=st)],
+        score=lambda st: [R.rslm_mx4_score(x, b, stream=st)],
+        backward=lambda st: [R.rslm_mx4_score_backward(s, b, stream=st)],
+        logprob=lambda st: [v for q in [R.rslm_logprob(s, t, 5, stream=st)]
+                            for v in (q.logprob, q.lse, q.entropy, q.stats, q.top_logprob, q.top_ids)],
+        gradient=lambda st: [R.rslm_logprob_backward(s, t, r, one, one, stream=st)])
+
+
+NAMES = ["quantize", "rotated", "dequantize", "matmul", "score", "backward", "logprob", "gradient"]
+
+
+@pytest.mark.parametrize("name", NAMES)
+@pytest.mark.parametrize("m", [3, 70])
+def test_stream_argument(R, name, m):
+    """Work on the stream that is passed: it waits for what is ahead of it there, the
+    results are whole once that stream is done, and they are not in memory that the
+    current stream still writes."""
+    dim, n = 200, 3000
+    x, b = torch.randn(m, dim, device="cuda"), R.rslm_mx4_quantize(torch.randn(n, dim, device="cuda"))
+    t = torch.arange(m, device="cuda")
+    call = calls_on(R, x, b, t, R.Plan(dim, 4))[name]
+    want = [v.clone() for v in call(None)]
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    # blocks of the results' sizes, freed while the current stream has yet to write them
+    old = [torch.empty_like(v) for v in want]
+    torch.cuda._sleep(20_000_000)
+    for v in old:
+        v.fill_(7)
+    del old, v
+    got = call(s)
+    s.synchronize()
+    kept = [v.clone() for v in got]
+    torch.cuda.synchronize()
+    for g, w, k in zip(got, want, kept):
+        assert torch.equal(g, w) and torch.equal(k, w)
+    # inputs that the stream has yet to write: the call comes after
+    y = x.clone()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+        x.zero_()
+        x.add_(y)
+    got = call(s)
+    # read on the current stream, and freed while it has yet to be read
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda._sleep(20_000_000)
+    kept = [g.clone() for g in got]
+    shapes = [torch.empty_like(g, device="meta") for g in got]
+    del got, g
+    with torch.cuda.stream(s):
+        new = [torch.full_like(v, 9, device="cuda") for v in shapes]
+    torch.cuda.synchronize()
+    assert len(new) == len(want)
+    for k, w in zip(kept, want):
+        assert torch.equal(k, w)
+
+
+def test_workspaces_of_streams_are_their_own(R):
+    """The same long call on three streams at once, as an argument: each has its own scratch."""
+    b = R.rslm_mx4_quantize(torch.randn(5000, 256, device="cuda"))
+    xs = [torch.full((40, 256), float(i + 1), device="cuda") for i in range(3)]
+    want = [R.rslm_mx4_score(x, b) for x in xs]
+    grads = [R.rslm_mx4_score_backward(w, b) for w in want]
+    logs = [R.rslm_logprob(w[:3], k=20) for w in want]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = [(R.rslm_mx4_score(x, b, stream=s), R.rslm_mx4_score_backward(w, b, stream=s),
+                R.rslm_logprob(w[:3], k=20, stream=s)) for x, w, s in zip(xs, want, streams)]
+        torch.cuda.synchronize()
+        for (y, g, r), w, d, e in zip(got, want, grads, logs):
+            assert torch.equal(y, w) and torch.equal(g, d)
+            assert torch.equal(r.lse, e.lse) and torch.equal(r.top_ids, e.top_ids)
