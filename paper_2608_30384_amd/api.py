@@ -7,6 +7,7 @@ on the plan's device, with the dtypes stated in the C header.
 """
 
 import ctypes as C
+import functools
 
 import numpy as np
 import torch
@@ -446,6 +447,19 @@ def rslm_rescore_rslm(plan2, codes2, scales2, q_rot, cand_scores, cand_ids, k_ou
 _FLOATS = {torch.float32: L.RSLM_F32, torch.float16: L.RSLM_F16, torch.bfloat16: L.RSLM_BF16}
 
 
+def _launch_stream(stream, device):
+    """The hipStream_t for kernels on tensors of `device`.  They are launched on the
+    current device, where those of another would be addresses out of range."""
+    index, current = device.index, torch._C._cuda_getDevice()
+    if index == current:
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(index)
+        if stream.device_index == current:
+            return stream.cuda_stream
+    raise ValueError(f"tensors and stream must be on the current device (cuda:{current}), got {device}"
+                     + ("" if stream is None else f" and a stream of cuda:{stream.device_index}"))
+
+
 def _float_type(dtype, name):
     if dtype not in _FLOATS:
         raise TypeError(f"{name} must be float32, float16 or bfloat16, got {dtype}")
@@ -465,13 +479,12 @@ def _need_rows(t, name, shape=None):
     return code, t.stride(0)
 
 
-def _no_history(**inputs):
-    """Refuses tensors that autograd would follow: the results have no history, and a
+def _no_history(t, name):
+    """Refuses a tensor that autograd would follow: the results have no history, and a
     gradient through them would be lost without an error."""
-    for name, t in inputs.items():
-        if t is not None and t.requires_grad and torch.is_grad_enabled():
-            raise ValueError(f"{name} requires a gradient, which these calls do not record: take it from the "
-                             f"_backward function, and call under torch.no_grad() or pass {name}.detach()")
+    if t is not None and t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, which these calls do not record: take it from the "
+                         f"_backward function, and call under torch.no_grad() or pass {name}.detach()")
 
 
 def _empty(shape, dtype, device, stream):
@@ -488,7 +501,10 @@ def _empty(shape, dtype, device, stream):
 
 def _out_rows(out, shape, dtype, device, stream, name="out"):
     if out is None:
-        return _empty(shape, dtype, device, stream), _float_type(dtype, name), shape[1]
+        code = _float_type(dtype, name)
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=device), code, shape[1]
+        return _empty(shape, dtype, device, stream), code, shape[1]
     if out.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {out.dtype}")
     code, stride = _need_rows(out, name, shape)
@@ -529,8 +545,9 @@ class Mx4Rows:
             raise ValueError("dim must be 1..65536")
         steps = (dim + 127) // 128
         rows = cls.__new__(cls)   # what __init__ checks holds
-        rows.codes = _empty((n, 64 * steps), torch.uint8, device, stream)
-        rows.scales = _empty((n, 4 * steps), torch.uint8, device, stream)
+        make = torch.empty if stream is None else functools.partial(_empty, stream=stream)
+        rows.codes = make((n, 64 * steps), dtype=torch.uint8, device=device)
+        rows.scales = make((n, 4 * steps), dtype=torch.uint8, device=device)
         rows.dim = int(dim)
         return rows
 
@@ -548,17 +565,21 @@ def rslm_mx4_quantize(x, plan=None, rows=None, stream=None):
     rotated by the plan first if one is given."""
     code, stride = _need_rows(x, "x")
     n, dim = x.shape
-    if plan is not None and plan.dim != dim:
-        raise ValueError("x must have the plan's dimension")
+    device = x.device
+    if plan is not None:
+        if plan.dim != dim:
+            raise ValueError("x must have the plan's dimension")
+        if plan.device != device:
+            raise ValueError(f"x must be on the plan's device ({plan.device}), got {device}")
     if rows is None:
-        rows = Mx4Rows.empty(n, dim, x.device, stream)
+        rows = Mx4Rows.empty(n, dim, device, stream)
     elif rows.n != n or rows.dim != dim:
         raise ValueError("rows must have the shape of x")
     else:
         _same_device(x, rows, "rows")
     L.check("rslm_mx4_quantize", L.lib().rslm_mx4_quantize(
-        plan.handle if plan is not None else None, _at(x), code, n, dim, stride, _at(rows.codes),
-        _at(rows.scales), _raw_stream(stream, x.device)))
+        plan.handle if plan is not None else None, x.data_ptr(), code, n, dim, stride, rows.codes.data_ptr(),
+        rows.scales.data_ptr(), _launch_stream(stream, device)))
     return rows
 
 
@@ -566,8 +587,8 @@ def rslm_mx4_dequantize(rows, dtype=torch.float32, out=None, stream=None):
     """The values of MX4 rows."""
     out, code, stride = _out_rows(out, (rows.n, rows.dim), dtype, rows.device, stream)
     L.check("rslm_mx4_dequantize", L.lib().rslm_mx4_dequantize(
-        _at(rows.codes), _at(rows.scales), rows.n, rows.dim, _at(out), code, stride,
-        _raw_stream(stream, out.device)))
+        rows.codes.data_ptr(), rows.scales.data_ptr(), rows.n, rows.dim, out.data_ptr(), code, stride,
+        _launch_stream(stream, out.device)))
     return out
 
 
@@ -578,15 +599,15 @@ def rslm_mx4_matmul(a, b, dtype=torch.float32, out=None, stream=None):
     _same_device(a, b, "b")
     out, code, stride = _out_rows(out, (a.n, b.n), dtype, a.device, stream)
     L.check("rslm_mx4_matmul", L.lib().rslm_mx4_matmul(
-        _at(a.codes), _at(a.scales), a.n, _at(b.codes), _at(b.scales), b.n, a.dim, _at(out),
-        code, stride, _raw_stream(stream, out.device)))
+        a.codes.data_ptr(), a.scales.data_ptr(), a.n, b.codes.data_ptr(), b.scales.data_ptr(), b.n, a.dim, out.data_ptr(),
+        code, stride, _launch_stream(stream, out.device)))
     return out
 
 
 def rslm_mx4_score(x, b, dtype=torch.float32, out=None, stream=None):
     """x b^T of float rows x and MX4 rows b; dtype: float32 or x's.  The gradient is
     ``rslm_mx4_score_backward``'s: autograd does not follow the call."""
-    _no_history(x=x)
+    _no_history(x, "x")
     code, stride = _need_rows(x, "x")
     if x.shape[1] != b.dim:
         raise ValueError("x must have b's dimension")
@@ -595,15 +616,15 @@ def rslm_mx4_score(x, b, dtype=torch.float32, out=None, stream=None):
     nb = L.lib().rslm_mx4_score_workspace(x.shape[0], b.n, b.dim, code)
     ws = _WS.get(nb, x.device, "mx4_score", stream) if nb else None
     L.check("rslm_mx4_score", L.lib().rslm_mx4_score(
-        _at(x), code, x.shape[0], stride, _at(b.codes), _at(b.scales), b.n, b.dim, _at(out),
-        ocode, ostride, _at(ws), nb, _raw_stream(stream, out.device)))
+        x.data_ptr(), code, x.shape[0], stride, b.codes.data_ptr(), b.scales.data_ptr(), b.n, b.dim, out.data_ptr(),
+        ocode, ostride, _at(ws), nb, _launch_stream(stream, out.device)))
     return out
 
 
 def rslm_mx4_score_backward(dout, b, dtype=None, out=None, stream=None):
     """The gradient of ``rslm_mx4_score`` with respect to x: dout b (dout.shape[0] x
     b.dim); dtype: dout's (default) or float32."""
-    _no_history(dout=dout)
+    _no_history(dout, "dout")
     code, stride = _need_rows(dout, "dout")
     if dout.shape[1] != b.n:
         raise ValueError("dout must have a column for every row of b")
@@ -613,8 +634,8 @@ def rslm_mx4_score_backward(dout, b, dtype=None, out=None, stream=None):
     nb = L.lib().rslm_mx4_score_backward_workspace(m, b.n, b.dim, code)
     ws = _WS.get(nb, dout.device, "mx4_backward", stream) if nb else None
     L.check("rslm_mx4_score_backward", L.lib().rslm_mx4_score_backward(
-        _at(dout), code, m, stride, _at(b.codes), _at(b.scales), b.n, b.dim, _at(out), ocode,
-        ostride, _at(ws), nb, _raw_stream(stream, out.device)))
+        dout.data_ptr(), code, m, stride, b.codes.data_ptr(), b.scales.data_ptr(), b.n, b.dim, out.data_ptr(), ocode,
+        ostride, _at(ws), nb, _launch_stream(stream, out.device)))
     return out
 
 
@@ -635,7 +656,7 @@ def rslm_logprob(scores, target=None, k=0, scale=1.0, stream=None):
     each row of scores, log-sum-exp, entropy, and the k most likely entries.
     scale: above 0, at most 2^127.  The gradient is ``rslm_logprob_backward``'s: autograd
     does not follow the call."""
-    _no_history(scores=scores)
+    _no_history(scores, "scores")
     code, stride = _need_rows(scores, "scores")
     _need(target, torch.int64, "target")
     m, n = scores.shape
@@ -653,9 +674,9 @@ def rslm_logprob(scores, target=None, k=0, scale=1.0, stream=None):
     nb = L.lib().rslm_logprob_workspace(m, n, k)
     ws = _WS.get(nb, scores.device, "logprob", stream) if nb else None
     L.check("rslm_logprob", L.lib().rslm_logprob(
-        _at(scores), code, m, n, stride, scale, _at(target), k, _at(r.logprob), _at(r.lse),
-        _at(r.entropy), _at(r.stats), _at(r.top_logprob), _at(r.top_ids), _at(ws), nb,
-        _raw_stream(stream, scores.device)))
+        scores.data_ptr(), code, m, n, stride, scale, _at(target), k, _at(r.logprob), r.lse.data_ptr(),
+        r.entropy.data_ptr(), r.stats.data_ptr(), r.top_logprob.data_ptr(), r.top_ids.data_ptr(), _at(ws), nb,
+        _launch_stream(stream, scores.device)))
     return r
 
 
@@ -664,7 +685,9 @@ def rslm_logprob_backward(scores, target, result, dlogprob=None, dentropy=None, 
     """The gradient of scores from those of logprob and entropy (None: zero);
     result: what ``rslm_logprob`` returned for these scores, whose scale it is (another
     one is refused)."""
-    _no_history(scores=scores, dlogprob=dlogprob, dentropy=dentropy)
+    _no_history(scores, "scores")
+    _no_history(dlogprob, "dlogprob")
+    _no_history(dentropy, "dentropy")
     if scale is not None and C.c_float(scale).value != C.c_float(result.scale).value:
         raise ValueError(f"scale must be that of the result ({result.scale}), got {scale}")
     code, stride = _need_rows(scores, "scores")
@@ -679,6 +702,6 @@ def rslm_logprob_backward(scores, target, result, dlogprob=None, dentropy=None, 
             _same_device(scores, t, name)
     out, _, ostride = _out_rows(out, (m, n), scores.dtype, scores.device, stream)
     L.check("rslm_logprob_backward", L.lib().rslm_logprob_backward(
-        _at(scores), code, m, n, stride, result.scale, _at(target), _at(result.stats), _at(result.entropy),
-        _at(dlogprob), _at(dentropy), _at(out), ostride, _raw_stream(stream, out.device)))
+        scores.data_ptr(), code, m, n, stride, result.scale, _at(target), result.stats.data_ptr(), result.entropy.data_ptr(),
+        _at(dlogprob), _at(dentropy), out.data_ptr(), ostride, _launch_stream(stream, out.device)))
     return out
