@@ -59,8 +59,6 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 // 32 coordinates 32 g .. + 31 of a group of 128, as the rows are stored, and
 // multiplies eight of them at a time: the order of the sum is free, so x is read
 // in that order from LDS, where a workgroup keeps its parts for all its tiles.
-constexpr int kFewRows = 16, kFewLds = 65536;
-__host__ __device__ inline int few_pitch(int steps) { return steps * 256 + 16; }   // bytes of a row of a part
 
 template <int T, int TO, int NT>
 __global__ void __launch_bounds__(256) k_mx4_score_few(const void *__restrict__ x, int m, int64_t stride,
@@ -430,48 +428,6 @@ static unsigned value_groups(int64_t n) {
   return unsigned(g < (1 << 20) ? g : (1 << 20));
 }
 
-static int type_parts(int type) { return type == RSLM_BF16 ? 1 : type == RSLM_F16 ? 2 : 3; }
-static int64_t groups_of(int64_t len) { return (len + 127) / 128; }
-
-// Rows of x in a workgroup's tile.  Of 128 and 256, of which a CU holds one
-// workgroup, what keeps the CU for less time: rounds of 256 workgroups times the
-// groups of each, a group of 256 rows taking 1.6 times that of 128 rows.  Scores, us
-// with tiles of 128 and 256: 300 x 100,000 x 768 bfloat16 90, 115; 257 x 20,000 x 1,024
-// float32 49, 74; 384 x 30,000 x 1,536 float16 93, 74.
-static int tile_rows(int64_t m, int64_t cols, int64_t len) {
-  if (m <= 128) return m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : 128;
-  auto time = [&](int64_t rows) {
-    const int64_t tiles = (cols + 255) / 256 * ((m + rows - 1) / rows), groups = groups_of(len);
-    const int64_t splits = tiles < 256 ? 256 / tiles : 1;
-    return (tiles * splits + 255) / 256 * ((groups + splits - 1) / splits);
-  };
-  return 5 * time(128) < 8 * time(256) ? 128 : 256;
-}
-
-// Parts into which the sums over `len` values are split where m x cols has too
-// few tiles for the GPU: at least two groups of 128 each, none without any.  As
-// many workgroups as the GPU holds at once (one of 8 wavefronts to a CU, two of 4),
-// and not one more, which all others would be waiting for: gradients of 256 x
-// 131,072 x 768 bfloat16 with 255 workgroups 62 us, with 258 103; 100 x 100,000 x 768
-// 41 and 64; 64 x 51,200 x 1,024 with 512 24, with 1,024 34.  The gradient has long
-// sums and small outputs; for scores, the parts (about 8 bytes written and read
-// for a value of each, at 5 TB/s) have to cost less than the groups that a
-// workgroup is spared (2 us each, for every part of a number).  us, whole and
-// split: 118 x 100 x 2,917 float16 80.0, 19.2; 100 x 8,192 x 4,096 float32 146,
-// 42; 300 x 2,000 x 1,024 bfloat16 32.9, 24.1; but 128 x 20,000 x 768 bfloat16 22.3,
-// 30.7, which stays whole.
-static int sum_splits(int type, int64_t m, int64_t cols, int64_t len, bool backward) {
-  const int bm = tile_rows(m, cols, len);
-  const int64_t tiles = (cols + 255) / 256 * ((m + bm - 1) / bm), groups = groups_of(len);
-  const int64_t want = (backward && bm <= 64 ? 512 : 256) / tiles;
-  const int64_t most = (groups + 1) / 2;
-  int64_t s = want < most ? want : most;
-  if (!backward)
-    while (s > 1 && m * cols * s > 1200000 * type_parts(type) * (groups - (groups + s - 1) / s)) --s;
-  if (s < 1) s = 1;
-  const int64_t per = (groups + s - 1) / s;
-  return int((groups + per - 1) / per);
-}
 static size_t parts_bytes(int64_t m, int64_t cols, int splits) {
   return splits > 1 ? (size_t(splits) * size_t(m) * size_t(cols) * sizeof(float) + 255) & ~size_t(255) : 0;
 }
@@ -538,10 +494,6 @@ static void launch_gemm_types(const Mx4GemmCall &c, int type, int out_type, int 
   else launch_gemm_rows<RSLM_BF16, RSLM_F32, TRANS>(c, splits, w);
 }
 
-// Few rows: whether a workgroup's LDS holds their parts.
-static bool score_few_ok(int type, int64_t m, int dim) {
-  return m <= kFewRows && int64_t(type_parts(type)) * m * few_pitch(mx4_steps(dim)) <= kFewLds;
-}
 template <int T, int TO>
 static void launch_score_few(const Mx4GemmCall &c) {
   constexpr int NT = 2;

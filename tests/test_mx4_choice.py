@@ -22,7 +22,7 @@ def ask(tmp_path_factory):
                     os.path.join(ROOT, "tests", "mx4_choice_driver.cpp"), "-o", exe], check=True)
 
     def ask(what, sizes):
-        text = "".join(f"{what} " + " ".join(map(str, s)) + "\n" for s in sizes)
+        text = "".join(f"{what} " + " ".join(map(str, (*s, 0, 0, 0, 0)[:5])) + "\n" for s in sizes)
         r = subprocess.run([exe], input=text, capture_output=True, text=True)
         assert r.returncode == 0, r.stderr
         out = [tuple(map(int, line.split())) for line in r.stdout.splitlines()]
@@ -52,3 +52,27 @@ def test_rows_of_the_longest_sums(ask):
         for own in (0, 31):
             for slab, (row,) in zip(slabs, ask("slab_row", [(own, s) for s in slabs])):
                 assert row == own + 32 * slab
+
+
+def test_gpu_tests_reach_every_arrangement(ask):
+    """The sizes of test_gpu_mx4_tiles.py take every height of tiles of each direction, in one
+    part and in several, and every form of 4-bit by 4-bit: a rule that changes fails here."""
+    pytest.importorskip("torch")
+    from tests import test_gpu_mx4_tiles as T
+
+    for type_ in (0, 1, 2):
+        score = ask("gemm", [(type_, *s, 0) for s in T.SCORE])
+        assert {t for t, _ in score} == {0, 16, 32, 64, 128, 256}
+        back = ask("gemm", [(type_, *s, 1) for s in T.BACKWARD])
+        assert {t for t, _ in back} == {16, 32, 64, 128, 256}
+        for got in (score, back):
+            assert {(t, p > 1) for t, p in got if t >= 64} == {(t, p) for t in (64, 128, 256) for p in (False, True)}, got
+        # 256 rows with odd and even numbers of groups in a part
+        for sizes, got, length in ((T.SCORE, score, 2), (T.BACKWARD, back, 1)):
+            per = [-(-(-(-s[length] // 128)) // p) for s, (t, p) in zip(sizes, got) if t == 256]
+            assert {v % 2 for v in per} == {0, 1} and max(per) >= 5
+    forms = {}
+    for (m, n, dim, _), (side, _, _) in zip(T.MATMUL, ask("form", [s[:2] for s in T.MATMUL])):
+        forms.setdefault(side, set()).add(-(-dim // 128))
+    assert set(forms) == {256, 128, 64, 32, 16}
+    assert {5, 6, 8, 9} <= forms[256] and max(forms[128]) >= 9
