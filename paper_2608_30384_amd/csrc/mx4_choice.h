@@ -69,25 +69,10 @@ inline bool score_few_ok(int type, int64_t m, int dim) {
   return m <= kFewRows && int64_t(type_parts(type)) * m * few_pitch((dim + 127) / 128) <= kFewLds;
 }
 
-// Rows of x in a workgroup's tile.  Of 128 and 256, of which a CU holds one
-// workgroup, what keeps the CU for less time: rounds of 256 workgroups times the
-// groups of each, a group of 256 rows taking 1.6 times that of 128 rows.  Scores, us
-// with tiles of 128 and 256: 300 x 100,000 x 768 bfloat16 90, 115; 257 x 20,000 x 1,024
-// float32 49, 74; 384 x 30,000 x 1,536 float16 93, 74.
-inline int tile_rows(int64_t m, int64_t cols, int64_t len) {
-  if (m <= 128) return m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : 128;
-  auto time = [&](int64_t rows) {
-    const int64_t tiles = (cols + 255) / 256 * ((m + rows - 1) / rows), groups = groups_of(len);
-    const int64_t splits = tiles < 256 ? 256 / tiles : 1;
-    return (tiles * splits + 255) / 256 * ((groups + splits - 1) / splits);
-  };
-  return 5 * time(128) < 8 * time(256) ? 128 : 256;
-}
-
 // Parts into which the sums over `len` values are split where m x cols has too
-// few tiles for the GPU: at least two groups of 128 each, none without any.  As
-// many workgroups as the GPU holds at once (one of 8 wavefronts to a CU, two of 4),
-// and not one more, which all others would be waiting for: gradients of 256 x
+// few tiles of bm rows for the GPU: at least two groups of 128 each, none without
+// any.  As many workgroups as the GPU holds at once (one of 8 wavefronts to a CU, two of
+// 4), and not one more, which all others would be waiting for: gradients of 256 x
 // 131,072 x 768 bfloat16 with 255 workgroups 62 us, with 258 103; 100 x 100,000 x 768
 // 41 and 64; 64 x 51,200 x 1,024 with 512 24, with 1,024 34.  The gradient has long
 // sums and small outputs; for scores, the parts (about 8 bytes written and read
@@ -96,8 +81,7 @@ inline int tile_rows(int64_t m, int64_t cols, int64_t len) {
 // split: 118 x 100 x 2,917 float16 80.0, 19.2; 100 x 8,192 x 4,096 float32 146,
 // 42; 300 x 2,000 x 1,024 bfloat16 32.9, 24.1; but 128 x 20,000 x 768 bfloat16 22.3,
 // 30.7, which stays whole.
-inline int sum_splits(int type, int64_t m, int64_t cols, int64_t len, bool backward) {
-  const int bm = tile_rows(m, cols, len);
+inline int splits_of(int type, int64_t m, int64_t cols, int64_t len, bool backward, int bm) {
   const int64_t tiles = (cols + 255) / 256 * ((m + bm - 1) / bm), groups = groups_of(len);
   const int64_t want = (backward && bm <= 64 ? 512 : 256) / tiles;
   const int64_t most = (groups + 1) / 2;
@@ -107,6 +91,25 @@ inline int sum_splits(int type, int64_t m, int64_t cols, int64_t len, bool backw
   if (s < 1) s = 1;
   const int64_t per = (groups + s - 1) / s;
   return int((groups + per - 1) / per);
+}
+
+// Rows of x in a workgroup's tile.  Of 128 and 256, of which a CU holds one
+// workgroup, what keeps the CU for less time: rounds of 256 workgroups times the
+// groups of each, a group of 256 rows taking 1.6 times that of 128 rows.  Scores, us
+// with tiles of 128 and 256: 300 x 100,000 x 768 bfloat16 90, 115; 257 x 20,000 x 1,024
+// float32 49, 74; 384 x 30,000 x 1,536 float16 93, 74; 256 x 32,000 x 1,024 bfloat16,
+// whose sums stay whole, 27, 38.
+inline int tile_rows(int type, int64_t m, int64_t cols, int64_t len, bool backward) {
+  if (m <= 128) return m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : 128;
+  auto time = [&](int rows) {
+    const int64_t tiles = (cols + 255) / 256 * ((m + rows - 1) / rows);
+    const int64_t parts = splits_of(type, m, cols, len, backward, rows);
+    return (tiles * parts + 255) / 256 * ((groups_of(len) + parts - 1) / parts);
+  };
+  return 5 * time(128) < 8 * time(256) ? 128 : 256;
+}
+inline int sum_splits(int type, int64_t m, int64_t cols, int64_t len, bool backward) {
+  return splits_of(type, m, cols, len, backward, tile_rows(type, m, cols, len, backward));
 }
 
 // The gradient's row of b, from the first of its part of the sum, whose code a thread

@@ -475,7 +475,7 @@ static void launch_gemm_rows(const Mx4GemmCall &c, int splits, char *ws) {
     xp = planes;
   }
   constexpr int kAG = NS == 1 ? 2 : 1, kSmall = NS == 1 ? 4 : NS == 2 ? 2 : 1;
-  switch (tile_rows(c.m, TRANS ? c.dim : c.n, len)) {
+  switch (tile_rows(T, c.m, TRANS ? c.dim : c.n, len, TRANS)) {
     case 16: launch_gemm<TO, NS, 1, 1, 4, 4, 4, TRANS>(c, xp, pitch, plane, splits, part); break;
     case 32: launch_gemm<TO, NS, 2, 1, 4, 4, 4, TRANS>(c, xp, pitch, plane, splits, part); break;
     case 64: launch_gemm<TO, NS, 4, 1, 4, 4, kSmall, TRANS>(c, xp, pitch, plane, splits, part); break;

@@ -26,10 +26,12 @@ HALF_ULP = {"f32": 0.0, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
 SCORE = [(1, 515, 768), (7, 300, 130), (16, 100, 200), (3, 1000, 33),               # few rows
          (16, 515, 2049), (32, 1030, 641), (17, 20011, 130), (64, 515, 1030), (40, 20011, 130),
          (100, 700, 513), (128, 20011, 384), (129, 257, 33), (200, 515, 2049),
-         (385, 2049, 1030), (257, 4099, 641), (257, 8193, 300), (513, 8193, 130), (385, 16385, 513)]
+         (385, 2049, 1030), (257, 4099, 641), (257, 8193, 300), (513, 8193, 130), (385, 16385, 513),
+         (139, 13001, 1030), (2947, 105, 4096), (130, 34400, 130)]
 BACKWARD = [(1, 70, 33), (4, 10007, 96), (16, 515, 300), (20, 5001, 100), (32, 129, 257), (50, 20011, 130), (64, 77, 4096),
             (100, 3001, 300), (129, 129, 700), (128, 256, 8192),
-            (257, 5000, 513), (513, 10007, 1025), (2049, 100, 4096), (2049, 600, 4096), (2049, 1000, 4096)]
+            (257, 5000, 513), (513, 10007, 1025), (2049, 100, 4096), (2049, 600, 4096), (2049, 1000, 4096),
+            (154, 34507, 300), (133, 50001, 130)]
 # the forms of 4-bit by 4-bit, of which 256 and 128 run ahead of their use from 5 groups on
 MATMUL = [(4097, 4100, 513, "f32"), (4100, 4090, 640, "bf16"), (4090, 4100, 768, "f16"), (4101, 4097, 1000, "f32"),
           (4096, 4103, 1100, "bf16"), (4097, 4097, 1281, "bf16"), (1030, 2051, 1100, "f32"), (700, 4100, 1300, "f16"),

@@ -5,6 +5,7 @@ import os
 import shutil
 import subprocess
 
+import numpy as np
 import pytest
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -22,7 +23,7 @@ def ask(tmp_path_factory):
                     os.path.join(ROOT, "tests", "mx4_choice_driver.cpp"), "-o", exe], check=True)
 
     def ask(what, sizes):
-        text = "".join(f"{what} " + " ".join(map(str, (*s, 0, 0, 0, 0)[:5])) + "\n" for s in sizes)
+        text = "".join(f"{what} " + " ".join(map(str, (*s, 0, 0, 0, 0, 0)[:6])) + "\n" for s in sizes)
         r = subprocess.run([exe], input=text, capture_output=True, text=True)
         assert r.returncode == 0, r.stderr
         out = [tuple(map(int, line.split())) for line in r.stdout.splitlines()]
@@ -52,6 +53,27 @@ def test_rows_of_the_longest_sums(ask):
         for own in (0, 31):
             for slab, (row,) in zip(slabs, ask("slab_row", [(own, s) for s in slabs])):
                 assert row == own + 32 * slab
+
+
+def test_height_of_tiles_by_the_parts_that_are_launched(ask):
+    """Of 128 and 256 rows what takes less time by the model of the header, a round of 256
+    workgroups at a time, with the parts of the sum that the launch really has."""
+    # measured, us with 256 and 128 rows: 38, 27; 37, 26; 30, 22; 32, 22; 31, 27; gradients 36, 29; 32, 27
+    sizes = [(2, 256, 32000, 1024, 0), (2, 256, 20000, 1024, 0), (2, 256, 30000, 768, 0), (2, 500, 16000, 768, 0),
+             (1, 161, 5818, 1024, 0), (1, 670, 734, 2048, 1), (2, 1240, 1895, 384, 1)]
+    assert [t for t, _ in ask("gemm", sizes)] == [128] * len(sizes)
+    rng = np.random.default_rng(0)
+    for back in (0, 1):
+        m, n, d = (np.exp(rng.uniform(np.log(lo), np.log(hi), 500)).astype(int) for lo, hi in ((129, 4000), (64, 200000), (33, 5000)))
+        sizes = [(int(i % 3), int(a), int(b), int(c), back) for i, (a, b, c) in enumerate(zip(m, n, d))]
+        parts = {h: [p for p, in ask("parts", [(*s, h) for s in sizes])] for h in (128, 256)}
+        for i, (s, (chosen, p)) in enumerate(zip(sizes, ask("gemm", sizes))):
+            cols, length = (s[3], s[2]) if back else (s[2], s[3])
+            time = {}
+            for h, cost in ((128, 5), (256, 8)):
+                groups, tiles = -(-length // 128), -(-cols // 256) * -(-s[1] // h)
+                time[h] = cost * -(-tiles * parts[h][i] // 256) * -(-groups // parts[h][i])
+            assert chosen == (128 if time[128] < time[256] else 256) and p == parts[chosen][i], (s, time)
 
 
 def test_gpu_tests_reach_every_arrangement(ask):
