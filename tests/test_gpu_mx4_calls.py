@@ -167,3 +167,40 @@ def test_workspaces_of_streams_are_their_own(R):
         for (y, g, r), w, d, e in zip(got, want, grads, logs):
             assert torch.equal(y, w) and torch.equal(g, d)
             assert torch.equal(r.lse, e.lse) and torch.equal(r.top_ids, e.top_ids)
+
+
+def test_captured_in_a_graph(R):
+    """A step of scores, log probabilities and both gradients, of one row and of many, captured
+    and replayed on new inputs, with the program's own work between: the bits of the eager calls."""
+    for m, n, dim in ((1, 20001, 256), (40, 5000, 200), (300, 3000, 384)):
+        b, plan = R.rslm_mx4_quantize(torch.randn(n, dim, device="cuda")), R.Plan(dim, 4)
+        x = torch.randn(m, dim, device="cuda")
+        t = torch.arange(m, device="cuda")
+        share = torch.full((m,), -1.0 / m, device="cuda")
+
+        def step():
+            q = R.rslm_mx4_quantize(x, plan)
+            s = R.rslm_mx4_score(x, b)
+            r = R.rslm_logprob(s, t, 7, scale=0.5)
+            d = R.rslm_logprob_backward(s, t, r, share, share)
+            return [q.codes, q.scales, R.rslm_mx4_matmul(q, b), s, r.logprob, r.lse, r.entropy, r.top_logprob, r.top_ids, d,
+                    R.rslm_mx4_score_backward(d, b)]
+
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step()
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs = step()
+        for i in range(4):
+            x.copy_(torch.randn(m, dim, device="cuda") * (i + 1))
+            want = [v.clone() for v in step()]
+            for v in outs:
+                v.zero_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            for v, w in zip(outs, want):
+                assert torch.equal(v, w), (m, i)
