@@ -536,7 +536,8 @@ int rslm_mx4_score_backward(const void *dout, int32_t dtype, int64_t m, int64_t 
  * alternative).
  *   scores: m rows of n, type dtype, stride >= 0; target: m int64 (NULL with
  *   logprob NULL); logprob, entropy, lse: m float32 or NULL; top_*:
- *   m x k, 0 <= k <= 1024.  m <= 8,388,607, 1 <= n < 2^31.  stats: m x 2
+ *   m x k, 0 <= k <= 1024 (beyond k of about 100 long rows are gone through
+ *   twice, and k near 1,024 takes tens of times a read of them).  m <= 8,388,607, 1 <= n < 2^31.  stats: m x 2
  *   float32, the row's largest score and log sum_j e^{z_j - z_max}, which the
  *   gradient takes: z_j - lse to full precision however large the scores are.
  *

@@ -12,19 +12,25 @@
 // thread whose piece of 16 entries reaches the one known so far notes the piece
 // in LDS.  At the end the noted pieces are read again (from the cache) for the
 // entries at or above the last such value, about k, which are ranked.  A row
-// that overflows the notes (one that ascends, say) is gone through once more, a
-// few entries at a time.  Few rows are cut into slices, joined by a second
-// kernel.
-// 4,096 x 32,768 bfloat16: 53 us without alternatives (5.1 TB/s), 73 with k = 10;
-// 97 where the bound came of ranking 64 parts' maxima, lane by lane, and 104 where
-// every entry at or above the first piece's bound went to the candidates at once.
-// 1 x 131,072 float32, k = 5: 7.4 us in 32 slices and 6.5 for the join, both the
-// latency of their barriers and reads.  Backward, 4,096 x 32,768 bfloat16: 112 us,
-// 4.8 TB/s read and written.
+// that overflows the notes is gone through once more, a few entries at a time: one that
+// ascends, say, and most long rows for k of about 200 and more, as the bound is weak
+// where k nears the 256 threads and there is none past them.  Few rows are cut into
+// slices, joined by a second kernel; the slices' candidates, up to 2 k each, share
+// its 2,048 places, so that a row has 51 slices at most at k = 20, 10 at k = 100, 2
+// at k = 1,024.
+// us a call, repeated by itself: 4,096 x 32,768 bfloat16 55 without alternatives (4.9
+// TB/s), 69 with k = 10 (VALU 72 % busy), 87 with 100, 374 with 200, 600 with 256, 4,400
+// with 1,024; one row of 1,000,000 float32 17, 20, 39, 227, 279, 16,200.  Of the
+// arrangements for k = 10 (73 then): 97 where the bound came of ranking 64 parts' maxima,
+// lane by lane, and 104 where every entry at or above the first piece's bound went to
+// the candidates at once.  1 x 131,072 float32, k = 20: 7.1 us in 32 slices and 6.4 for
+// the join, both the latency of their barriers and reads.  Backward, 4,096 x 32,768
+// bfloat16: 106 us behind the forward pass (5.1 TB/s read and written), 127 by itself;
+// VALU 94 % busy, so that neither memory nor the arithmetic has much room.
 //
 // An entry of -infinity (or one that scale makes so) is masked: probability 0,
 // no alternative, gradient 0.  A row of nothing else has lse -infinity and
-// entropy 0.  Bound by memory: one read forward, a read and a write backward.
+// entropy 0.  Floors: one read forward, a read and a write backward.
 #include "mx4_dev.h"
 #include "select_dev.h"
 
