@@ -530,16 +530,17 @@ int rslm_mx4_score_backward(const void *dout, int32_t dtype, int64_t m, int64_t 
  *   entropy  = lse - sum_j p_j z_j,  p_j = e^{z_j - lse}
  *   top_*    = the k largest entries by (score desc, index asc), as log
  *              probabilities and indices, padded with (-inf, -1)
- * An entry whose z is -infinity is masked: probability 0, log probability
- * -infinity, no alternative.  A row of masked entries has lse -infinity and
- * entropy 0; a NaN or +infinity makes lse and entropy NaN (a NaN is no
- * alternative).
+ * An entry whose z is -infinity in float32 is masked: probability 0, log
+ * probability -infinity, no alternative.  A row of masked entries has lse
+ * -infinity and entropy 0; a score of NaN or +infinity makes lse and entropy NaN
+ * (a NaN is no alternative), one whose z alone passes float32 only lse +infinity.
  *   scores: m rows of n, type dtype, stride >= 0; target: m int64 (NULL with
  *   logprob NULL); logprob, entropy, lse: m float32 or NULL; top_*:
  *   m x k, 0 <= k <= 1024 (beyond k of about 100 long rows are gone through
- *   twice, and k near 1,024 takes tens of times a read of them).  m <= 8,388,607, 1 <= n < 2^31.  stats: m x 2
- *   float32, the row's largest score and log sum_j e^{z_j - z_max}, which the
- *   gradient takes: z_j - lse to full precision however large the scores are.
+ *   twice, and k near 1,024 takes tens of times a read of them).
+ *   m <= 8,388,607, 1 <= n < 2^31.  stats: m x 2 float32, the row's largest score
+ *   and log sum_j e^{z_j - z_max}, which the gradient takes: z_j - lse to full
+ *   precision however large the scores are.
  *
  * rslm_logprob_backward: the gradient of the scores from those of logprob and
  * entropy (m float32 each; NULL: zero), given stats and entropy:

@@ -654,8 +654,8 @@ class LogProb:
 def rslm_logprob(scores, target=None, k=0, scale=1.0, stream=None):
     """Log probability of the entry target[i] (int64; outside the row: none) of
     each row of scores, log-sum-exp, entropy, and the k most likely entries.
-    k: up to 1,024, meant for about 100 and less.  scale: above 0, at most 2^127.  The gradient is ``rslm_logprob_backward``'s: autograd
-    does not follow the call."""
+    k: up to 1,024, meant for about 100 and less.  scale: above 0, at most 2^127.
+    The gradient is ``rslm_logprob_backward``'s: autograd does not follow the call."""
     _no_history(scores, "scores")
     code, stride = _need_rows(scores, "scores")
     _need(target, torch.int64, "target")

@@ -106,3 +106,13 @@ def test_gradients_as_large_and_as_small_as_a_float(R, n, size, scale):
     tol = 2.0 ** -24 * 3 * (150 + 8 * (np.log(n) + 4)) * terms + 2.0 ** -126
     assert np.isfinite(g).all()
     assert (np.abs(g - want) <= tol).all(), (g, want, tol)
+
+
+@pytest.mark.parametrize("n", [6, 9000])
+def test_z_past_the_largest_float(R, n):
+    """Finite scores whose z is not: the log-sum-exp alone is infinite, and entries whose z
+    is below float32 are masked."""
+    x = np.full((3, n), -3e38, dtype=np.float32)
+    x[0, :4] = 3e38, 3e38, 1e38, -1e38
+    x[1, 0] = 2e38
+    check(R, x, 2.0, [1, 0, 2], [1.0, -2.0, 1.0], [0.0, 1.0, 1.0])
