@@ -522,6 +522,98 @@ int rslm_mx4_score_backward(const void *dout, int32_t dtype, int64_t m, int64_t 
                             int64_t dx_stride, void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
+ * Microscaled 8-bit rows (MX8): queries or activations as the matrix cores
+ * multiply them with MX4 rows.  As MX4 rows, but with an E4M3 code, a byte, for
+ * every coordinate (bit 7 the sign, 4 bits of exponent with bias 7, 3 of
+ * significand; up to 448, subnormal steps of 2^-9; 0x7f and 0xff NaN):
+ *   codes  : n x 128 steps bytes, 16-byte aligned;  scales: as MX4's.
+ *
+ * rslm_mx8_quantize: as rslm_mx4_quantize, with
+ *   s    = the least at which max|x| <= 448 * 2^(s - 127), at least 0; 255 where
+ *          the 32 hold an infinity or a NaN;
+ *   code = x / 2^(s - 127) to the nearest, ties to the even code: off by at most
+ *          2^-4 of x, or by 2^-10 of 2^(s - 127) where that is more.
+ * rslm_mx8_dequantize: the values, rounded to the type asked for (float32 holds
+ *   them exactly, bfloat16 those of 2^-130 and more; from 2^128 on, which 3.4e38
+ *   is rounded to, both have infinity).
+ * rslm_mx8_score: their products with MX4 rows,
+ *   out[i][j] = sum_d a_i[d] b_j[d],  out: m rows of n, type dtype,
+ *   row i at i * stride elements (stride >= n).  m <= 4,194,240.
+ *   Float32 results have the error of a float32 sum of exact products (values of
+ *   a below 2^-130 apart).  For float16 and bfloat16 results the matrix cores drop,
+ *   of each product of coordinates 8 i .. 8 i + 7, what lies more than 13 places
+ *   below the leading place of the largest of them: less than 2^-13 of the largest
+ *   for each of the others, mostly some 2^-17 of a result in all.
+ * ------------------------------------------------------------------------ */
+int rslm_mx8_quantize(const rslm_plan *plan, const void *x, int32_t dtype, int64_t n, int32_t dim,
+                      int64_t stride, uint8_t *codes, uint8_t *scales, void *stream);
+int rslm_mx8_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t n, int32_t dim, void *out,
+                        int32_t dtype, int64_t stride, void *stream);
+int rslm_mx8_score(const uint8_t *a_codes, const uint8_t *a_scales, int64_t m, const uint8_t *b_codes,
+                   const uint8_t *b_scales, int64_t n, int32_t dim, void *out, int32_t dtype, int64_t stride,
+                   void *stream);
+
+/* ------------------------------------------------------------------------
+ * Root-mean-square norm, behind the residual's addition.  Of each row,
+ *   h    = x + residual, rounded to their type (x without a residual)
+ *   rstd = 1 / sqrt(mean_d h[d]^2 + eps), in float32
+ *   y    = h * rstd * weight  (weight NULL: ones)
+ * and y as it is (type dtype), as MX8 rows (quantised from float32), or both.
+ *   x, residual: n rows of dim, type dtype, strides >= 0; h: written where there
+ *   is a residual; it may be x or residual (the same stride).  y, codes and
+ *   scales: NULL where not asked for.  weight: dim values of type weight_dtype.
+ *   rstd: n float32.  eps > 0, finite.  The mean of squares has to be within
+ *   float32 (|h| up to about 10^19): past it rstd is 0.  A row with a NaN or an
+ *   infinity gives NaN (an infinity: where it stands, and 0 elsewhere).
+ *
+ * rslm_rmsnorm_backward: the gradients from those of y (dy) and of h (dh, that of
+ * the residual's other readers; NULL: zero), given h and rstd; with g = dy *
+ * weight and u = h * rstd,
+ *   dx      = rstd * (g - u * mean_d(g u)) + dh  (x's and the residual's)
+ *   dweight = sum over rows of dy * u  (dim values of type weight_dtype)
+ *   dx or dweight NULL: not computed.  dx may be dy, h or dh (the same stride).
+ *   Gradients go past the rounding to 8 bits as if it were not there.  Sums are
+ *   float32 in a fixed order.  ws (for dweight): 16-byte aligned.
+ * n <= 2^31 - 256, 1 <= dim <= 65,536.
+ * ------------------------------------------------------------------------ */
+int rslm_rmsnorm(const void *x, int32_t dtype, int64_t n, int32_t dim, int64_t x_stride, const void *residual,
+                 int64_t residual_stride, const void *weight, int32_t weight_dtype, float eps, void *h,
+                 int64_t h_stride, void *y, int64_t y_stride, uint8_t *codes, uint8_t *scales, float *rstd,
+                 void *stream);
+size_t rslm_rmsnorm_backward_workspace(int64_t n, int32_t dim);
+int rslm_rmsnorm_backward(const void *dy, int32_t dtype, int64_t n, int32_t dim, int64_t dy_stride, const void *h,
+                          int64_t h_stride, const float *rstd, const void *weight, int32_t weight_dtype,
+                          const void *dh, int64_t dh_stride, void *dx, int64_t dx_stride, void *dweight, void *ws,
+                          size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Rows of a table for given ids (tokens), times a number:
+ *   out[i] = scale * table[ids[i]];  0 where ids[i] is outside [0, rows).
+ *   rslm_embed: a float table, rows of dim at stride >= 0; rslm_mx4_embed: MX4
+ *   rows.  ids: n int32 (id_bytes 4) or int64 (8).  out: n rows of dim, any float
+ *   type, computed in float32 and rounded once; out_stride >= dim.
+ * rslm_embed_backward: the gradient of a float table,
+ *   dtable[v] = scale * sum over i with ids[i] = v of dout[i],
+ *   dtable: rows of dim, type dout's or float32 (else RSLM_ERR_UNSUPPORTED),
+ *   table_stride >= dim.  Every row is written, 0 for an id that does not occur;
+ *   with accumulate != 0 the sums are added to what dtable holds, and rows whose
+ *   ids do not occur are left alone.  Sums are float32, in the order of i cut
+ *   into runs by n, dim and the ids alone: results do not change from call to call.
+ *   dout: stride >= 0.  ws: 16-byte aligned.
+ * n, rows <= 2^31 - 256, 1 <= dim <= 65,536.
+ * ------------------------------------------------------------------------ */
+int rslm_embed(const void *table, int32_t dtype, int64_t rows, int32_t dim, int64_t stride, const void *ids,
+               int32_t id_bytes, int64_t n, float scale, void *out, int32_t out_dtype, int64_t out_stride,
+               void *stream);
+int rslm_mx4_embed(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t dim, const void *ids,
+                   int32_t id_bytes, int64_t n, float scale, void *out, int32_t out_dtype, int64_t out_stride,
+                   void *stream);
+size_t rslm_embed_backward_workspace(int64_t n, int64_t rows, int32_t dim);
+int rslm_embed_backward(const void *dout, int32_t dtype, int64_t n, int32_t dim, int64_t stride, const void *ids,
+                        int32_t id_bytes, int64_t rows, float scale, int32_t accumulate, void *dtable,
+                        int32_t table_dtype, int64_t table_stride, void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
  * Log probabilities over rows of scores.  With z_j = scale * scores[i][j]
  * (scale: the inverse temperature, above 0 and at most 2^127), of each row i:
  *   lse      = log sum_j e^{z_j}
@@ -556,6 +648,40 @@ int rslm_logprob(const void *scores, int32_t dtype, int64_t m, int64_t n, int64_
 int rslm_logprob_backward(const void *scores, int32_t dtype, int64_t m, int64_t n, int64_t stride, float scale,
                           const int64_t *target, const float *stats, const float *entropy, const float *dlogprob,
                           const float *dentropy, void *dscores, int64_t dstride, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Verification of drafted tokens from given random numbers.  Of each of b
+ * sequences, with k drafted tokens x_0 .. (counts[i] of them; NULL: k) and
+ *   p_j = softmax(scale * target[i][j]), 0 <= j <= k, the scores after the first
+ *         j drafted tokens,
+ *   q_j = softmax(draft_scale * draft[i][j]), those that x_j was drawn from
+ *         (draft NULL: the drafted token is certain, q_j(x_j) = 1),
+ * in order, x_j stands while u_j q_j(x_j) < p_j(x_j).  Then one token more is
+ * drawn: past the last draft from p, at a draft j that falls from max(p_j - q_j, 0),
+ * or from p_j where that is zero throughout: of the weights r, the first token t
+ * with r_0 + .. + r_t > u_k sum(r).  So the tokens have the target's distribution.
+ *   target: scores of b x (k + 1) rows of n, type dtype, sequence i at i *
+ *   target_seq_stride and its rows target_stride apart (elements, >= 0);
+ *   draft: b x k rows in the same way; tokens: b x k int64 (one outside [0, n)
+ *   falls); uniforms: b x (k + 1) float32 of [0, 1), u_0 .. u_{k-1} for the
+ *   drafts and u_k for the drawn token (taken into [0, 1 - 2^-24]); counts:
+ *   b int32, taken into 0 .. k; rows past a count are not read.
+ *   out_tokens: b x (k + 1) int64: the drafts that stand, the drawn token, -1.
+ *   accepted: b int32, how many stand.  logprob: b x (k + 1) float32 or NULL: log
+ *   p_j of each token of out_tokens, 0 for -1.
+ * A score of -infinity is masked: it has no probability.  A target's row without
+ * any, or with a NaN or +infinity, lets its draft fall and draws -1; such a draft's
+ * row lets it fall, and p is drawn from.  Sums and weights are float64, an
+ * exponential within 2^-44 of its value.
+ * k <= 64, 1 <= n <= 2^31 - 8,193, b (2 k + 1) <= 8,388,607; scales above 0, at
+ * most 2^127.  k = 0 draws a token from each row.  ws: 16-byte aligned; draft:
+ * whether there are draft scores.
+ * ------------------------------------------------------------------------ */
+size_t rslm_verify_workspace(int64_t b, int32_t k, int64_t n, int32_t draft);
+int rslm_verify(const void *target, int32_t dtype, int64_t b, int32_t k, int64_t n, int64_t target_seq_stride,
+                int64_t target_stride, float scale, const void *draft, int64_t draft_seq_stride, int64_t draft_stride,
+                float draft_scale, const int64_t *tokens, const float *uniforms, const int32_t *counts,
+                int64_t *out_tokens, int32_t *accepted, float *logprob, void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
  * Profiling hook (not part of the method): in later rslm_scan_topk calls

@@ -35,6 +35,10 @@ EXPORTS = [
     "rslm_mx4_quantize", "rslm_mx4_dequantize", "rslm_mx4_matmul", "rslm_mx4_score_workspace", "rslm_mx4_score",
     "rslm_mx4_score_backward_workspace", "rslm_mx4_score_backward",
     "rslm_logprob_workspace", "rslm_logprob", "rslm_logprob_backward",
+    "rslm_mx8_quantize", "rslm_mx8_dequantize", "rslm_mx8_score",
+    "rslm_rmsnorm", "rslm_rmsnorm_backward_workspace", "rslm_rmsnorm_backward",
+    "rslm_embed", "rslm_mx4_embed", "rslm_embed_backward_workspace", "rslm_embed_backward",
+    "rslm_verify_workspace", "rslm_verify",
 ]
 
 
@@ -121,6 +125,19 @@ def _declare(lib):
                                    SZ, P]),
         "rslm_logprob_backward": (C.c_int, [P, I32, I64, I64, I64, C.c_float, P, P, P, P, P, P,
                                             I64, P]),
+        "rslm_mx8_quantize": (C.c_int, [P, P, I32, I64, I32, I64, P, P, P]),
+        "rslm_mx8_dequantize": (C.c_int, [P, P, I64, I32, P, I32, I64, P]),
+        "rslm_mx8_score": (C.c_int, [P, P, I64, P, P, I64, I32, P, I32, I64, P]),
+        "rslm_rmsnorm": (C.c_int, [P, I32, I64, I32, I64, P, I64, P, I32, C.c_float, P, I64, P, I64, P, P, P, P]),
+        "rslm_rmsnorm_backward_workspace": (SZ, [I64, I32]),
+        "rslm_rmsnorm_backward": (C.c_int, [P, I32, I64, I32, I64, P, I64, P, P, I32, P, I64, P, I64, P, P, SZ, P]),
+        "rslm_embed": (C.c_int, [P, I32, I64, I32, I64, P, I32, I64, C.c_float, P, I32, I64, P]),
+        "rslm_mx4_embed": (C.c_int, [P, P, I64, I32, P, I32, I64, C.c_float, P, I32, I64, P]),
+        "rslm_embed_backward_workspace": (SZ, [I64, I64, I32]),
+        "rslm_embed_backward": (C.c_int, [P, I32, I64, I32, I64, P, I32, I64, C.c_float, I32, P, I32, I64, P, SZ, P]),
+        "rslm_verify_workspace": (SZ, [I64, I32, I64, I32]),
+        "rslm_verify": (C.c_int, [P, I32, I64, I32, I64, I64, I64, C.c_float, P, I64, I64, C.c_float, P, P, P, P, P, P, P,
+                                  SZ, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)

@@ -523,10 +523,10 @@ def _same_device(a, b, name):
         raise ValueError(f"{name} must be on {a.device}, got {b.device}")
 
 
-class Mx4Rows:
-    """A matrix of microscaled 4-bit rows: ``codes`` (n x 64 steps uint8) and
-    ``scales`` (n x 4 steps uint8) of ``dim`` coordinates, steps = ceil(dim / 128),
-    zero past dim (``rslm_mx4_quantize`` writes them so)."""
+class _MxRows:
+    """Rows of microscaled codes, ``_bytes`` of them to a group of 128 coordinates."""
+
+    _bytes = 0
 
     def __init__(self, codes, scales, dim):
         _need(codes, torch.uint8, "codes")
@@ -534,8 +534,9 @@ class Mx4Rows:
         if not 1 <= dim <= 65536:
             raise ValueError("dim must be 1..65536")
         steps = (dim + 127) // 128
-        if codes.dim() != 2 or codes.shape[1] != 64 * steps or tuple(scales.shape) != (codes.shape[0], 4 * steps):
-            raise ValueError(f"codes / scales must be n x {64 * steps} and n x {4 * steps}")
+        if (codes.dim() != 2 or codes.shape[1] != self._bytes * steps
+                or tuple(scales.shape) != (codes.shape[0], 4 * steps)):
+            raise ValueError(f"codes / scales must be n x {self._bytes * steps} and n x {4 * steps}")
         _same_device(codes, scales, "scales")
         self.codes, self.scales, self.dim = codes, scales, int(dim)
 
@@ -546,7 +547,7 @@ class Mx4Rows:
         steps = (dim + 127) // 128
         rows = cls.__new__(cls)   # what __init__ checks holds
         make = torch.empty if stream is None else functools.partial(_empty, stream=stream)
-        rows.codes = make((n, 64 * steps), dtype=torch.uint8, device=device)
+        rows.codes = make((n, cls._bytes * steps), dtype=torch.uint8, device=device)
         rows.scales = make((n, 4 * steps), dtype=torch.uint8, device=device)
         rows.dim = int(dim)
         return rows
@@ -560,9 +561,28 @@ class Mx4Rows:
         return self.codes.device
 
 
-def rslm_mx4_quantize(x, plan=None, rows=None, stream=None):
-    """MX4 rows of the rows of x (float32, float16 or bfloat16, any row stride),
-    rotated by the plan first if one is given."""
+class Mx4Rows(_MxRows):
+    """A matrix of microscaled 4-bit rows: ``codes`` (n x 64 steps uint8) and
+    ``scales`` (n x 4 steps uint8) of ``dim`` coordinates, steps = ceil(dim / 128),
+    zero past dim (``rslm_mx4_quantize`` writes them so)."""
+
+    _bytes = 64
+
+
+class Mx8Rows(_MxRows):
+    """A matrix of microscaled 8-bit rows: ``codes`` (n x 128 steps uint8) and
+    ``scales`` (n x 4 steps uint8) of ``dim`` coordinates, steps = ceil(dim / 128),
+    zero past dim (``rslm_mx8_quantize`` and ``rslm_rmsnorm`` write them so)."""
+
+    _bytes = 128
+
+
+def _need_mx(rows, kind, name):
+    if not isinstance(rows, kind):
+        raise TypeError(f"{name} must be {kind.__name__}, got {type(rows).__name__}")
+
+
+def _quantize(fn, kind, x, plan, rows, stream):
     code, stride = _need_rows(x, "x")
     n, dim = x.shape
     device = x.device
@@ -572,28 +592,42 @@ def rslm_mx4_quantize(x, plan=None, rows=None, stream=None):
         if plan.device != device:
             raise ValueError(f"x must be on the plan's device ({plan.device}), got {device}")
     if rows is None:
-        rows = Mx4Rows.empty(n, dim, device, stream)
-    elif rows.n != n or rows.dim != dim:
-        raise ValueError("rows must have the shape of x")
+        rows = kind.empty(n, dim, device, stream)
     else:
+        _need_mx(rows, kind, "rows")
+        if rows.n != n or rows.dim != dim:
+            raise ValueError("rows must have the shape of x")
         _same_device(x, rows, "rows")
-    L.check("rslm_mx4_quantize", L.lib().rslm_mx4_quantize(
+    L.check(fn, getattr(L.lib(), fn)(
         plan.handle if plan is not None else None, x.data_ptr(), code, n, dim, stride, rows.codes.data_ptr(),
         rows.scales.data_ptr(), _launch_stream(stream, device)))
     return rows
 
 
-def rslm_mx4_dequantize(rows, dtype=torch.float32, out=None, stream=None):
-    """The values of MX4 rows."""
+def _dequantize(fn, kind, rows, dtype, out, stream):
+    _need_mx(rows, kind, "rows")
     out, code, stride = _out_rows(out, (rows.n, rows.dim), dtype, rows.device, stream)
-    L.check("rslm_mx4_dequantize", L.lib().rslm_mx4_dequantize(
+    L.check(fn, getattr(L.lib(), fn)(
         rows.codes.data_ptr(), rows.scales.data_ptr(), rows.n, rows.dim, out.data_ptr(), code, stride,
         _launch_stream(stream, out.device)))
     return out
 
 
+def rslm_mx4_quantize(x, plan=None, rows=None, stream=None):
+    """MX4 rows of the rows of x (float32, float16 or bfloat16, any row stride),
+    rotated by the plan first if one is given."""
+    return _quantize("rslm_mx4_quantize", Mx4Rows, x, plan, rows, stream)
+
+
+def rslm_mx4_dequantize(rows, dtype=torch.float32, out=None, stream=None):
+    """The values of MX4 rows."""
+    return _dequantize("rslm_mx4_dequantize", Mx4Rows, rows, dtype, out, stream)
+
+
 def rslm_mx4_matmul(a, b, dtype=torch.float32, out=None, stream=None):
     """a b^T of two sets of MX4 rows (a.n x b.n)."""
+    _need_mx(a, Mx4Rows, "a")
+    _need_mx(b, Mx4Rows, "b")
     if a.dim != b.dim:
         raise ValueError("a and b must have the same dimension")
     _same_device(a, b, "b")
@@ -608,6 +642,7 @@ def rslm_mx4_score(x, b, dtype=torch.float32, out=None, stream=None):
     """x b^T of float rows x and MX4 rows b; dtype: float32 or x's.  The gradient is
     ``rslm_mx4_score_backward``'s: autograd does not follow the call."""
     _no_history(x, "x")
+    _need_mx(b, Mx4Rows, "b")
     code, stride = _need_rows(x, "x")
     if x.shape[1] != b.dim:
         raise ValueError("x must have b's dimension")
@@ -625,6 +660,7 @@ def rslm_mx4_score_backward(dout, b, dtype=None, out=None, stream=None):
     """The gradient of ``rslm_mx4_score`` with respect to x: dout b (dout.shape[0] x
     b.dim); dtype: dout's (default) or float32."""
     _no_history(dout, "dout")
+    _need_mx(b, Mx4Rows, "b")
     code, stride = _need_rows(dout, "dout")
     if dout.shape[1] != b.n:
         raise ValueError("dout must have a column for every row of b")
@@ -635,6 +671,196 @@ def rslm_mx4_score_backward(dout, b, dtype=None, out=None, stream=None):
     ws = _WS.get(nb, dout.device, "mx4_backward", stream) if nb else None
     L.check("rslm_mx4_score_backward", L.lib().rslm_mx4_score_backward(
         dout.data_ptr(), code, m, stride, b.codes.data_ptr(), b.scales.data_ptr(), b.n, b.dim, out.data_ptr(), ocode,
+        ostride, _at(ws), nb, _launch_stream(stream, out.device)))
+    return out
+
+
+# ------------------------------------------------------------------ 8-bit (MX8) rows
+def rslm_mx8_quantize(x, plan=None, rows=None, stream=None):
+    """MX8 rows of the rows of x (float32, float16 or bfloat16, any row stride),
+    rotated by the plan first if one is given."""
+    return _quantize("rslm_mx8_quantize", Mx8Rows, x, plan, rows, stream)
+
+
+def rslm_mx8_dequantize(rows, dtype=torch.float32, out=None, stream=None):
+    """The values of MX8 rows."""
+    return _dequantize("rslm_mx8_dequantize", Mx8Rows, rows, dtype, out, stream)
+
+
+def rslm_mx8_score(a, b, dtype=torch.float32, out=None, stream=None):
+    """a b^T of MX8 rows a and MX4 rows b (a.n x b.n).  For float32 results products
+    are exact; for 16-bit ones the matrix cores drop what lies far below their
+    rounding (``include/rslm.h``), at twice the rate."""
+    _need_mx(a, Mx8Rows, "a")
+    _need_mx(b, Mx4Rows, "b")
+    if a.dim != b.dim:
+        raise ValueError("a and b must have the same dimension")
+    _same_device(a, b, "b")
+    out, code, stride = _out_rows(out, (a.n, b.n), dtype, a.device, stream)
+    L.check("rslm_mx8_score", L.lib().rslm_mx8_score(
+        a.codes.data_ptr(), a.scales.data_ptr(), a.n, b.codes.data_ptr(), b.scales.data_ptr(), b.n, a.dim, out.data_ptr(),
+        code, stride, _launch_stream(stream, out.device)))
+    return out
+
+
+# ------------------------------------------------------------------ norms
+class RmsNorm:
+    """What ``rslm_rmsnorm`` returns: h (x + residual; x itself without one), y (None
+    if not asked for), rows (Mx8Rows or None) and rstd (float32, an entry a row)."""
+
+    def __init__(self, h, y, rows, rstd):
+        self.h, self.y, self.rows, self.rstd = h, y, rows, rstd
+
+
+def _need_weight(weight, dim, like, name="weight"):
+    """The type code of a vector of dim floats."""
+    if weight is None:
+        return L.RSLM_F32
+    code = _float_type(weight.dtype, name)
+    _need(weight, weight.dtype, name)
+    if tuple(weight.shape) != (dim,):
+        raise ValueError(f"{name} must be ({dim},), got {tuple(weight.shape)}")
+    _same_device(like, weight, name)
+    return code
+
+
+def _like_rows(t, like, name):
+    """The row stride of a matrix of the type, shape and device of `like`."""
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
+    stride = _need_rows(t, name, tuple(like.shape))[1]
+    _same_device(like, t, name)
+    return stride
+
+
+def _need_dim(t, name):
+    if not 1 <= t.shape[1] <= 65536:
+        raise ValueError(f"{name} must have 1..65536 columns")
+
+
+def rslm_rmsnorm(x, weight=None, residual=None, eps=1e-6, y=True, rows=False, h=None, stream=None):
+    """h = x + residual and its root-mean-square norm times weight (None: ones), as
+    floats of x's type (y), as MX8 rows (rows), or both.  x and residual: float32,
+    float16 or bfloat16, any row stride; weight: any of these types; h: where to
+    write the sum (may be x or residual).  The gradients are
+    ``rslm_rmsnorm_backward``'s: autograd does not follow the call."""
+    for t, name in ((x, "x"), (weight, "weight"), (residual, "residual")):
+        _no_history(t, name)
+    code, stride = _need_rows(x, "x")
+    _need_dim(x, "x")
+    n, dim = x.shape
+    wcode = _need_weight(weight, dim, x)
+    rstride = hstride = 0
+    if residual is not None:
+        rstride = _like_rows(residual, x, "residual")
+        h, _, hstride = _out_rows(h, (n, dim), x.dtype, x.device, stream, "h")
+    elif h is not None:
+        raise ValueError("h is written with a residual only")
+    r = RmsNorm(h if residual is not None else x, _empty((n, dim), x.dtype, x.device, stream) if y else None,
+                Mx8Rows.empty(n, dim, x.device, stream) if rows else None,
+                _empty((n,), torch.float32, x.device, stream))
+    L.check("rslm_rmsnorm", L.lib().rslm_rmsnorm(
+        x.data_ptr(), code, n, dim, stride, _at(residual), rstride, _at(weight), wcode, eps, _at(h), hstride, _at(r.y), dim,
+        r.rows.codes.data_ptr() if rows else None, r.rows.scales.data_ptr() if rows else None, r.rstd.data_ptr(),
+        _launch_stream(stream, x.device)))
+    return r
+
+
+def rslm_rmsnorm_backward(dy, result, weight=None, dh=None, dweight=True, out=None, stream=None):
+    """(dx, dweight): the gradients of x (and of the residual: they are the same) and of
+    weight (None without one, or if not asked for), from those of y and of h (dh; None:
+    zero); result: what ``rslm_rmsnorm`` returned.  dy, dh and dx have x's type, dweight
+    weight's.  The rounding of MX8 rows counts as if it were not there."""
+    for t, name in ((dy, "dy"), (weight, "weight"), (dh, "dh")):
+        _no_history(t, name)
+    h, rstd = result.h, result.rstd
+    code, stride = _need_rows(dy, "dy")
+    _need_dim(dy, "dy")
+    n, dim = dy.shape
+    hstride = _like_rows(h, dy, "result.h")
+    _need(rstd, torch.float32, "result.rstd")
+    if rstd.shape != (n,):
+        raise ValueError("result.rstd must have an entry for every row of dy")
+    _same_device(dy, rstd, "result.rstd")
+    wcode = _need_weight(weight, dim, dy)
+    dhstride = _like_rows(dh, dy, "dh") if dh is not None else 0
+    out, _, ostride = _out_rows(out, (n, dim), dy.dtype, dy.device, stream)
+    dw = ws = None
+    nb = 0
+    if dweight and weight is not None:
+        dw = _empty((dim,), weight.dtype, dy.device, stream)
+        nb = L.lib().rslm_rmsnorm_backward_workspace(n, dim)
+        ws = _scratch(nb, dy.device, stream)
+    L.check("rslm_rmsnorm_backward", L.lib().rslm_rmsnorm_backward(
+        dy.data_ptr(), code, n, dim, stride, h.data_ptr(), hstride, rstd.data_ptr(), _at(weight), wcode, _at(dh), dhstride,
+        out.data_ptr(), ostride, _at(dw), _at(ws), nb, _launch_stream(stream, dy.device)))
+    return out, dw
+
+
+def _scratch(nbytes, device, stream):
+    """A call's own workspace: a captured call's is its graph's, which no other call
+    or graph writes."""
+    return _empty((nbytes,), torch.uint8, device, stream) if nbytes else None
+
+
+# ------------------------------------------------------------------ tables of rows
+def _need_ids(ids, name="ids"):
+    """Bytes of an id of a vector of int32 or int64."""
+    if ids.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"{name} must be int32 or int64, got {ids.dtype}")
+    _need(ids, ids.dtype, name)
+    if ids.dim() != 1:
+        raise ValueError(f"{name} must be one-dimensional, got {tuple(ids.shape)}")
+    return 4 if ids.dtype == torch.int32 else 8
+
+
+def rslm_embed(table, ids, scale=1.0, dtype=None, out=None, stream=None):
+    """scale * table[ids] (len(ids) x dim): rows of a float table (any row stride) or
+    of Mx4Rows, zero for an id outside the table (-1, say).  ids: int32 or int64.
+    dtype: any float type (None: the table's, float32 for Mx4Rows).  The gradient of
+    a float table is ``rslm_embed_backward``'s: autograd does not follow the call."""
+    id_bytes = _need_ids(ids)
+    n = ids.shape[0]
+    if isinstance(table, _MxRows):
+        _need_mx(table, Mx4Rows, "table")
+        _same_device(table, ids, "ids")
+        out, ocode, ostride = _out_rows(out, (n, table.dim), torch.float32 if dtype is None else dtype, table.device, stream)
+        L.check("rslm_mx4_embed", L.lib().rslm_mx4_embed(
+            table.codes.data_ptr(), table.scales.data_ptr(), table.n, table.dim, ids.data_ptr(), id_bytes, n, scale,
+            out.data_ptr(), ocode, ostride, _launch_stream(stream, out.device)))
+        return out
+    _no_history(table, "table")
+    code, stride = _need_rows(table, "table")
+    _need_dim(table, "table")
+    _same_device(table, ids, "ids")
+    out, ocode, ostride = _out_rows(out, (n, table.shape[1]), table.dtype if dtype is None else dtype, table.device, stream)
+    L.check("rslm_embed", L.lib().rslm_embed(
+        table.data_ptr(), code, table.shape[0], table.shape[1], stride, ids.data_ptr(), id_bytes, n, scale, out.data_ptr(),
+        ocode, ostride, _launch_stream(stream, out.device)))
+    return out
+
+
+def rslm_embed_backward(dout, ids, rows, scale=1.0, dtype=None, out=None, accumulate=False, stream=None):
+    """The gradient of a float table of `rows` rows from that of ``rslm_embed``'s
+    result: of each row scale times the sum of its ids' rows of dout, zero for ids
+    that do not occur; with accumulate added to out, in which rows of ids that do not
+    occur are left alone.  dtype: dout's (default) or float32.  Ids outside the table
+    have no gradient.  Results do not change from call to call."""
+    _no_history(dout, "dout")
+    code, stride = _need_rows(dout, "dout")
+    _need_dim(dout, "dout")
+    id_bytes = _need_ids(ids)
+    n, dim = dout.shape
+    if ids.shape[0] != n:
+        raise ValueError("ids must have an entry for every row of dout")
+    _same_device(dout, ids, "ids")
+    if accumulate and out is None:
+        raise ValueError("accumulate needs out")
+    out, ocode, ostride = _out_rows(out, (rows, dim), dout.dtype if dtype is None else dtype, dout.device, stream)
+    nb = L.lib().rslm_embed_backward_workspace(n, rows, dim)
+    ws = _scratch(nb, dout.device, stream)
+    L.check("rslm_embed_backward", L.lib().rslm_embed_backward(
+        dout.data_ptr(), code, n, dim, stride, ids.data_ptr(), id_bytes, rows, scale, int(accumulate), out.data_ptr(), ocode,
         ostride, _at(ws), nb, _launch_stream(stream, out.device)))
     return out
 
@@ -705,3 +931,70 @@ def rslm_logprob_backward(scores, target, result, dlogprob=None, dentropy=None, 
         scores.data_ptr(), code, m, n, stride, result.scale, _at(target), result.stats.data_ptr(), result.entropy.data_ptr(),
         _at(dlogprob), _at(dentropy), out.data_ptr(), ostride, _launch_stream(stream, out.device)))
     return out
+
+
+# ------------------------------------------------------------------ drafted tokens
+class Verified:
+    """What ``rslm_verify`` returns: tokens (b x (k + 1) int64: the drafts that stand,
+    the token drawn after them, then -1), accepted (b int32: how many stand) and
+    logprob (b x (k + 1) float32: of each token under the target; 0 for -1)."""
+
+    def __init__(self, tokens, accepted, logprob):
+        self.tokens, self.accepted, self.logprob = tokens, accepted, logprob
+
+
+def _need_scores3(t, shape, like, name):
+    """The type code and the strides of sequences and rows of a b x rows x n tensor."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    code = _float_type(t.dtype, name)
+    if t.dim() != 3 or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name} must be {'three-dimensional' if shape is None else shape}, got {tuple(t.shape)}")
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    if like is not None:
+        if t.dtype != like.dtype:
+            raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
+        _same_device(like, t, name)
+    return code, t.stride(0), t.stride(1)
+
+
+def rslm_verify(target, tokens, uniforms, draft=None, counts=None, scale=1.0, draft_scale=None, stream=None):
+    """Which drafted tokens stand, and the token after them, from given random numbers
+    (``include/rslm.h`` has the rule).  target: scores, b x (k + 1) x n, row j after
+    the first j drafted tokens; tokens: b x k int64; uniforms: b x (k + 1) float32 of
+    [0, 1), one for each draft and one for the drawn token; draft: the scores that the
+    drafts were drawn from, b x k x n of target's type (None: the drafts are
+    certain); counts: b int32, how many drafts each sequence has (None: k).  scale:
+    the inverse temperature; draft_scale: the draft's (None: the same).  k up to 64;
+    k = 0 draws a token from each row of target.  The scores' rows may have any strides."""
+    _no_history(target, "target")
+    _no_history(draft, "draft")
+    code, tseq, trow = _need_scores3(target, None, None, "target")
+    b, k, n = target.shape[0], target.shape[1] - 1, target.shape[2]
+    if k < 0 or k > 64 or n < 1:
+        raise ValueError(f"target must be b x (k + 1) x n with k up to 64 and n at least 1, got {tuple(target.shape)}")
+    _need(tokens, torch.int64, "tokens")
+    _need(uniforms, torch.float32, "uniforms")
+    _need(counts, torch.int32, "counts")
+    for t, shape, name in ((tokens, (b, k), "tokens"), (uniforms, (b, k + 1), "uniforms"), (counts, (b,), "counts")):
+        if t is not None:
+            if tuple(t.shape) != shape:
+                raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
+            _same_device(target, t, name)
+    dseq = drow = 0
+    if draft is not None:
+        _, dseq, drow = _need_scores3(draft, (b, k, n), target, "draft")
+    r = Verified(_empty((b, k + 1), torch.int64, target.device, stream), _empty((b,), torch.int32, target.device, stream),
+                 _empty((b, k + 1), torch.float32, target.device, stream))
+    if b == 0:
+        return r
+    with_draft = draft is not None and k > 0
+    nb = L.lib().rslm_verify_workspace(b, k, n, with_draft)
+    ws = _scratch(nb, target.device, stream)
+    L.check("rslm_verify", L.lib().rslm_verify(
+        target.data_ptr(), code, b, k, n, tseq, trow, scale, draft.data_ptr() if with_draft else None, dseq, drow,
+        scale if draft_scale is None else draft_scale, tokens.data_ptr(), uniforms.data_ptr(), _at(counts),
+        r.tokens.data_ptr(), r.accepted.data_ptr(), r.logprob.data_ptr(), _at(ws), nb,
+        _launch_stream(stream, target.device)))
+    return r

@@ -1,10 +1,11 @@
-// Quantisation of float rows to MX4 rows (mx4_dev.h), with the rotation of
-// rotate.hip in the same pass where a plan asks for it, and back to floats.
+// Quantisation of float rows to MX4 or MX8 rows (mx4_dev.h; the kernels' B is the
+// bits of a code), with the rotation of rotate.hip in the same pass where a plan asks
+// for it, and back to floats.
 //
 // Both directions are bound by memory: a row of D float32 is read (4 D bytes)
-// and 0.53 D bytes are written, or the reverse.  16 lanes take 128
+// and 0.53 D bytes (MX8: 1.03 D) are written, or the reverse.  16 lanes take 128
 // coordinates, 8 consecutive ones each: one 16- or 32-byte load, one 4-byte
-// word of codes, and the 32 coordinates of a scale are those of four adjacent
+// word of codes (8-byte for MX8), and the 32 coordinates of a scale are those of four adjacent
 // lanes, whose largest magnitude is found by two exchanges inside the quad.
 #include "mx4_dev.h"
 #include "rows_dev.h"
@@ -19,7 +20,8 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
 
 // One group of 128 coordinates: lane r of 16 holds coordinates 8 r + i and
 // writes their codes; the first lane of each quad writes its scale.
-__device__ __forceinline__ void mx4_put8(const float (&x)[8], uint8_t *codes, uint8_t *scales, int r) {
+template <int B>
+__device__ __forceinline__ void mx_put8(const float (&x)[8], uint8_t *codes, uint8_t *scales, int r) {
   uint32_t top = 0u;
   float v[8];
 #pragma unroll
@@ -27,8 +29,10 @@ __device__ __forceinline__ void mx4_put8(const float (&x)[8], uint8_t *codes, ui
     v[i] = x[i] + 0.f;   // -0 to +0: the sign of a cancelled sum depends on its order
     top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
   }
-  const uint32_t s = e8m0_code(quad_max(top));
-  *reinterpret_cast<uint32_t *>(codes + 4 * r) = mx4_codes8(v, s);
+  top = quad_max(top);
+  const uint32_t s = B == 4 ? e8m0_code(top) : e8m0_code8(top);
+  if constexpr (B == 4) *reinterpret_cast<uint32_t *>(codes + 4 * r) = mx4_codes8(v, s);
+  else *reinterpret_cast<uint2 *>(codes + 8 * r) = mx8_codes8(v, s);
   if ((r & 3) == 0) scales[r >> 2] = uint8_t(s);
 }
 
@@ -37,8 +41,8 @@ __device__ __forceinline__ void mx4_put8(const float (&x)[8], uint8_t *codes, ui
 // are read on end: 40,001 x 2,049 bfloat16 in 77 us, and in 107 with one group
 // to 16 lanes in the order of the columns (back to floats 37 and 52).
 constexpr int kFlight = 4;
-template <int T>
-__global__ void __launch_bounds__(256) k_mx4_quantize(const void *__restrict__ x, int64_t n, int dim,
+template <int B, int T>
+__global__ void __launch_bounds__(256) k_mx_quantize(const void *__restrict__ x, int64_t n, int dim,
                                                       int64_t stride, int steps, int each,
                                                       uint8_t *__restrict__ codes,
                                                       uint8_t *__restrict__ scales) {
@@ -56,14 +60,14 @@ __global__ void __launch_bounds__(256) k_mx4_quantize(const void *__restrict__ x
         if (t + u < t1) {
           float v[8];
           raw_values<T>(v, raw[u]);
-          mx4_put8(v, codes + (row * steps + t + u) * 64, scales + (row * steps + t + u) * 4, r);
+          mx_put8<B>(v, codes + (row * steps + t + u) * (16 * B), scales + (row * steps + t + u) * 4, r);
         }
     }
   }
 }
 
-template <int T>
-__global__ void __launch_bounds__(256) k_mx4_dequantize(const uint8_t *__restrict__ codes,
+template <int B, int T>
+__global__ void __launch_bounds__(256) k_mx_dequantize(const uint8_t *__restrict__ codes,
                                                         const uint8_t *__restrict__ scales, int64_t n,
                                                         int dim, int steps, int each, void *__restrict__ out,
                                                         int64_t stride) {
@@ -82,7 +86,8 @@ __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint8_t *__restric
           const int64_t g = row * steps + min(t + u, t1 - 1);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            w[u][h] = *reinterpret_cast<const uint16_t *>(codes + g * 64 + 32 * h + 2 * r);
+            const uint8_t *at = codes + g * (16 * B) + (8 * h * B + r * (B / 2));
+            w[u][h] = B == 4 ? *reinterpret_cast<const uint16_t *>(at) : *reinterpret_cast<const uint32_t *>(at);
             s[u][h] = scales[g * 4 + 2 * h + (r >> 3)];
           }
         }
@@ -90,19 +95,24 @@ __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint8_t *__restric
         for (int u = 0; u < kFlight; ++u)
 #pragma unroll
           for (int h = 0; h < 2; ++h)
-            store_float4<T>(orow, 128 * (t + u) + 64 * h + 4 * r, t + u < t1 ? dim : 0, mx4_values4(w[u][h], s[u][h]));
+            store_float4<T>(orow, 128 * (t + u) + 64 * h + 4 * r, t + u < t1 ? dim : 0,
+                            B == 4 ? mx4_values4(w[u][h], s[u][h]) : mx8_values4(w[u][h], s[u][h]));
       } else {
-        uint32_t w[kFlight], s[kFlight];
+        uint2 w[kFlight];
+        uint32_t s[kFlight];
 #pragma unroll
         for (int u = 0; u < kFlight; ++u) {
           const int64_t g = row * steps + min(t + u, t1 - 1);
-          w[u] = *reinterpret_cast<const uint32_t *>(codes + g * 64 + 4 * r);
+          const uint8_t *at = codes + g * (16 * B) + B * r;
+          if constexpr (B == 4) w[u].x = *reinterpret_cast<const uint32_t *>(at);
+          else w[u] = *reinterpret_cast<const uint2 *>(at);
           s[u] = scales[g * 4 + (r >> 2)];
         }
 #pragma unroll
         for (int u = 0; u < kFlight; ++u) {
           float v[8];
-          mx4_values8(v, w[u], s[u]);
+          if constexpr (B == 4) mx4_values8(v, w[u].x, s[u]);
+          else mx8_values8(v, w[u], s[u]);
           store_float8<T>(v, orow, 128 * (t + u) + 8 * r, t + u < t1 ? dim : 0);
         }
       }
@@ -120,8 +130,8 @@ __device__ __forceinline__ void load_float8_any(float (&v)[8], const void *row, 
 // rows (rows_dev.h), whose lanes end with 8 consecutive coordinates of each of
 // their blocks, as the quantiser takes them.  Every pass is scaled as it ends,
 // so the coordinates, and with them the codes, have the bits of rslm_fwht's.
-template <int RPV, int NBR, bool FULL>
-__global__ void __launch_bounds__(256, NBR <= 4 ? 4 : 2) k_mx4_quantize_rot(
+template <int B, int RPV, int NBR, bool FULL>
+__global__ void __launch_bounds__(256, NBR <= 4 ? 4 : 2) k_mx_quantize_rot(
     const void *__restrict__ x, int dtype, int64_t n, int64_t stride, uint8_t *__restrict__ codes,
     uint8_t *__restrict__ scales, RotParams rp) {
   constexpr int VPW = 4 / RPV;
@@ -174,7 +184,7 @@ __global__ void __launch_bounds__(256, NBR <= 4 ? 4 : 2) k_mx4_quantize_rot(
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = z[8 * j + i];
-        mx4_put8(v, codes + (row * steps + b) * 64, scales + (row * steps + b) * 4, ln.r);
+        mx_put8<B>(v, codes + (row * steps + b) * (16 * B), scales + (row * steps + b) * 4, ln.r);
       }
     }
   }
@@ -223,7 +233,8 @@ __device__ __forceinline__ void small_butterflies(float (&v)[8], int r, int B, f
 // divide it, which goes through LDS, as does the permutation between the passes.
 // 284,367 x 64 float32: 38 us (2.2 TB/s), 65 at dim 100; 83 with the butterflies in
 // LDS too.
-__global__ void __launch_bounds__(256) k_mx4_quantize_rot_small(const void *__restrict__ x, int dtype,
+template <int BITS>
+__global__ void __launch_bounds__(256) k_mx_quantize_rot_small(const void *__restrict__ x, int dtype,
                                                                 int64_t n, int64_t stride,
                                                                 uint8_t *__restrict__ codes,
                                                                 uint8_t *__restrict__ scales,
@@ -277,7 +288,7 @@ __global__ void __launch_bounds__(256) k_mx4_quantize_rot_small(const void *__re
         wave_sync_r();
       }
     }
-    if (live) mx4_put8(v, codes + row * 64, scales + row * 4, r);
+    if (live) mx_put8<BITS>(v, codes + row * (16 * BITS), scales + row * 4, r);
   }
 }
 
@@ -310,43 +321,39 @@ struct QuantizeCall {
   hipStream_t s;
 };
 
-template <int RPV, int NBR, bool FULL>
+template <int B, int RPV, int NBR, bool FULL>
 static void launch_quantize_rot_one(const rslm_plan *p, const QuantizeCall &c) {
   const size_t shm = size_t(16 / RPV) * rows_stride(p->rot.D) * 4 + 128 * RPV * NBR * 2;
-  constexpr auto kernel = k_mx4_quantize_rot<RPV, NBR, FULL>;
+  constexpr auto kernel = k_mx_quantize_rot<B, RPV, NBR, FULL>;
   const int64_t groups = (c.n + 16 / RPV - 1) / (16 / RPV);
   hipLaunchKernelGGL(kernel, dim3(rows_grid<kernel>(shm, groups)), dim3(256), shm, c.s, c.x, c.dtype,
                      c.n, c.stride, c.codes, c.scales, p->rot);
 }
 
+template <int B>
 static void launch_quantize_rot(const rslm_plan *p, const QuantizeCall &c) {
   const int D = p->rot.D;
   if (!rows_ok(p->rot)) {
     const unsigned groups = row_groups(c.n);
-    hipLaunchKernelGGL(k_mx4_quantize_rot_small, dim3(groups < 4096 ? groups : 4096), dim3(256), 0, c.s, c.x,
+    hipLaunchKernelGGL(k_mx_quantize_rot_small<B>, dim3(groups < 4096 ? groups : 4096), dim3(256), 0, c.s, c.x,
                        c.dtype, c.n, c.stride, c.codes, c.scales, p->rot);
     return;
   }
 #define RSLM_QUANT_ROWS(RPV, NBR)                                              \
   {                                                                            \
     if (rows_only_full(RPV, NBR) || D == 128 * RPV * NBR)                      \
-      launch_quantize_rot_one<RPV, NBR, true>(p, c);                           \
+      launch_quantize_rot_one<B, RPV, NBR, true>(p, c);                           \
     else                                                                       \
-      launch_quantize_rot_one<RPV, NBR, rows_only_full(RPV, NBR)>(p, c);       \
+      launch_quantize_rot_one<B, RPV, NBR, rows_only_full(RPV, NBR)>(p, c);       \
   }
   const int nbt = rows_blocks(p->rot);
   RSLM_ROWS_SWITCH(nbt, D == 384, RSLM_QUANT_ROWS)
 #undef RSLM_QUANT_ROWS
 }
 
-}  // namespace rslm
-
-using namespace rslm;
-
-extern "C" {
-
-int rslm_mx4_quantize(const rslm_plan *plan, const void *x, int32_t dtype, int64_t n, int32_t dim,
-                      int64_t stride, uint8_t *codes, uint8_t *scales, void *stream) {
+template <int B>
+static int quantize_rows(const rslm_plan *plan, const void *x, int dtype, int64_t n, int dim, int64_t stride,
+                         uint8_t *codes, uint8_t *scales, void *stream) {
   if (n < 0 || n > kMx4MaxRows || dim < 1 || dim > kMx4MaxDim || !float_type_ok(dtype) || stride < 0)
     return RSLM_ERR_INVALID_ARG;
   if (plan && plan->rot.D != dim) return RSLM_ERR_INVALID_ARG;
@@ -356,20 +363,21 @@ int rslm_mx4_quantize(const rslm_plan *plan, const void *x, int32_t dtype, int64
     return RSLM_ERR_INVALID_ARG;
   const hipStream_t s = as_stream(stream);
   if (plan && plan->rot.passes > 0) {
-    launch_quantize_rot(plan, QuantizeCall{x, dtype, n, stride, codes, scales, s});
+    launch_quantize_rot<B>(plan, QuantizeCall{x, dtype, n, stride, codes, scales, s});
     return check_launch();
   }
   const int steps = mx4_steps(dim), each = groups_each(n, steps);
   const dim3 grid(row_groups(n), unsigned((steps + each - 1) / each));
-#define RSLM_QUANT(T) \
-  hipLaunchKernelGGL(k_mx4_quantize<T>, grid, dim3(256), 0, s, x, n, dim, stride, steps, each, codes, scales)
+#define RSLM_QUANT(T)                                                                                             \
+  hipLaunchKernelGGL((k_mx_quantize<B, T>), grid, dim3(256), 0, s, x, n, dim, stride, steps, each, codes, scales)
   RSLM_MX4_TYPES(dtype, RSLM_QUANT)
 #undef RSLM_QUANT
   return check_launch();
 }
 
-int rslm_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t n, int32_t dim, void *out,
-                        int32_t dtype, int64_t stride, void *stream) {
+template <int B>
+static int dequantize_rows(const uint8_t *codes, const uint8_t *scales, int64_t n, int dim, void *out, int dtype,
+                           int64_t stride, void *stream) {
   if (n < 0 || n > kMx4MaxRows || dim < 1 || dim > kMx4MaxDim || !float_type_ok(dtype) ||
       (n > 1 && stride < dim))
     return RSLM_ERR_INVALID_ARG;
@@ -380,11 +388,37 @@ int rslm_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t n, 
   const hipStream_t s = as_stream(stream);
   const int steps = mx4_steps(dim), each = groups_each(n, steps);
   const dim3 grid(row_groups(n), unsigned((steps + each - 1) / each));
-#define RSLM_DEQUANT(T) \
-  hipLaunchKernelGGL(k_mx4_dequantize<T>, grid, dim3(256), 0, s, codes, scales, n, dim, steps, each, out, stride)
+#define RSLM_DEQUANT(T)                                                                                            \
+  hipLaunchKernelGGL((k_mx_dequantize<B, T>), grid, dim3(256), 0, s, codes, scales, n, dim, steps, each, out, stride)
   RSLM_MX4_TYPES(dtype, RSLM_DEQUANT)
 #undef RSLM_DEQUANT
   return check_launch();
+}
+
+}  // namespace rslm
+
+using namespace rslm;
+
+extern "C" {
+
+int rslm_mx4_quantize(const rslm_plan *plan, const void *x, int32_t dtype, int64_t n, int32_t dim,
+                      int64_t stride, uint8_t *codes, uint8_t *scales, void *stream) {
+  return quantize_rows<4>(plan, x, dtype, n, dim, stride, codes, scales, stream);
+}
+
+int rslm_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t n, int32_t dim, void *out,
+                        int32_t dtype, int64_t stride, void *stream) {
+  return dequantize_rows<4>(codes, scales, n, dim, out, dtype, stride, stream);
+}
+
+int rslm_mx8_quantize(const rslm_plan *plan, const void *x, int32_t dtype, int64_t n, int32_t dim,
+                      int64_t stride, uint8_t *codes, uint8_t *scales, void *stream) {
+  return quantize_rows<8>(plan, x, dtype, n, dim, stride, codes, scales, stream);
+}
+
+int rslm_mx8_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t n, int32_t dim, void *out,
+                        int32_t dtype, int64_t stride, void *stream) {
+  return dequantize_rows<8>(codes, scales, n, dim, out, dtype, stride, stream);
 }
 
 }  // extern "C"

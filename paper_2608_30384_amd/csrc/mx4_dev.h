@@ -3,7 +3,8 @@
 // 2^(s - 127) for every 32 coordinates (s = 255: NaN).  A row of D coordinates
 // takes steps = ceil(D / 128) groups of 64 bytes of codes and 4 scales, zero
 // past D, so that every group of 128 coordinates is one operand of the scaled
-// matrix instruction and starts on a 64-byte boundary.
+// matrix instruction and starts on a 64-byte boundary.  And of the 8-bit (MX8)
+// rows: E4M3 codes, a byte each, 128 bytes to a group, with the same scales.
 #pragma once
 
 #include "rslm_internal.h"
@@ -206,6 +207,48 @@ __device__ __forceinline__ uint4 mx4_bf16x8(uint32_t w, float a) {
                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, a, 1)),
                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, a, 2)),
                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, a, 3)));
+}
+
+// E8M0 code of a block of E4M3 codes, of the largest magnitude's bits: the least
+// scale that keeps it within their 448 = 1.75 2^8, so that no code saturates and
+// every rounding is by half a unit (2^-4 of a value) at most.
+__device__ __forceinline__ uint32_t e8m0_code8(uint32_t top) {
+  const uint32_t e = (top >> 23) + ((top & 0x7fffffu) > 0x600000u);
+  return top >= 0x7f800000u ? 255u : e > 8u ? e - 8u : 0u;
+}
+
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+
+// E4M3 codes of 8 coordinates at the scale s, to nearest, ties to the even code.
+__device__ __forceinline__ uint2 mx8_codes8(const float (&v)[8], uint32_t s) {
+  const float a = e8m0_arg(s);
+  i16x2 lo = {0, 0}, hi = {0, 0};
+  lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, v[0], v[1], a, false);
+  lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, v[2], v[3], a, true);
+  hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, v[4], v[5], a, false);
+  hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(hi, v[6], v[7], a, true);
+  return s == 255u ? make_uint2(0u, 0u)
+                   : make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+}
+// Values of the 4 codes of w at the scale s.
+__device__ __forceinline__ f32x4 mx8_values4(uint32_t w, uint32_t s) {
+  const float a = e8m0_arg(s);
+  const f32x2 p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(int(w), a, false);
+  const f32x2 p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(int(w), a, true);
+  return f32x4{p0.x, p0.y, p1.x, p1.y};
+}
+__device__ __forceinline__ void mx8_values8(float (&v)[8], uint2 w, uint32_t s) {
+  const f32x4 a = mx8_values4(w.x, s), b = mx8_values4(w.y, s);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+}
+// 8 codes' values in bfloat16, which holds every one of 2^-130 and more exactly.
+__device__ __forceinline__ uint4 mx8_bf16x8(uint2 w, float a) {
+  return make_uint4(
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(int(w.x), a, false)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(int(w.x), a, true)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(int(w.y), a, false)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(int(w.y), a, true)));
 }
 
 // ---- loads from memory to LDS, which go past the registers

@@ -1,0 +1,289 @@
+// The residual's addition and the root-mean-square norm, to floats and to MX8 rows
+// (mx4_dev.h), and its gradient:
+//   h = round(x + residual),  rstd = (mean h^2 + eps)^(-1/2),  y = (h rstd) w;
+//   dx = dh + rstd (g - n mean(g n)),  g = dy w,  n = h rstd;  dw = sum over rows of dy n.
+// Sums are float32; h is rounded to its type first, as the next layer reads it.
+//
+// Bound by memory: x and the residual are read, h and y (or 1.03 bytes a coordinate of
+// codes and scales) are written, once each; backward h, dy and dh are read and dx written.
+#include "mx4_dev.h"
+#include "rows_dev.h"
+
+namespace rslm {
+
+constexpr int kNormThreads = 256;
+
+struct NormArgs {
+  const void *x, *residual, *weight;
+  int wtype;
+  int64_t n;
+  int dim;
+  int64_t xstride, rstride, hstride, ystride;
+  float eps;
+  void *h, *y;
+  uint8_t *codes, *scales;
+  float *rstd;
+};
+
+template <int T>
+__device__ __forceinline__ const typename FloatType<T>::type *row_of(const void *p, int64_t row, int64_t stride) {
+  return static_cast<const typename FloatType<T>::type *>(p) + row * stride;
+}
+template <int T>
+__device__ __forceinline__ typename FloatType<T>::type *row_of(void *p, int64_t row, int64_t stride) {
+  return static_cast<typename FloatType<T>::type *>(p) + row * stride;
+}
+
+// w[c .. c + 7] of a weight of any type; ones without a weight.
+__device__ __forceinline__ void load_weight8(float (&w)[8], const void *p, int type, int c, int dim) {
+  if (!p) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = 1.f;
+  } else if (type == RSLM_F32) {
+    load_float8<RSLM_F32>(w, p, c, dim);
+  } else if (type == RSLM_F16) {
+    load_float8<RSLM_F16>(w, p, c, dim);
+  } else {
+    load_float8<RSLM_BF16>(w, p, c, dim);
+  }
+}
+
+// The sum of the workgroup's v, in every thread; `sums` has a place for each
+// wavefront, and is free again after the caller's next barrier.
+__device__ __forceinline__ float group_sum(float v, float *sums) {
+  v = wave_sum(v);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float s = sums[0];
+#pragma unroll
+  for (int i = 1; i < kNormThreads / 64; ++i) s += sums[i];
+  return s;
+}
+
+__device__ __forceinline__ uint32_t quad_top(uint32_t v) {
+  v = max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), kDppQuadXor1, 0xf, 0xf, true)));
+  return max(v, uint32_t(__builtin_amdgcn_mov_dpp(int(v), 0x4E, 0xf, 0xf, true)));   // quad_perm [2, 3, 0, 1]
+}
+
+// Codes of 8 coordinates, four adjacent lanes having the 32 of a scale.
+__device__ __forceinline__ void put_mx8(const float (&v)[8], uint8_t *codes, uint8_t *scales, int chunk) {
+  uint32_t top = 0u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+  const uint32_t s = e8m0_code8(quad_top(top));
+  *reinterpret_cast<uint2 *>(codes + 8 * chunk) = mx8_codes8(v, s);
+  if ((chunk & 3) == 0) scales[chunk >> 2] = uint8_t(s);
+}
+
+// A row of any length to a workgroup, which reads it twice (h, written in between,
+// the second time; from the cache).
+template <int T>
+__global__ void __launch_bounds__(kNormThreads) k_norm_long(NormArgs a) {
+  __shared__ float sums[2][kNormThreads / 64];
+  const int tid = threadIdx.x, chunks = mx4_steps(a.dim) * 16;
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x, turn ^= 1) {
+    const auto *x = row_of<T>(a.x, row, a.xstride);
+    float sum = 0.f;
+    for (int c = 8 * tid; c < a.dim; c += 8 * kNormThreads) {
+      float v[8];
+      load_float8<T>(v, x, c, a.dim);
+      if (a.residual) {
+        float r[8];
+        load_float8<T>(r, row_of<T>(a.residual, row, a.rstride), c, a.dim);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = float(typename FloatType<T>::type(v[i] + r[i]));
+        store_float8<T>(v, row_of<T>(a.h, row, a.hstride), c, a.dim);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = fmaf(v[i], v[i], sum);
+    }
+    const float rstd = 1.f / sqrtf(group_sum(sum, sums[turn]) / float(a.dim) + a.eps);
+    if (tid == 0) a.rstd[row] = rstd;
+    if (!a.y && !a.codes) continue;
+    // a thread reads back what it wrote itself
+    const auto *h = a.residual ? row_of<T>(static_cast<const void *>(a.h), row, a.hstride) : x;
+    for (int k = tid; k < chunks; k += kNormThreads) {
+      float v[8], w[8];
+      load_float8<T>(v, h, 8 * k, a.dim);
+      load_weight8(w, a.weight, a.wtype, 8 * k, a.dim);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = v[i] * rstd * w[i] + 0.f;
+      if (a.y) store_float8<T>(v, row_of<T>(a.y, row, a.ystride), 8 * k, a.dim);
+      if (a.codes) put_mx8(v, a.codes + row * chunks * 8, a.scales + row * (chunks / 4), k);
+    }
+  }
+}
+
+struct NormBackArgs {
+  const void *dy, *h, *weight, *dh;
+  int wtype;
+  int64_t n;
+  int dim;
+  int64_t dystride, hstride, dhstride, dxstride;
+  const float *rstd;
+  void *dx;
+  float *partial;   // strips x dim
+  int64_t per;      // rows of a strip
+};
+
+template <int T>
+__global__ void __launch_bounds__(kNormThreads) k_norm_backward_long(NormBackArgs a) {
+  __shared__ float sums[2][kNormThreads / 64];
+  const int tid = threadIdx.x;
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x, turn ^= 1) {
+    const auto *dy = row_of<T>(a.dy, row, a.dystride), *h = row_of<T>(a.h, row, a.hstride);
+    const float rstd = a.rstd[row];
+    float sum = 0.f;
+    for (int c = 8 * tid; c < a.dim; c += 8 * kNormThreads) {
+      float d[8], v[8], w[8];
+      load_float8<T>(d, dy, c, a.dim);
+      load_float8<T>(v, h, c, a.dim);
+      load_weight8(w, a.weight, a.wtype, c, a.dim);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = fmaf(d[i] * w[i], v[i] * rstd, sum);
+    }
+    const float mean = group_sum(sum, sums[turn]) / float(a.dim);
+    for (int c = 8 * tid; c < a.dim; c += 8 * kNormThreads) {
+      float d[8], v[8], w[8], e[8];
+      load_float8<T>(d, dy, c, a.dim);
+      load_float8<T>(v, h, c, a.dim);
+      load_weight8(w, a.weight, a.wtype, c, a.dim);
+      if (a.dh) load_float8<T>(e, row_of<T>(a.dh, row, a.dhstride), c, a.dim);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float g = rstd * (d[i] * w[i] - v[i] * rstd * mean);
+        d[i] = a.dh ? g + e[i] : g;
+      }
+      store_float8<T>(d, row_of<T>(a.dx, row, a.dxstride), c, a.dim);
+    }
+  }
+}
+
+// dy n summed over the rows of a strip, 2,048 columns to a workgroup.
+template <int T>
+__global__ void __launch_bounds__(kNormThreads) k_norm_dweight(NormBackArgs a) {
+  const int c = (int(blockIdx.x) * kNormThreads + int(threadIdx.x)) * 8;
+  if (c >= a.dim) return;
+  const int64_t r0 = int64_t(blockIdx.y) * a.per, r1 = min(a.n, r0 + a.per);
+  float acc[8] = {};
+  for (int64_t row = r0; row < r1; ++row) {
+    float d[8], v[8];
+    load_float8<T>(d, row_of<T>(a.dy, row, a.dystride), c, a.dim);
+    load_float8<T>(v, row_of<T>(a.h, row, a.hstride), c, a.dim);
+    const float rstd = a.rstd[row];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = fmaf(d[i], v[i] * rstd, acc[i]);
+  }
+  store_float8<RSLM_F32>(acc, a.partial + int64_t(blockIdx.y) * a.dim, c, a.dim);
+}
+
+// The strips' sums of a column, eight parts of them to eight threads, in a fixed order.
+__global__ void __launch_bounds__(256) k_norm_join(const float *__restrict__ partial, int strips, int dim,
+                                                   void *__restrict__ dweight, int wtype) {
+  __shared__ float sums[8][32];
+  const int col = threadIdx.x & 31, part = threadIdx.x >> 5;
+  const int c = int(blockIdx.x) * 32 + col;
+  float s = 0.f;
+  if (c < dim)
+    for (int i = part; i < strips; i += 8) s += partial[int64_t(i) * dim + c];
+  sums[part][col] = s;
+  __syncthreads();
+  if (part || c >= dim) return;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) s += sums[i][col];
+  if (wtype == RSLM_F32) store_float<RSLM_F32>(dweight, c, s);
+  else if (wtype == RSLM_F16) store_float<RSLM_F16>(dweight, c, s);
+  else store_float<RSLM_BF16>(dweight, c, s);
+}
+
+constexpr int kNormStrips = 512;
+
+static int64_t norm_strips(int64_t n) { return n < kNormStrips ? n : kNormStrips; }
+
+template <int T>
+static void launch_norm(const NormArgs &a, hipStream_t s) {
+  const dim3 grid(unsigned(a.n < 65536 ? a.n : 65536));
+  hipLaunchKernelGGL(k_norm_long<T>, grid, dim3(kNormThreads), 0, s, a);
+}
+
+template <int T>
+static void launch_norm_backward(const NormBackArgs &b, void *dweight, int dwtype, hipStream_t s) {
+  NormBackArgs a = b;
+  const dim3 grid(unsigned(a.n < 65536 ? a.n : 65536));
+  if (a.dx) hipLaunchKernelGGL(k_norm_backward_long<T>, grid, dim3(kNormThreads), 0, s, a);
+  if (!dweight) return;
+  const int64_t strips = norm_strips(a.n);
+  a.per = strips ? (a.n + strips - 1) / strips : 0;
+  if (strips)
+    hipLaunchKernelGGL(k_norm_dweight<T>, dim3(unsigned((a.dim + 2047) / 2048), unsigned(strips)), dim3(kNormThreads),
+                       0, s, a);
+  hipLaunchKernelGGL(k_norm_join, dim3(unsigned((a.dim + 31) / 32)), dim3(256), 0, s, a.partial, int(strips), a.dim,
+                     dweight, dwtype);
+}
+
+static bool norm_sizes_ok(int64_t n, int dim, int dtype) {
+  return n >= 0 && n <= kMx4MaxRows && dim >= 1 && dim <= kMx4MaxDim && float_type_ok(dtype);
+}
+
+}  // namespace rslm
+
+using namespace rslm;
+
+extern "C" {
+
+int rslm_rmsnorm(const void *x, int32_t dtype, int64_t n, int32_t dim, int64_t x_stride, const void *residual,
+                 int64_t residual_stride, const void *weight, int32_t weight_dtype, float eps, void *h,
+                 int64_t h_stride, void *y, int64_t y_stride, uint8_t *codes, uint8_t *scales, float *rstd,
+                 void *stream) {
+  if (!norm_sizes_ok(n, dim, dtype) || x_stride < 0 || residual_stride < 0 || !(eps > 0.f) || !(eps < INFINITY) ||
+      (weight && !float_type_ok(weight_dtype)) || (residual && n > 1 && h_stride < dim) ||
+      (y && n > 1 && y_stride < dim) || !codes != !scales)
+    return RSLM_ERR_INVALID_ARG;
+  if (n == 0) return RSLM_OK;
+  const int e = float_bytes(dtype);
+  if (!x || !rstd || (residual && !h) || !aligned_to(x, e) || !aligned_to(residual, e) || !aligned_to(h, e) ||
+      !aligned_to(y, e) || !aligned_to(weight, weight ? float_bytes(weight_dtype) : 1) || !aligned_to(codes, 16) ||
+      !aligned_to(scales, 4) || !aligned_to(rstd, 4))
+    return RSLM_ERR_INVALID_ARG;
+  const NormArgs a{x,        residual, weight, weight_dtype, n, dim,   x_stride, residual_stride, h_stride,
+                   y_stride, eps,      h,      y,            codes, scales, rstd};
+  const hipStream_t s = as_stream(stream);
+  if (dtype == RSLM_F32) launch_norm<RSLM_F32>(a, s);
+  else if (dtype == RSLM_F16) launch_norm<RSLM_F16>(a, s);
+  else launch_norm<RSLM_BF16>(a, s);
+  return check_launch();
+}
+
+size_t rslm_rmsnorm_backward_workspace(int64_t n, int32_t dim) {
+  if (!norm_sizes_ok(n, dim, RSLM_F32)) return 0;
+  return size_t(norm_strips(n)) * dim * sizeof(float);
+}
+
+int rslm_rmsnorm_backward(const void *dy, int32_t dtype, int64_t n, int32_t dim, int64_t dy_stride, const void *h,
+                          int64_t h_stride, const float *rstd, const void *weight, int32_t weight_dtype,
+                          const void *dh, int64_t dh_stride, void *dx, int64_t dx_stride, void *dweight, void *ws,
+                          size_t ws_bytes, void *stream) {
+  if (!norm_sizes_ok(n, dim, dtype) || dy_stride < 0 || h_stride < 0 || dh_stride < 0 ||
+      ((weight || dweight) && !float_type_ok(weight_dtype)) || (dx && n > 1 && dx_stride < dim))
+    return RSLM_ERR_INVALID_ARG;
+  const int e = float_bytes(dtype), we = weight || dweight ? float_bytes(weight_dtype) : 1;
+  if ((n > 0 && (!dy || !h || !rstd)) || !aligned_to(dy, e) || !aligned_to(h, e) || !aligned_to(dh, e) ||
+      !aligned_to(dx, e) || !aligned_to(rstd, 4) || !aligned_to(weight, we) || !aligned_to(dweight, we))
+    return RSLM_ERR_INVALID_ARG;
+  if (dweight && n > 0) {
+    if (ws_bytes < rslm_rmsnorm_backward_workspace(n, dim)) return RSLM_ERR_WORKSPACE;
+    if (!ws || !aligned_to(ws, 16)) return RSLM_ERR_INVALID_ARG;
+  }
+  if ((n == 0 || !dx) && !dweight) return RSLM_OK;
+  const NormBackArgs a{dy,        h,        weight,    dh,        weight_dtype, n, dim,
+                       dy_stride, h_stride, dh_stride, dx_stride, rstd, n > 0 ? dx : nullptr, static_cast<float *>(ws), 0};
+  const hipStream_t s = as_stream(stream);
+  if (dtype == RSLM_F32) launch_norm_backward<RSLM_F32>(a, dweight, weight_dtype, s);
+  else if (dtype == RSLM_F16) launch_norm_backward<RSLM_F16>(a, dweight, weight_dtype, s);
+  else launch_norm_backward<RSLM_BF16>(a, dweight, weight_dtype, s);
+  return check_launch();
+}
+
+}  // extern "C"
