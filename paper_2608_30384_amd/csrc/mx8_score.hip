@@ -9,6 +9,9 @@
 #include "mx4_choice.h"
 #include "mx4_dev.h"
 
+#include <type_traits>
+#include <utility>
+
 namespace rslm {
 
 struct Mx8ScoreCall {
@@ -107,6 +110,193 @@ __global__ void __launch_bounds__(256) k_mx8_score(const uint8_t *__restrict__ a
   }
 }
 
+// ---- large products: tiles in LDS ------------------------------------------
+//
+// A workgroup of 4 wavefronts takes 32 MF rows of a by 256 of b, each wavefront 16 MF by
+// 128, one group of 128 coordinates after another.  The memory unit writes codes and
+// scales to LDS by itself, into one of three places for a group: in group t those of t + 2
+// are asked for, and one barrier, behind the last read of group t's place, waits for those
+// of t + 1 alone, a group and a half old.  The rows of b of the next group, and the first
+// two fragments of a's, are then read to registers under the group's last instructions,
+// each fragment of b behind the last one that uses the register; the others of a two
+// fragments ahead.  A read or a load or two fit behind a matrix
+// instruction, which the unit works on for 32 cycles.
+//
+// LDS, by lines of 128 bytes: a row of a, or two of b.  A line's eight 16-byte pieces are
+// exchanged by its number, so that the rows of a read fall on different banks; the
+// exchange is in the address that a lane of the load gives.  Rows of b are dealt to the
+// fragments so that two of them share out 32 rows, eight to a lane, which are 16 bytes of
+// out.
+constexpr int kS8LineA = 128;   // bytes of a row of a
+constexpr int kS8LineB = 64;    // bytes of a row of b
+
+// f(0), .., f(N - 1), each with a constant of its own.
+template <int... I, class F>
+__device__ __forceinline__ void for_each_of(std::integer_sequence<int, I...>, F &&f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void for_each(F &&f) {
+  for_each_of(std::make_integer_sequence<int, N>{}, f);
+}
+
+// 64 lanes x 4 bytes from the buffer to LDS (load_to_lds of 16).
+__device__ __forceinline__ void load_to_lds4(i32x4 buf, uint32_t lds, uint32_t offset) {
+  asm volatile("s_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               :
+               : "{m0}"(lds), "v"(offset), "s"(buf)
+               : "memory");
+}
+
+template <int T, int MF>
+__global__ void __launch_bounds__(256, 1) k_mx8_score_tile(
+    const uint8_t *__restrict__ ac, const uint8_t *__restrict__ as, int64_t m, const uint8_t *__restrict__ bc,
+    const uint8_t *__restrict__ bs, int64_t n, int steps, void *__restrict__ out, int64_t stride, int mtiles) {
+  static_assert(T != RSLM_F32, "16-bit results");
+  static_assert(MF == 8 || MF == 4, "the places of reads and loads between the instructions");
+  constexpr int BM = 32 * MF, BN = kMmN;
+  constexpr int LA = BM / 32, LB = BN / 64, kLoads = LA + LB + 2;   // loads of a wavefront and group
+  constexpr int kA = BM * kS8LineA, kB = BN * kS8LineB, kS = 4 * (BM + BN);
+  constexpr int kB0 = 3 * kA, kS0 = kB0 + 3 * kB, kNone = kS0 + 3 * kS;
+  __shared__ __align__(1024) uint8_t lds[kNone + 256];
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
+  const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // Workgroups go to the 8 XCDs in turn: each XCD takes a run of tiles, in which those of
+  // 8 rows of tiles are neighbours.
+  const int tiles = gridDim.x, per = tiles / 8, rest = tiles % 8;
+  const int xcd = blockIdx.x % 8, at = blockIdx.x / 8 + xcd * per + min(xcd, rest);
+  const int ntiles = tiles / mtiles;
+  const int band = at / (8 * ntiles), rows = min(8, mtiles - 8 * band), in = at - band * 8 * ntiles;
+  const int64_t m0 = int64_t(8 * band + in % rows) * BM, n0 = int64_t(in / rows) * BN;
+  const uint32_t cpa = 128u * steps, cpb = 64u * steps, sp = 4u * steps;
+  const i32x4 ra = buffer_of(ac + m0 * cpa, (m - m0) * cpa), rb = buffer_of(bc + n0 * cpb, (n - n0) * cpb);
+  const i32x4 rsa = buffer_of(as + m0 * sp, (m - m0) * sp), rsb = buffer_of(bs + n0 * sp, (n - n0) * sp);
+  const uint32_t lds0 = lds_address(lds);
+
+  // ---- loads.  A lane of one has line l / 8 of 8 and place l % 8 of it.
+  const int line = lane >> 3, place = lane & 7;
+  const uint32_t va = (wid * (8 * LA) + line) * cpa + ((place ^ line) << 4);
+  // b: line / 2 rows; the exchange, by bit 0 and bits 2 and 3 of the line
+  uint32_t vb[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int slot = place ^ ((line & 1) | ((((line + 8 * j) >> 2) & 3) << 1));
+    vb[j] = (wid * (16 * LB) + 16 * j + 2 * line + (slot >> 2)) * cpb + ((slot & 3) << 4);
+  }
+  const uint32_t vs = (wid * 64 + lane) * sp;
+  // load i of group t, to place p; past the last group from past the end, which gives zeros
+  auto load = [&](int t, int p, int i) {
+    const uint32_t past = t < steps ? 0u : 0x80000000u;
+    if (i < LA)
+      load_to_lds(ra, lds0 + p * kA + (wid * LA + i) * 1024, (va + (8 * i) * cpa + t * kS8LineA) | past);
+    else if (i < LA + LB)
+      load_to_lds(rb, lds0 + kB0 + p * kB + (wid * LB + i - LA) * 1024,
+                  (vb[(i - LA) & 1] + (32 * ((i - LA) >> 1)) * cpb + t * kS8LineB) | past);
+    else if (i == LA + LB)
+      load_to_lds4(rsa, lds0 + (wid * 64 < BM ? kS0 + p * kS + wid * 256 : kNone), (vs + t * 4) | past);
+    else
+      load_to_lds4(rsb, lds0 + kS0 + p * kS + 4 * BM + wid * 256, (vs + t * 4) | past);
+  };
+
+  // ---- reads
+  const int wm = (wid >> 1) * (16 * MF), wn = (wid & 1) * 128;
+  // row of b of lane l's part of fragment j
+  auto b_row = [](int l, int j) { return 32 * (j >> 1) + 8 * (l >> 2) + 4 * (j & 1) + (l & 3); };
+  const int ra_lo = (wm + r) * kS8LineA + ((g ^ (r & 7)) << 4);
+  const int ra_hi = (wm + r) * kS8LineA + (((4 + g) ^ (r & 7)) << 4);
+  const int rb_row = wn + b_row(r, 0);
+  const int rb_off = kB0 + (rb_row >> 1) * 128 + (((4 * (r & 1) + g) ^ (((r >> 1) & 1) | ((r >> 2) << 1))) << 4);
+  const int rsa_off = kS0 + (wm + r) * 4 + g, rsb_off = kS0 + 4 * BM + rb_row * 4 + g;
+  Mx8Frag fa[4];
+  Mx4FragB fb[8];
+  auto read_a = [&](int p, int k, int part) {
+    if (part == 0) fa[k & 3].lo = *reinterpret_cast<const i32x4 *>(&lds[p * kA + ra_lo + 16 * k * kS8LineA]);
+    else if (part == 1) fa[k & 3].hi = *reinterpret_cast<const i32x4 *>(&lds[p * kA + ra_hi + 16 * k * kS8LineA]);
+    else fa[k & 3].s = lds[p * kS + rsa_off + 64 * k];
+  };
+  auto read_b = [&](int p, int j) {
+    fb[j].q = *reinterpret_cast<const i32x4 *>(&lds[p * kB + rb_off + (b_row(0, j) >> 1) * 128]);
+    fb[j].s = lds[p * kS + rsb_off + b_row(0, j) * 4];
+  };
+
+  f32x4 acc[MF][8] = {};
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(p, p, i);
+  arrive<kLoads>();
+#pragma unroll
+  for (int j = 0; j < 8; ++j) read_b(0, j);
+#pragma unroll
+  for (int i = 0; i < 6; ++i) read_a(0, i / 3, i % 3);
+
+  // Group t is in place p, the next one in p1, and p2 is free to be written.
+  int p = 0;
+  for (int t = 0; t < steps; ++t) {
+    const int p1 = p == 2 ? 0 : p + 1, p2 = p1 == 2 ? 0 : p1 + 1;
+    for_each<8 * MF>([&](auto q_) __attribute__((always_inline)) {
+      constexpr int q = decltype(q_)::value, each = MF == 8 ? 3 : 1;
+      constexpr int k = q / 8, j = q % 8;
+      if constexpr (q == 8 * (MF - 2)) arrive<kLoads>();
+      acc[k][j] = mx84_mfma(fb[j], fa[k & 3], acc[k][j]);
+      if constexpr (k < MF - 2 && j % 2 == 1 && j < 7) read_a(p, k + 2, j >> 1);
+      if constexpr (q % each == 0 && q / each < kLoads) load(t + 2, p2, q / each);
+      if constexpr (k == MF - 2 && j < 6) read_a(p1, j / 3, j % 3);
+      if constexpr (k == MF - 1) read_b(p1, j);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    p = p1;
+  }
+
+  // Through LDS, so that a store writes 4 rows of 256 consecutive bytes, a part of LDS
+  // for each wavefront.
+  typedef typename FloatType<T>::type Out;
+  struct __attribute__((packed, aligned(alignof(Out)))) Wide {
+    uint32_t v[4];
+  };
+  constexpr int kOwn = MF == 8 ? 32768 : 16384;
+  static_assert(4 * kOwn <= kNone, "LDS of the stores");
+  arrive<0>();   // the last operands have been read, and the last loads have come, everywhere
+  uint8_t *own = lds + wid * kOwn;
+#pragma unroll
+  for (int k = 0; k < MF; ++k)
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+      const int piece = b_row(4 * g, j) / 8, row = 16 * k + r;
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        w[i] = uint32_t(float_to_h16<T>(acc[k][j + (i >> 1)][2 * (i & 1)])) |
+               uint32_t(float_to_h16<T>(acc[k][j + (i >> 1)][2 * (i & 1) + 1])) << 16;
+      *reinterpret_cast<uint4 *>(own + row * 256 + 16 * (piece ^ r)) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the wavefront's own part
+#pragma unroll 4
+  for (int i = 0; i < 4 * MF; ++i) {
+    const int row = 4 * i + (lane >> 4), piece = lane & 15;
+    const uint4 v = *reinterpret_cast<const uint4 *>(own + row * 256 + 16 * (piece ^ (row & 15)));
+    const int64_t orow = m0 + wm + row, c = n0 + wn + piece * 8;
+    if (orow >= m) continue;
+    Out *o = static_cast<Out *>(out) + orow * stride + c;
+    if (c + 8 <= n) {   // rows may begin anywhere
+      *reinterpret_cast<Wide *>(o) = __builtin_bit_cast(Wide, v);
+    } else {
+      Out e[8];
+      __builtin_memcpy(e, &v, 16);
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (c + q < n) o[q] = e[q];
+    }
+  }
+}
+
+template <int T, int MF>
+static void launch_score8_tile(const Mx8ScoreCall &c) {
+  const int64_t mt = (c.m + 32 * MF - 1) / (32 * MF), nt = (c.n + kMmN - 1) / kMmN;
+  hipLaunchKernelGGL((k_mx8_score_tile<T, MF>), dim3(unsigned(mt * nt)), dim3(256), 0, c.s, c.ac, c.as, c.m, c.bc, c.bs,
+                     c.n, c.steps, c.out, c.stride, int(mt));
+}
+
 template <int T, int F>
 static void launch_score8_direct(const Mx8ScoreCall &c) {
   const Mx4DirectGrid g = matmul_direct_grid(c.m, c.n, 16 * F);
@@ -116,6 +306,11 @@ static void launch_score8_direct(const Mx8ScoreCall &c) {
 
 template <int T>
 static void launch_score8(const Mx8ScoreCall &c) {
+  if constexpr (T != RSLM_F32) {
+    const Mx4MatmulForm form = matmul_form(c.m, c.n);
+    if (form == kMmTile256) return launch_score8_tile<T, 8>(c);
+    if (form == kMmTile128) return launch_score8_tile<T, 4>(c);
+  }
   if (c.m > 32 || matmul_direct_grid(c.m, c.n, 16).x > kMostWorkgroups) launch_score8_direct<T, 4>(c);
   else if (c.m > 16) launch_score8_direct<T, 2>(c);
   else launch_score8_direct<T, 1>(c);
