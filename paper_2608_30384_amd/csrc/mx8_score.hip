@@ -110,6 +110,115 @@ __global__ void __launch_bounds__(256) k_mx8_score(const uint8_t *__restrict__ a
   }
 }
 
+// ---- few rows of a -----------------------------------------------------------
+//
+// Bound by reading b, once.  A wavefront takes 16 rows of b, with two groups of them
+// asked for at once; a's rows are in LDS (HELD) where they fit.  Where there are few rows
+// of b, the wavefronts of a workgroup share out the groups of the same 16 (SPLIT), and
+// their sums are added in a fixed order.
+constexpr int kFew8Flight = 2;
+constexpr int kFew8Lds = 65536;   // bytes of a's codes
+
+template <int T, bool SPLIT, bool HELD>
+__global__ void __launch_bounds__(256) k_mx8_score_few(const uint8_t *__restrict__ ac, const uint8_t *__restrict__ as,
+                                                       int m, const uint8_t *__restrict__ bc,
+                                                       const uint8_t *__restrict__ bs, int64_t n, int steps,
+                                                       void *__restrict__ out, int64_t stride, int64_t tiles) {
+  constexpr bool kExact = T == RSLM_F32;
+  constexpr int U = kFew8Flight, kStep = SPLIT ? 4 : 1;
+  extern __shared__ uint4 few8_lds[];   // codes, 128 bytes of a row after another's, then scales
+  __shared__ f32x4 sums[SPLIT ? 256 : 1];
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
+  const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  uint32_t *held_scales = reinterpret_cast<uint32_t *>(few8_lds + m * steps * 8);
+  const int64_t each = SPLIT ? int64_t(gridDim.x) : int64_t(gridDim.x) * 4;
+  int64_t tile = SPLIT ? int64_t(blockIdx.x) : int64_t(blockIdx.x) * 4 + wid;
+  const int t0 = SPLIT ? wid : 0;
+  // the tile's place, the same for all lanes, and a lane's place in it
+  const uint8_t *pc, *ps;
+  uint32_t own;
+  Mx4FragB b[U];
+  auto fetch = [&](int t) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = min(t + kStep * u, steps - 1);
+      b[u].q = *reinterpret_cast<const i32x4 *>(pc + at * 64 + (own * 64 + 16 * g));
+      b[u].s = (ps + at * 4)[own * 4 + g];
+    }
+  };
+  auto begin = [&] {   // past the last tile: its rows again
+    const int64_t from = min(tile, tiles - 1) * 16;
+    own = uint32_t(min(int64_t(r), n - 1 - from)) * uint32_t(steps);
+    pc = bc + from * steps * 64, ps = bs + from * steps * 4;
+    fetch(t0);
+  };
+  begin();
+  if constexpr (HELD) {
+    for (int i = tid; i < m * steps * 8; i += 256) {
+      // piece i % 8 of line i / 8, exchanged by the row's number
+      const int line = i >> 3, row = line % m, t = line / m;
+      few8_lds[(i & ~7) | ((i ^ row) & 7)] =
+          reinterpret_cast<const uint4 *>(ac)[(int64_t(row) * steps + t) * 8 + (i & 7)];
+    }
+    for (int i = tid; i < m * steps; i += 256)
+      held_scales[i] = reinterpret_cast<const uint32_t *>(as)[int64_t(i % m) * steps + i / m];
+    __syncthreads();
+  }
+  const int row_a = min(r, m - 1);
+  const int first_piece = kExact ? 2 * g : g, second_piece = kExact ? 2 * g + 1 : 4 + g;
+  while (tile < tiles) {
+    const int64_t here = tile;
+    tile += each;
+    f32x4 acc = {};
+    for (int t = t0; t < steps; t += kStep * U) {
+      Mx4FragB now[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) now[u] = b[u];
+      if (t + kStep * U < steps) fetch(t + kStep * U);
+      else begin();   // the next tile's
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int at = t + kStep * u;
+        if (at >= steps) break;
+        Mx8Frag a;
+        if constexpr (HELD) {
+          const i32x4 *line = reinterpret_cast<const i32x4 *>(few8_lds) + (at * m + row_a) * 8;
+          a.lo = line[first_piece ^ (row_a & 7)], a.hi = line[second_piece ^ (row_a & 7)];
+          a.s = reinterpret_cast<const uint8_t *>(held_scales)[(at * m + row_a) * 4 + g];
+        } else {
+          const int64_t from = int64_t(row_a) * steps + at;
+          const i32x4 *line = reinterpret_cast<const i32x4 *>(ac) + from * 8;
+          a.lo = line[first_piece], a.hi = line[second_piece];
+          a.s = as[from * 4 + g];
+        }
+        if constexpr (kExact) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const i32x4 w = q < 2 ? a.lo : a.hi;
+            acc = mx_mfma_bf16(mx4_bf16x8(uint32_t(now[u].q[q]), e8m0_arg(now[u].s)),
+                               mx8_bf16x8(make_uint2(uint32_t(w[2 * (q & 1)]), uint32_t(w[2 * (q & 1) + 1])), e8m0_arg(a.s)),
+                               acc);
+          }
+        } else {
+          acc = mx84_mfma(now[u], a, acc);
+        }
+      }
+    }
+    if constexpr (SPLIT) {
+      sums[tid] = acc;
+      __syncthreads();
+      if (wid == 0) {
+#pragma unroll
+        for (int w = 1; w < 4; ++w) acc += sums[64 * w + lane];
+      }
+      __syncthreads();
+      if (wid) continue;
+    }
+    if (r < m)
+      store_float4<T>(static_cast<typename FloatType<T>::type *>(out) + r * stride, here * 16 + 4 * g, n, acc);
+  }
+}
+
 // ---- large products: tiles in LDS ------------------------------------------
 //
 // A workgroup of 4 wavefronts takes 32 MF rows of a by 256 of b, each wavefront 16 MF by
@@ -149,7 +258,7 @@ __device__ __forceinline__ void load_to_lds4(i32x4 buf, uint32_t lds, uint32_t o
 }
 
 template <int T, int MF>
-__global__ void __launch_bounds__(256, 1) k_mx8_score_tile(
+__global__ void __launch_bounds__(256, MF == 4 ? 2 : 1) k_mx8_score_tile(
     const uint8_t *__restrict__ ac, const uint8_t *__restrict__ as, int64_t m, const uint8_t *__restrict__ bc,
     const uint8_t *__restrict__ bs, int64_t n, int steps, void *__restrict__ out, int64_t stride, int mtiles) {
   static_assert(T != RSLM_F32, "16-bit results");
@@ -157,7 +266,8 @@ __global__ void __launch_bounds__(256, 1) k_mx8_score_tile(
   constexpr int BM = 32 * MF, BN = kMmN;
   constexpr int LA = BM / 32, LB = BN / 64, kLoads = LA + LB + 2;   // loads of a wavefront and group
   constexpr int kA = BM * kS8LineA, kB = BN * kS8LineB, kS = 4 * (BM + BN);
-  constexpr int kB0 = 3 * kA, kS0 = kB0 + 3 * kB, kNone = kS0 + 3 * kS;
+  constexpr int kPlaces = MF == 4 ? 2 : 3;
+  constexpr int kB0 = kPlaces * kA, kS0 = kB0 + kPlaces * kB, kNone = kS0 + kPlaces * kS;
   __shared__ __align__(1024) uint8_t lds[kNone + 256];
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -224,7 +334,7 @@ __global__ void __launch_bounds__(256, 1) k_mx8_score_tile(
   for (int p = 0; p < 2; ++p)
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load(p, p, i);
-  arrive<kLoads>();
+  arrive<kLoads>();   // the first group's
 #pragma unroll
   for (int j = 0; j < 8; ++j) read_b(0, j);
 #pragma unroll
@@ -233,14 +343,15 @@ __global__ void __launch_bounds__(256, 1) k_mx8_score_tile(
   // Group t is in place p, the next one in p1, and p2 is free to be written.
   int p = 0;
   for (int t = 0; t < steps; ++t) {
-    const int p1 = p == 2 ? 0 : p + 1, p2 = p1 == 2 ? 0 : p1 + 1;
+    const int p1 = p == kPlaces - 1 ? 0 : p + 1, p2 = p1 == kPlaces - 1 ? 0 : p1 + 1;
     for_each<8 * MF>([&](auto q_) __attribute__((always_inline)) {
-      constexpr int q = decltype(q_)::value, each = MF == 8 ? 3 : 1;
+      constexpr int q = decltype(q_)::value;
       constexpr int k = q / 8, j = q % 8;
-      if constexpr (q == 8 * (MF - 2)) arrive<kLoads>();
+      if constexpr (q == 8 * (MF - 2)) arrive<MF == 4 ? 0 : kLoads>();
       acc[k][j] = mx84_mfma(fb[j], fa[k & 3], acc[k][j]);
       if constexpr (k < MF - 2 && j % 2 == 1 && j < 7) read_a(p, k + 2, j >> 1);
-      if constexpr (q % each == 0 && q / each < kLoads) load(t + 2, p2, q / each);
+      if constexpr (MF == 8 && q % 3 == 0 && q / 3 < kLoads) load(t + 2, p2, q / 3);
+      if constexpr (MF == 4 && q >= 16 && q - 16 < kLoads) load(t + 2, p, q - 16);
       if constexpr (k == MF - 2 && j < 6) read_a(p1, j / 3, j % 3);
       if constexpr (k == MF - 1) read_b(p1, j);
       __builtin_amdgcn_sched_barrier(0);
@@ -304,16 +415,35 @@ static void launch_score8_direct(const Mx8ScoreCall &c) {
                      c.bc, c.bs, c.n, c.steps, c.out, c.stride);
 }
 
+template <int T, bool SPLIT, bool HELD>
+static void launch_score8_few_one(const Mx8ScoreCall &c) {
+  const int64_t tiles = (c.n + 15) / 16, wg = SPLIT ? tiles : (tiles + 3) / 4;
+  const size_t lds = HELD ? size_t(c.m) * c.steps * 132 : 0;
+  // no more workgroups than the GPU holds at once, so that each fills its LDS once, and the
+  // same number of tiles to each
+  const int64_t most = 256 * (lds > 40960 ? 2 : lds > 20480 ? 3 : 4), rounds = (wg + most - 1) / most;
+  hipLaunchKernelGGL((k_mx8_score_few<T, SPLIT, HELD>), dim3(unsigned((wg + rounds - 1) / rounds)), dim3(256), lds, c.s, c.ac,
+                     c.as, int(c.m), c.bc, c.bs, c.n, c.steps, c.out, c.stride, tiles);
+}
+template <int T>
+static void launch_score8_few(const Mx8ScoreCall &c) {
+  const bool split = (c.n + 15) / 16 < 4096 && c.steps >= 4, held = c.m * c.steps * 128 <= kFew8Lds;
+  if (split && held) launch_score8_few_one<T, true, true>(c);
+  else if (split) launch_score8_few_one<T, true, false>(c);
+  else if (held) launch_score8_few_one<T, false, true>(c);
+  else launch_score8_few_one<T, false, false>(c);
+}
+
 template <int T>
 static void launch_score8(const Mx8ScoreCall &c) {
-  if constexpr (T != RSLM_F32) {
-    const Mx4MatmulForm form = matmul_form(c.m, c.n);
-    if (form == kMmTile256) return launch_score8_tile<T, 8>(c);
-    if (form == kMmTile128) return launch_score8_tile<T, 4>(c);
+  if (c.m <= 16) return launch_score8_few<T>(c);
+  if constexpr (T == RSLM_F32) {
+    if (c.m > 32 || matmul_direct_grid(c.m, c.n, 32).x > kMostWorkgroups) launch_score8_direct<T, 4>(c);
+    else launch_score8_direct<T, 2>(c);
+  } else {
+    if (matmul_form(c.m, c.n) == kMmTile256 && c.steps >= 12) launch_score8_tile<T, 8>(c);
+    else launch_score8_tile<T, 4>(c);
   }
-  if (c.m > 32 || matmul_direct_grid(c.m, c.n, 16).x > kMostWorkgroups) launch_score8_direct<T, 4>(c);
-  else if (c.m > 16) launch_score8_direct<T, 2>(c);
-  else launch_score8_direct<T, 1>(c);
 }
 
 }  // namespace rslm
