@@ -79,17 +79,43 @@ __global__ void __launch_bounds__(256) k_embed(EmbedArgs a) {
 }
 
 // ---- the sort
+//
+// Of 65,536 entries 4 kernels of a few us each, bound by their chains of reads, barriers
+// and votes; the table is filled with zeros beside them, by workgroups of their own.
 
 // A token of the sort: its id (the number of rows: none) and its place.
 typedef uint2 Entry;   // x: id, y: place
 
 constexpr int kSortThreads = 256;
-constexpr int kSortEach = 16;                                // entries of a thread
+constexpr int kSortEach = 8;                                 // entries of a thread
 constexpr int kSortRound = kSortThreads * kSortEach;         // entries of a workgroup's round
 constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kSortMaxBits = 9;
 constexpr int kSortMaxBins = 1 << kSortMaxBits;
 constexpr int kSortMaxTiles = 256;
+
+// A part of the table's rows, to be filled with zeros by the workgroups past `from`.
+struct Fill {
+  void *table;
+  int64_t row0, row1, stride;
+  int dim, type, from;
+};
+
+__device__ __forceinline__ void fill_rows(const Fill &f) {
+  const float zero[8] = {};
+  const int pieces = (f.dim + 7) / 8;
+  const int64_t n = (f.row1 - f.row0) * pieces, step = int64_t(gridDim.x - f.from) * 256;
+  for (int64_t i = int64_t(blockIdx.x - f.from) * 256 + threadIdx.x; i < n; i += step) {
+    const int64_t row = i / pieces;
+    const int c = int(i - row * pieces) * 8;
+    if (f.type == RSLM_F32)
+      store_float8<RSLM_F32>(zero, static_cast<float *>(f.table) + (f.row0 + row) * f.stride, c, f.dim);
+    else
+      store_float8<RSLM_F16>(zero, static_cast<uint16_t *>(f.table) + (f.row0 + row) * f.stride, c, f.dim);
+  }
+}
+
+__global__ void __launch_bounds__(256) k_embed_fill(Fill f) { fill_rows(f); }
 
 struct SortArgs {
   const void *ids;         // of the first pass; null: entries
@@ -100,114 +126,199 @@ struct SortArgs {
   int64_t n, per;          // per: entries of a workgroup, a multiple of kSortRound
   int shift, bits, tiles;
   uint32_t *counts;        // tiles x bins
+  Fill fill;
 };
 
-__device__ __forceinline__ Entry sort_entry(const SortArgs &a, int64_t i) {
-  if (!a.ids) return a.in[i];
+__device__ __forceinline__ Entry id_entry(const SortArgs &a, int64_t i) {
   const int64_t id = id_at(a.ids, a.wide, i);
   return make_uint2(id >= 0 && id < a.rows ? uint32_t(id) : uint32_t(a.rows), uint32_t(i));
 }
+__device__ __forceinline__ Entry sort_entry(const SortArgs &a, int64_t i) { return a.ids ? id_entry(a, i) : a.in[i]; }
 
 // How many entries of a workgroup's run have each digit.
 __global__ void __launch_bounds__(kSortThreads) k_sort_count(SortArgs a) {
+  if (int(blockIdx.x) >= a.tiles) return fill_rows(a.fill);
   __shared__ uint32_t bins[kSortMaxBins];
   const int nb = 1 << a.bits;
   for (int b = threadIdx.x; b < nb; b += kSortThreads) bins[b] = 0u;
   __syncthreads();
   const int64_t i0 = int64_t(blockIdx.x) * a.per, i1 = min(a.n, i0 + a.per);
-  for (int64_t i = i0 + threadIdx.x; i < i1; i += kSortThreads)
-    atomicAdd(&bins[(sort_entry(a, i).x >> a.shift) & (nb - 1)], 1u);
-  __syncthreads();
-  for (int b = threadIdx.x; b < nb; b += kSortThreads) a.counts[int64_t(blockIdx.x) * nb + b] = bins[b];
-}
-
-// Entries to their places: behind those of lower digits, those of the same digit in the
-// workgroups before this one, and those of the same digit before it here.  A wavefront
-// takes 16 x 64 consecutive entries of a round; lanes with the same digit are found by a
-// vote on each of its bits.
-__global__ void __launch_bounds__(kSortThreads) k_sort_move(SortArgs a) {
-  __shared__ uint32_t start[kSortMaxBins];              // of this workgroup's next entry of a digit
-  __shared__ uint32_t own[kSortWaves][kSortMaxBins];    // counts, then places, of a wavefront's entries
-  __shared__ uint32_t sums[kSortThreads];
-  const int nb = 1 << a.bits, tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
-  // each thread: neighbouring digits
-  const int each = (nb + kSortThreads - 1) / kSortThreads;
-  uint32_t total[2] = {}, before[2] = {};
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const int b = tid * each + q;
-    if (q < each && b < nb)
-      for (int t = 0; t < a.tiles; ++t) {
-        const uint32_t c = a.counts[int64_t(t) * nb + b];
-        total[q] += c;
-        before[q] += t < int(blockIdx.x) ? c : 0u;
-      }
-  }
-  uint32_t sum = total[0] + total[1];
-  sums[tid] = sum;
-  __syncthreads();
-  for (int off = 1; off < kSortThreads; off <<= 1) {
-    const uint32_t o = tid >= off ? sums[tid - off] : 0u;
-    __syncthreads();
-    sum += o;
-    sums[tid] = sum;
-    __syncthreads();
-  }
-  uint32_t at = sum - total[0] - total[1];
-#pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const int b = tid * each + q;
-    if (q < each && b < nb) start[b] = at + before[q];
-    at += total[q];
-  }
-  const int64_t i0 = int64_t(blockIdx.x) * a.per, i1 = min(a.n, i0 + a.per);
   for (int64_t r0 = i0; r0 < i1; r0 += kSortRound) {
-    for (int b = tid; b < nb; b += kSortThreads)
-#pragma unroll
-      for (int w = 0; w < kSortWaves; ++w) own[w][b] = 0u;
-    __syncthreads();
     Entry e[kSortEach];
-    const int64_t w0 = r0 + wid * (64 * kSortEach) + lane;
 #pragma unroll
     for (int k = 0; k < kSortEach; ++k) {
-      const int64_t i = w0 + 64 * k;
+      const int64_t i = r0 + k * kSortThreads + threadIdx.x;
       e[k] = i < i1 ? sort_entry(a, i) : make_uint2(0u, 0u);
     }
 #pragma unroll
     for (int k = 0; k < kSortEach; ++k)
-      if (w0 + 64 * k < i1) atomicAdd(&own[wid][(e[k].x >> a.shift) & (nb - 1)], 1u);
-    __syncthreads();
-    for (int b = tid; b < nb; b += kSortThreads) {
-      uint32_t p = start[b];
+      if (r0 + k * kSortThreads + threadIdx.x < i1) atomicAdd(&bins[(e[k].x >> a.shift) & (nb - 1)], 1u);
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < nb; b += kSortThreads) a.counts[int64_t(blockIdx.x) * nb + b] = bins[b];
+}
+
+struct SortSmem {
+  uint32_t start[kSortMaxBins];              // of this workgroup's next entry of a digit
+  uint32_t own[kSortWaves][kSortMaxBins];    // counts, then places, of a wavefront's entries
+  uint32_t sums[kSortWaves];
+};
+
+// sm.start: the sum of total over the lower digits, plus before.  Thread t has the digits
+// 2 t and 2 t + 1 (`each` 2), or t.
+__device__ __forceinline__ void sort_starts(SortSmem &sm, const uint32_t (&total)[2], const uint32_t (&before)[2],
+                                            int each, int nb) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  const uint32_t mine = total[0] + total[1];
+  uint32_t upto = mine;
 #pragma unroll
-      for (int w = 0; w < kSortWaves; ++w) {
-        const uint32_t c = own[w][b];
-        own[w][b] = p;
-        p += c;
-      }
-      start[b] = p;
+  for (int off = 1; off < 64; off <<= 1) {
+    const uint32_t o = __shfl_up(upto, off, 64);
+    upto += lane >= off ? o : 0u;
+  }
+  if (lane == 63) sm.sums[tid >> 6] = upto;
+  __syncthreads();
+  uint32_t at = upto - mine;
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) at += w < (tid >> 6) ? sm.sums[w] : 0u;
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    const int b = tid * each + q;
+    if (q < each && b < nb) sm.start[b] = at + before[q];
+    at += total[q];
+  }
+}
+
+// A round's `count` entries e to their places.  A wavefront has 64 kSortEach consecutive
+// ones, 64 at a time; lanes with the same digit are found by a vote on each of its bits.
+// sm.start moves on.
+template <class Out>
+__device__ __forceinline__ void sort_round(SortSmem &sm, const Entry (&e)[kSortEach], int count, int shift, int bits,
+                                           Out &&out) {
+  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, nb = 1 << bits;
+  for (int b = tid; b < nb; b += kSortThreads)
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) sm.own[w][b] = 0u;
+  __syncthreads();
+  const int first = wid * (64 * kSortEach) + lane;
+#pragma unroll
+  for (int k = 0; k < kSortEach; ++k)
+    if (first + 64 * k < count) atomicAdd(&sm.own[wid][(e[k].x >> shift) & (nb - 1)], 1u);
+  __syncthreads();
+  for (int b = tid; b < nb; b += kSortThreads) {
+    uint32_t p = sm.start[b];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      const uint32_t c = sm.own[w][b];
+      sm.own[w][b] = p;
+      p += c;
     }
-    __syncthreads();
+    sm.start[b] = p;
+  }
+  __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kSortEach; ++k) {
-      const bool on = w0 + 64 * k < i1;
-      const uint32_t d = (e[k].x >> a.shift) & (nb - 1);
-      uint64_t same = __ballot(on);
-      for (int bit = 0; bit < a.bits; ++bit) {
-        const uint64_t set = __ballot(on && (d >> bit & 1));
+  for (int k = 0; k < kSortEach; ++k) {
+    const bool on = first + 64 * k < count;
+    const uint32_t d = (e[k].x >> shift) & (nb - 1);
+    uint64_t same = __ballot(on);
+#pragma unroll
+    for (int bit = 0; bit < kSortMaxBits; ++bit)
+      if (bit < bits) {
+        const uint64_t set = __ballot(d >> bit & 1);   // that of lanes without an entry does not matter
         same &= (d >> bit & 1) ? set : ~set;
       }
-      if (on) {
-        const int rank = __popcll(same & ((1ull << lane) - 1));
-        const uint32_t p = own[wid][d] + rank;
-        a.out[p] = e[k];
-        // the wavefront's reads of this step come before the write, its next ones after
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (rank == 0) own[wid][d] = p + __popcll(same);
-      }
+    if (on) {
+      const int rank = __popcll(same & ((1ull << lane) - 1));
+      const uint32_t p = sm.own[wid][d] + rank;
+      out(p, e[k]);
+      // the wavefront's reads of this step come before the write, its next ones after
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (rank == 0) sm.own[wid][d] = p + __popcll(same);
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+  __syncthreads();
+}
+
+// Entries to their places: behind those of lower digits, those of the same digit in the
+// workgroups before this one, and those of the same digit before it here.
+__global__ void __launch_bounds__(kSortThreads) k_sort_move(SortArgs a) {
+  if (int(blockIdx.x) >= a.tiles) return fill_rows(a.fill);
+  __shared__ SortSmem sm;
+  const int nb = 1 << a.bits, tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+  const int64_t i0 = int64_t(blockIdx.x) * a.per, i1 = min(a.n, i0 + a.per);
+  Entry e[kSortEach];
+  auto read = [&](int64_t r0) {
+#pragma unroll
+    for (int k = 0; k < kSortEach; ++k) {
+      const int64_t i = r0 + wid * (64 * kSortEach) + lane + 64 * k;
+      e[k] = i < i1 ? sort_entry(a, i) : make_uint2(0u, 0u);
+    }
+  };
+  read(i0);
+  const int each = nb > kSortThreads ? 2 : 1;   // neighbouring digits of a thread
+  uint32_t total[2] = {}, before[2] = {};
+  if (tid * each < nb) {
+    const uint32_t *c = a.counts + tid * each;
+    constexpr int U = 16;   // tiles' counts asked for at once
+    for (int t0 = 0; t0 < a.tiles; t0 += U) {
+      uint32_t v[U][2];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t at = int64_t(min(t0 + u, a.tiles - 1)) * nb;
+        v[u][0] = c[at];
+        v[u][1] = c[at + each - 1];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const uint32_t w = t0 + u < a.tiles && q < each ? v[u][q] : 0u;
+          total[q] += w;
+          before[q] += t0 + u < int(blockIdx.x) ? w : 0u;
+        }
+    }
+  }
+  sort_starts(sm, total, before, each, nb);
+  for (int64_t r0 = i0; r0 < i1; r0 += kSortRound) {
+    if (r0 > i0) read(r0);
+    sort_round(sm, e, int(i1 - r0 < kSortRound ? i1 - r0 : kSortRound), a.shift, a.bits,
+               [&](uint32_t p, const Entry &v) { a.out[p] = v; });
+  }
+}
+
+// All passes over one round's entries, in LDS.
+__global__ void __launch_bounds__(kSortThreads) k_sort_small(SortArgs a, int passes) {
+  if (int(blockIdx.x) >= 1) return fill_rows(a.fill);
+  __shared__ SortSmem sm;
+  __shared__ Entry held[kSortRound];
+  const int nb = 1 << a.bits, tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, n = int(a.n);
+  const int first = wid * (64 * kSortEach) + lane;
+  Entry e[kSortEach];
+#pragma unroll
+  for (int k = 0; k < kSortEach; ++k) e[k] = first + 64 * k < n ? id_entry(a, first + 64 * k) : make_uint2(0u, 0u);
+  const int each = nb > kSortThreads ? 2 : 1;
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = pass * a.bits;
+    for (int b = tid; b < nb; b += kSortThreads) sm.start[b] = 0u;
     __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kSortEach; ++k)
+      if (first + 64 * k < n) atomicAdd(&sm.start[(e[k].x >> shift) & (nb - 1)], 1u);
+    __syncthreads();
+    uint32_t total[2] = {}, before[2] = {};
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+      if (q < each && tid * each + q < nb) total[q] = sm.start[tid * each + q];
+    sort_starts(sm, total, before, each, nb);   // a barrier between these reads and its writes
+    if (pass + 1 < passes) {
+      sort_round(sm, e, n, shift, a.bits, [&](uint32_t p, const Entry &v) { held[p] = v; });
+#pragma unroll
+      for (int k = 0; k < kSortEach; ++k)
+        if (first + 64 * k < n) e[k] = held[first + 64 * k];
+    } else {
+      sort_round(sm, e, n, shift, a.bits, [&](uint32_t p, const Entry &v) { a.out[p] = v; });
+    }
   }
 }
 
@@ -230,42 +341,71 @@ struct EmbedSumArgs {
 };
 
 constexpr int kSumCols = 512;   // columns of a wavefront
-constexpr int kSumFlight = 4;   // rows asked for at once
+constexpr int kSumFlight = 4;   // rows asked for at once, twice
 
-template <int TO>
-__device__ __forceinline__ void put_row(const EmbedSumArgs &a, uint32_t id, int c, const float (&acc)[8]) {
+// A lane's 8 columns of a row: those from `at` on, of which the first `skip` are another
+// lane's.  So a row's last columns too are read and written 8 at a time, and no branch
+// keeps a wavefront's loads apart (of 65,536 x 768 bfloat16, with a branch for the last
+// columns 72 us; so and twice as many chunks ?).  Rows of less than 8: WIDE false.
+struct SumLane {
+  int at, skip;
+};
+__device__ __forceinline__ SumLane sum_lane(int dim) {
+  const int c = int(blockIdx.y) * kSumCols + 8 * int(threadIdx.x & 63);
+  const int at = min(c, dim - 8);
+  return SumLane{at, min(c - at, 8)};
+}
+template <int T, bool WIDE>
+__device__ __forceinline__ void sum_load(Raw8<T> &p, const void *row, const SumLane &l, int dim) {
+  typedef typename FloatType<T>::type F;
+  if constexpr (!WIDE) {
+    load_raw8<T>(p, row, 0, dim);
+  } else if constexpr (T == RSLM_F32) {
+    const F32x8u a = *reinterpret_cast<const F32x8u *>(static_cast<const F *>(row) + l.at);
+    __builtin_memcpy(&p, &a, sizeof(a));
+  } else {
+    const H16x8u a = *reinterpret_cast<const H16x8u *>(static_cast<const F *>(row) + l.at);
+    __builtin_memcpy(&p, &a, sizeof(a));
+  }
+}
+template <int T, bool WIDE>
+__device__ __forceinline__ void sum_store(const float (&v)[8], void *row, const SumLane &l, int dim) {
+  if constexpr (!WIDE) {
+    if (l.skip == 0) store_float8<T>(v, row, 0, dim);
+  } else if (l.skip == 0) {
+    store_float8<T>(v, row, l.at, dim);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i >= l.skip) store_float<T>(row, l.at + i, v[i]);
+  }
+}
+
+template <int TO, bool WIDE>
+__device__ __forceinline__ void put_row(const EmbedSumArgs &a, uint32_t id, const SumLane &l, const float (&acc)[8]) {
   typename FloatType<TO>::type *o = static_cast<typename FloatType<TO>::type *>(a.dtable) + int64_t(id) * a.dstride;
   float v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = acc[i] * a.scale;
   if (a.add) {
-    float old[8];
-    load_float8<TO>(old, o, c, a.dim);
+    Raw8<TO> old;
+    sum_load<TO, WIDE>(old, o, l, a.dim);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += old[i];
+    for (int i = 0; i < 8; ++i) v[i] += float(old.v[i]);
   }
-  store_float8<TO>(v, o, c, a.dim);
-}
-
-template <int TO>
-__global__ void __launch_bounds__(256) k_embed_fill(void *p, int64_t rows, int64_t stride, int dim) {
-  const float zero[8] = {};
-  const int pieces = (dim + 7) / 8;
-  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < rows * pieces; i += int64_t(gridDim.x) * 256) {
-    const int64_t row = i / pieces;
-    store_float8<TO>(zero, static_cast<typename FloatType<TO>::type *>(p) + row * stride, int(i - row * pieces) * 8, dim);
-  }
+  sum_store<TO, WIDE>(v, o, l, a.dim);
 }
 
 // A wavefront: `chunk` sorted entries by 512 columns.  Runs inside them go to the table,
 // those that begin before or go on after to `head` and `tail`.
-template <int T, int TO>
+template <int T, int TO, bool WIDE>
 __global__ void __launch_bounds__(256) k_embed_sum(EmbedSumArgs a) {
   const int lane = threadIdx.x & 63;
-  const int64_t chunk = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int64_t chunk = int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (chunk >= a.chunks) return;
   const int64_t e0 = chunk * a.chunk, e1 = min(a.n, e0 + a.chunk);
-  const int c = int(blockIdx.y) * kSumCols + 8 * lane;
+  SumLane l = sum_lane(WIDE ? a.dim : 8);
+  if (!WIDE) l.skip = lane ? 8 : 0;
   const uint32_t none = a.rows;
   uint32_t id = e0 > 0 ? a.sorted[e0 - 1].x : none;   // of the run that acc sums
   bool from_before = true;
@@ -274,68 +414,106 @@ __global__ void __launch_bounds__(256) k_embed_sum(EmbedSumArgs a) {
     const int count = int(e1 - b < 64 ? e1 - b : 64);
     Entry mine = make_uint2(none, 0u);
     if (lane < count) mine = a.sorted[b + lane];
-    for (int k = 0; k < count; k += kSumFlight) {
-      Raw8<T> raw[kSumFlight];
-      uint32_t next[kSumFlight];
+    Raw8<T> raw[2][kSumFlight];
+    auto fetch = [&](int set, int k) {
 #pragma unroll
       for (int u = 0; u < kSumFlight; ++u) {
-        const int at = min(k + u, count - 1);
-        next[u] = __builtin_amdgcn_readlane(mine.x, at);
-        const uint32_t place = __builtin_amdgcn_readlane(mine.y, at);
-        // entries outside the table are last, and their rows are not read
-        load_raw8<T>(raw[u], static_cast<const typename FloatType<T>::type *>(a.dout) + int64_t(place) * a.stride, c,
-                     next[u] == none ? 0 : a.dim);
+        // behind the last entry, that one's row again; of one outside the table its row, unused
+        const uint32_t place = __builtin_amdgcn_readlane(mine.y, min(k + u, count - 1));
+        sum_load<T, WIDE>(raw[set][u], static_cast<const typename FloatType<T>::type *>(a.dout) + int64_t(place) * a.stride,
+                          l, a.dim);
       }
+    };
+    fetch(0, 0);
+    for (int k0 = 0; k0 < count; k0 += 2 * kSumFlight) {
 #pragma unroll
-      for (int u = 0; u < kSumFlight; ++u) {
-        if (k + u >= count) break;
-        if (next[u] != id) {
-          if (b + k + u > e0 && id != none) {
-            if (from_before) store_float8<RSLM_F32>(acc, a.head + chunk * a.dim, c, a.dim);
-            else put_row<TO>(a, id, c, acc);
+      for (int set = 0; set < 2; ++set) {
+        const int k = k0 + set * kSumFlight;
+        fetch(set ^ 1, k + kSumFlight);
+#pragma unroll
+        for (int u = 0; u < kSumFlight; ++u) {
+          if (k + u >= count) break;
+          const uint32_t next = __builtin_amdgcn_readlane(mine.x, k + u);
+          if (next != id) {
+            if (b + k + u > e0 && id != none) {
+              if (from_before) sum_store<RSLM_F32, WIDE>(acc, a.head + chunk * a.dim, l, a.dim);
+              else put_row<TO, WIDE>(a, id, l, acc);
+            }
+            id = next;
+            from_before = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] = 0.f;
           }
-          id = next[u];
-          from_before = false;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+          for (int i = 0; i < 8; ++i) acc[i] += float(raw[set][u].v[i]);
         }
-        float v[8];
-        raw_values<T>(v, raw[u]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) acc[i] += v[i];
       }
     }
   }
   if (id == none) return;
   const bool goes_on = e1 < a.n && a.sorted[e1].x == id;
-  if (from_before) store_float8<RSLM_F32>(acc, a.head + chunk * a.dim, c, a.dim);
-  else if (goes_on) store_float8<RSLM_F32>(acc, a.tail + chunk * a.dim, c, a.dim);
-  else put_row<TO>(a, id, c, acc);
+  if (from_before) sum_store<RSLM_F32, WIDE>(acc, a.head + chunk * a.dim, l, a.dim);
+  else if (goes_on) sum_store<RSLM_F32, WIDE>(acc, a.tail + chunk * a.dim, l, a.dim);
+  else put_row<TO, WIDE>(a, id, l, acc);
 }
 
-// Runs over several chunks: the tail of the one that they begin in, and the heads after it.
-template <int TO>
+// Runs over several chunks: the tail of the one that they begin in, and the heads after
+// it, every fourth of them to a wavefront.
+template <int TO, bool WIDE>
 __global__ void __launch_bounds__(256) k_embed_join(EmbedSumArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t chunk = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (chunk >= a.chunks) return;
-  const int64_t e0 = chunk * a.chunk, e1 = e0 + a.chunk;
-  if (e1 >= a.n) return;
+  __shared__ float sums[3][kSumCols];
+  __shared__ int ends;
+  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+  const int64_t chunk = blockIdx.x, e0 = chunk * a.chunk, e1 = e0 + a.chunk;
   const uint32_t id = a.sorted[e1 - 1].x;
-  if (id == a.rows || a.sorted[e1].x != id) return;
-  if (e0 > 0 && a.sorted[e0 - 1].x == id) return;   // began before
-  const int c = int(blockIdx.y) * kSumCols + 8 * lane;
-  float acc[8];
-  load_float8<RSLM_F32>(acc, a.tail + chunk * a.dim, c, a.dim);
-  for (int64_t j = chunk + 1;; ++j) {
-    float v[8];
-    load_float8<RSLM_F32>(v, a.head + j * a.dim, c, a.dim);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] += v[i];
-    const int64_t end = (j + 1) * a.chunk;
-    if (end >= a.n || a.sorted[end].x != id) break;
+  const uint32_t behind = a.sorted[e1].x, ahead = e0 > 0 ? a.sorted[e0 - 1].x : a.rows;
+  if (id == a.rows || behind != id || ahead == id) return;   // ends here, or began before
+  // the last head: that of the first chunk whose end is not the run's
+  int64_t last = chunk + 1;
+  for (;; last += 256) {
+    if (tid == 0) ends = 256;
+    __syncthreads();
+    const int64_t end = (last + tid + 1) * a.chunk;
+    if (end >= a.n || a.sorted[end].x != id) atomicMin(&ends, tid);
+    __syncthreads();
+    const int first = ends;
+    __syncthreads();
+    if (first < 256) {
+      last += first;
+      break;
+    }
   }
-  put_row<TO>(a, id, c, acc);
+  SumLane l = sum_lane(WIDE ? a.dim : 8);
+  if (!WIDE) l.skip = lane ? 8 : 0;
+  float acc[8] = {};
+  if (wid == 0) {
+    Raw8<RSLM_F32> v;
+    sum_load<RSLM_F32, WIDE>(v, a.tail + chunk * a.dim, l, a.dim);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = v.v[i];
+  }
+  constexpr int U = 4;
+  for (int64_t j = chunk + 1 + wid; j <= last; j += 4 * U) {
+    Raw8<RSLM_F32> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      sum_load<RSLM_F32, WIDE>(v[u], a.head + min(j + 4 * u, last) * a.dim, l, a.dim);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[i] += j + 4 * u <= last ? v[u].v[i] : 0.f;
+  }
+  if (wid > 0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[wid - 1][8 * lane + i] = acc[i];
+  }
+  __syncthreads();
+  if (wid > 0) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] += sums[w][8 * lane + i];
+  put_row<TO, WIDE>(a, id, l, acc);
 }
 
 // ---- host
@@ -357,10 +535,10 @@ static EmbedPlan embed_plan(int64_t n, int64_t rows, int dim) {
   const int64_t rounds = (n + kSortRound - 1) / kSortRound;
   p.per = (rounds + kSortMaxTiles - 1) / kSortMaxTiles * kSortRound;
   p.tiles = p.per ? int((n + p.per - 1) / p.per) : 0;
-  // 16 wavefronts to a CU, chunks of 16 to 512 entries
+  // 16 wavefronts to a CU, chunks of 8 to 512 entries
   const int64_t cols = (dim + kSumCols - 1) / kSumCols;
-  p.chunk = 16;
-  while (p.chunk < 512 && (n + p.chunk - 1) / p.chunk * cols > 8192) p.chunk *= 2;
+  p.chunk = 8;
+  while (p.chunk < 512 && (n + p.chunk - 1) / p.chunk * cols > 4096) p.chunk *= 2;
   p.chunks = (n + p.chunk - 1) / p.chunk;
   p.entries = rounded(size_t(n) * sizeof(Entry));
   p.counts = rounded(size_t(p.tiles) * (size_t(1) << p.bits) * 4);
@@ -369,11 +547,18 @@ static EmbedPlan embed_plan(int64_t n, int64_t rows, int dim) {
   return p;
 }
 
+template <int T, int TO, bool WIDE>
+static void launch_sums_one(const EmbedSumArgs &a, hipStream_t s) {
+  const dim3 grid(unsigned((a.chunks + 3) / 4), unsigned((a.dim + kSumCols - 1) / kSumCols));
+  hipLaunchKernelGGL((k_embed_sum<T, TO, WIDE>), grid, dim3(256), 0, s, a);
+  // the last chunk has none after it
+  if (a.chunks > 1)
+    hipLaunchKernelGGL((k_embed_join<TO, WIDE>), dim3(unsigned(a.chunks - 1), grid.y), dim3(256), 0, s, a);
+}
 template <int T, int TO>
 static void launch_sums(const EmbedSumArgs &a, hipStream_t s) {
-  const dim3 grid(unsigned((a.chunks + 3) / 4), unsigned((a.dim + kSumCols - 1) / kSumCols));
-  hipLaunchKernelGGL((k_embed_sum<T, TO>), grid, dim3(256), 0, s, a);
-  if (a.chunks > 1) hipLaunchKernelGGL(k_embed_join<TO>, grid, dim3(256), 0, s, a);
+  if (a.dim >= 8) launch_sums_one<T, TO, true>(a, s);
+  else launch_sums_one<T, TO, false>(a, s);
 }
 
 template <int S>
@@ -403,6 +588,12 @@ static int embed_call(EmbedArgs a, int stype, int out_dtype, void *stream) {
   else if (stype == RSLM_BF16) launch_embed<RSLM_BF16>(a, out_dtype, s);
   else launch_embed<kMx4Table>(a, out_dtype, s);
   return check_launch();
+}
+
+// Workgroups that fill rows with zeros, 8 values a thread.
+static unsigned fill_groups(int64_t rows, int dim) {
+  const int64_t wg = (rows * ((dim + 7) / 8) + 255) / 256;
+  return unsigned(wg < 2048 ? wg : 2048);
 }
 
 static bool ids_ok(const void *ids, int id_bytes) { return ids && aligned_to(ids, id_bytes); }
@@ -461,27 +652,40 @@ int rslm_embed_backward(const void *dout, int32_t dtype, int64_t n, int32_t dim,
   if (n > 0 && ws_bytes < p.total) return RSLM_ERR_WORKSPACE;
   if (n > 0 && (!ws || !aligned_to(ws, 16))) return RSLM_ERR_INVALID_ARG;
   const hipStream_t s = as_stream(stream);
-  if (!accumulate) {
-    const int64_t pieces = rows * ((dim + 7) / 8), wg = (pieces + 255) / 256;
-    const dim3 grid(unsigned(wg < 8192 ? wg : 8192));
-    if (table_dtype == RSLM_F32)
-      hipLaunchKernelGGL(k_embed_fill<RSLM_F32>, grid, dim3(256), 0, s, dtable, rows, table_stride, dim);
-    else
-      hipLaunchKernelGGL(k_embed_fill<RSLM_F16>, grid, dim3(256), 0, s, dtable, rows, table_stride, dim);
+  if (n == 0) {
+    const dim3 grid(fill_groups(rows, dim));
+    hipLaunchKernelGGL(k_embed_fill, grid, dim3(256), 0, s, Fill{dtable, 0, rows, table_stride, dim, table_dtype, 0});
+    return check_launch();
   }
-  if (n == 0) return check_launch();
   char *w = static_cast<char *>(ws);
   Entry *in = reinterpret_cast<Entry *>(w), *out = reinterpret_cast<Entry *>(w + p.entries);
   SortArgs a{ids, id_bytes == 8, rows, in, out, n, p.per, 0, p.bits, p.tiles,
              reinterpret_cast<uint32_t *>(w + 2 * p.entries)};
-  for (int pass = 0; pass < p.passes; ++pass) {
-    hipLaunchKernelGGL(k_sort_count, dim3(unsigned(p.tiles)), dim3(kSortThreads), 0, s, a);
-    hipLaunchKernelGGL(k_sort_move, dim3(unsigned(p.tiles)), dim3(kSortThreads), 0, s, a);
-    a.ids = nullptr;
-    a.shift += p.bits;
-    const Entry *sorted = a.out;
-    a.out = const_cast<Entry *>(a.in);
-    a.in = sorted;
+  // a part of the table's rows is filled beside each kernel of the sort
+  const int64_t parts = p.tiles == 1 ? 1 : 2 * p.passes;
+  int64_t part = 0;
+  auto grid = [&] {
+    const int64_t row0 = rows * part / parts, row1 = rows * (part + 1) / parts;
+    ++part;
+    a.fill = Fill{dtable, row0, row1, table_stride, dim, table_dtype, p.tiles};
+    return dim3(unsigned(p.tiles) + (accumulate ? 0u : fill_groups(row1 - row0, dim)));
+  };
+  if (p.tiles == 1) {
+    const dim3 g = grid();
+    hipLaunchKernelGGL(k_sort_small, g, dim3(kSortThreads), 0, s, a, p.passes);
+    a.in = a.out;
+  } else {
+    for (int pass = 0; pass < p.passes; ++pass) {
+      const dim3 g0 = grid();
+      hipLaunchKernelGGL(k_sort_count, g0, dim3(kSortThreads), 0, s, a);
+      const dim3 g1 = grid();
+      hipLaunchKernelGGL(k_sort_move, g1, dim3(kSortThreads), 0, s, a);
+      a.ids = nullptr;
+      a.shift += p.bits;
+      const Entry *sorted = a.out;
+      a.out = const_cast<Entry *>(a.in);
+      a.in = sorted;
+    }
   }
   float *sums = reinterpret_cast<float *>(w + 2 * p.entries + p.counts);
   const EmbedSumArgs b{a.in,  n,   uint32_t(rows), p.chunk, p.chunks,     dout,   stride,
