@@ -672,7 +672,7 @@ int rslm_logprob_backward(const void *scores, int32_t dtype, int64_t m, int64_t 
  * A score of -infinity is masked: it has no probability.  A target's row without
  * any, or with a NaN or +infinity, lets its draft fall and draws -1; such a draft's
  * row lets it fall, and p is drawn from.  Sums and weights are float64, an
- * exponential within 2^-44 of its value.
+ * exponential within 2^-42 of its value.
  * k <= 64, 1 <= n <= 2^31 - 8,193, b (2 k + 1) <= 8,388,607; scales above 0, at
  * most 2^127.  k = 0 draws a token from each row.  ws: 16-byte aligned; draft:
  * whether there are draft scores.

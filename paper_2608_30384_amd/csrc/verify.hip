@@ -5,28 +5,47 @@
 // from p_i: the first j with r_0 + .. + r_j > u_K sum r.
 //
 // All of it is in float64: at 131,072 entries an error of 1e-7 in the sums would draw
-// another token once in some hundred.  An exponential is then a table of 64 entries, a
-// polynomial and a scaling.
+// another token once in some hundred.  An exponential is then a table of 256 entries, a
+// polynomial of degree 3 and a scaling, some 18 instructions, which bound the first kernel
+// where there are many rows.
 //
-// Bound by one read of the scores, where there are many rows: a first kernel sums them,
-// a slice of a row to a workgroup; a second settles which drafts stand (each workgroup
-// for itself) and sums r over the slices where it is not p; a third draws.
+// Three kernels.  The first sums the exponentials of every row, a slice of 1,024 entries
+// (more where a row has over 262,144) to a wavefront.  The second settles which drafts
+// stand, each workgroup for itself, and where one falls sums r over the slices.  The third
+// settles the same and draws: the slice, then the token.
 #include "mx4_dev.h"
 
 namespace rslm {
 
 constexpr int kVfThreads = 256;
-constexpr int kVfEach = 16;                         // entries of a thread in a piece
-constexpr int kVfPiece = kVfThreads * kVfEach;
-constexpr int kVfMaxSlices = 64;                    // a lane of a wavefront to each
+constexpr int kVfWaves = kVfThreads / 64;
+constexpr int kVfEach = 16;                         // entries of a lane in a block
+constexpr int kVfBlock = 64 * kVfEach;
+constexpr int kVfMaxSlices = 256;
 constexpr int kVfMaxDrafts = 64;
 constexpr double kLn2d = 0.693147180559945309417;
 
-// Sum of 2^(scale log2(e) (v - m)) over a slice, m its largest score; z is NaN where a
-// score is NaN or +infinity.
+// 2^(i / 256).
+struct VfTable {
+  double v[256];
+};
+constexpr VfTable vf_table() {
+  VfTable t{};
+  for (int i = 0; i < 256; ++i) {
+    const double x = kLn2d * i / 256;
+    double e = 1;
+    for (int k = 24; k > 0; --k) e = 1 + e * x / k;   // the exponential's series
+    t.v[i] = e;
+  }
+  return t;
+}
+__device__ const VfTable kVfTable = vf_table();
+
+// A sum of weights 2^((v - top) scale / 256) of scores v, `top` the largest; z is NaN where
+// a score is NaN or +infinity.  (With v scale - top scale in one fused step a score of 1e20
+// and more would not be 0 beside itself.)
 struct VfSum {
-  double z;
-  float m;
+  double z, top;
 };
 
 struct VerifyArgs {
@@ -37,9 +56,10 @@ struct VerifyArgs {
   const int64_t *tokens;
   const float *uniforms;
   const int32_t *counts;
-  double tscale, dscale;            // times 64 log2(e)
-  int slices;
-  int64_t per;
+  double tscale, dscale;            // times 256 log2(e)
+  int slices, blocks;               // of a row; blocks of a slice
+  int each, groups;                 // slices of a wavefront, workgroups of a row, in the first kernel
+  int oeach, ogroups;               // and of a sequence in the second
   VfSum *tsums, *dsums;             // b x (k + 1) x slices, b x k x slices
   double *rsums;                    // b x slices
   int64_t *out;
@@ -47,42 +67,35 @@ struct VerifyArgs {
   float *logprob;
 };
 
-// 2^(y / 64), y <= 0.  y = i + f with |f| <= 1/2: the table has 2^((i mod 64) / 64), and
-// 2^(f / 64) is its Taylor polynomial of degree 4, off by 4e-14 of itself.
-__device__ __forceinline__ double exp64(double y, const double *table) {
-  constexpr double l = kLn2d / 64;
+// 2^(y / 256), y <= 0.  y = i + f with |f| <= 1/2: the table has 2^((i mod 256) / 256), and
+// 2^(f / 256) is its Taylor polynomial of degree 3, off by 1.4e-13 of itself.  0 for -infinity
+// (and NaN).
+__device__ __forceinline__ double exp256(double y, const double *table) {
+  constexpr double l = kLn2d / 256;
   constexpr double big = 6755399441055744.0;   // 1.5 2^52: adding it rounds to a whole number
-  y = fmax(y, -80000.0);                       // 2^-1250: zero
+  y = fmax(y, -320000.0);                      // 2^-1250: zero
   const double t = y + big;
   const double f = y - (t - big);
   const int i = int(uint32_t(__builtin_bit_cast(uint64_t, t)));
-  double p = fma(f, l * l * l * l / 24, l * l * l / 6);
-  p = fma(f, p, l * l / 2);
-  p = fma(f, p, l);
-  const double e = table[i & 63];
-  return ldexp(fma(e, f * p, e), i >> 6);
+  const double p = fma(f, fma(f, l * l * l / 6, l * l / 2), l);
+  const double e = table[i & 255];
+  return ldexp(fma(e, f * p, e), i >> 8);
 }
-__device__ __forceinline__ void fill_table(double *table) {
-  if (threadIdx.x < 64) table[threadIdx.x] = exp2(double(threadIdx.x) / 64);
-  __syncthreads();
+__device__ __forceinline__ double weight64(float v, double top, double scale, const double *table) {
+  return exp256((double(v) - top) * scale, table);
 }
-// of a score v beside the largest one m; 0 for -infinity
-__device__ __forceinline__ double weight64(float v, double m, double scale, const double *table) {
-  return exp64((double(v) - m) * scale, table);
-}
+// Without a barrier: that is the caller's.
+__device__ __forceinline__ void fill_table(double *table) { table[threadIdx.x] = kVfTable.v[threadIdx.x]; }
 
-__device__ __forceinline__ VfSum vf_join(const VfSum &a, const VfSum &b, double scale, const double *table) {
-  const float m = fmaxf(a.m, b.m);
-  if (m == -__builtin_inff()) return VfSum{a.z + b.z, m};
-  return VfSum{a.z * weight64(a.m, m, scale, table) + b.z * weight64(b.m, m, scale, table), m};
-}
-__device__ __forceinline__ VfSum vf_join_wave(VfSum s, double scale, const double *table) {
+__device__ __forceinline__ double wave_sum64(double v) {
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) {
-    const VfSum o{__shfl_xor(s.z, off, 64), __shfl_xor(s.m, off, 64)};
-    s = vf_join(s, o, scale, table);
-  }
-  return s;
+  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+  return v;
+}
+__device__ __forceinline__ double wave_max64(double v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v = fmax(v, __shfl_xor(v, off, 64));
+  return v;
 }
 
 __device__ __forceinline__ int vf_count(const VerifyArgs &a, int b) {
@@ -97,71 +110,102 @@ __device__ __forceinline__ const typename FloatType<T>::type *draft_row(const Ve
   return static_cast<const typename FloatType<T>::type *>(a.draft) + b * a.dseq + i * a.drow;
 }
 
-// x[j .. j + 7], -infinity at and past end.
+// A lane's entries of the block at j, as they are stored: 8 at 8 lane, 8 at 512 + 8 lane;
+// -infinity at and past end, which the block may be behind.
 template <int T>
-__device__ __forceinline__ void load_scores8(Raw8<T> &p, const typename FloatType<T>::type *x, int64_t j, int64_t end) {
-  const int64_t left = end - j;
-  load_raw8<T>(p, x + (left > 0 ? j : 0), 0, left >= 8 ? 8 : left > 0 ? int(left) : 0);
-  if (left < 8) {
+struct VfRaw {
+  Raw8<T> v[kVfEach / 8];
+};
+template <int T>
+__device__ __forceinline__ void load_block(VfRaw<T> &p, const typename FloatType<T>::type *x, int64_t j, int64_t end) {
+  typedef typename FloatType<T>::type F;
+  const int lane = threadIdx.x & 63;
+  if (j + kVfBlock <= end) {   // the same for all lanes: no branch keeps the loads apart
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i >= left) p.v[i] = typename FloatType<T>::type(-__builtin_inff());
+    for (int u = 0; u < kVfEach / 8; ++u) load_raw8<T>(p.v[u], x + j + u * 512 + 8 * lane, 0, 8);
+  } else {
+#pragma unroll
+    for (int u = 0; u < kVfEach / 8; ++u)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int64_t at = j + u * 512 + 8 * lane + i;
+        const F e = x[min(at, end - 1)];
+        p.v[u].v[i] = at < end ? e : F(-__builtin_inff());
+      }
   }
 }
 
 template <int T>
 __global__ void __launch_bounds__(kVfThreads) k_verify_sums(VerifyArgs a) {
-  __shared__ double table[64];
-  __shared__ VfSum parts[kVfThreads / 64];
-  const int tid = threadIdx.x;
-  const int slice = int(blockIdx.x) % a.slices;
-  const int64_t row = int64_t(blockIdx.x) / a.slices;
-  const int64_t trows = int64_t(a.b) * (a.k + 1);
+  __shared__ double table[256];
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t row = int64_t(blockIdx.x) / a.groups, trows = int64_t(a.b) * (a.k + 1);
   const bool draft = row >= trows;
   const int64_t at = draft ? row - trows : row;
-  const int each = draft ? a.k : a.k + 1;
-  const int b = int(at / each), i = int(at % each);
+  const int b = int(at / (draft ? a.k : a.k + 1)), i = int(at - int64_t(b) * (draft ? a.k : a.k + 1));
   // rows past the sequence's last draft are not read
   if (i >= vf_count(a, b) + (draft ? 0 : 1)) return;
   const auto *x = draft ? draft_row<T>(a, b, i) : target_row<T>(a, b, i);
   const double scale = draft ? a.dscale : a.tscale;
-  const int64_t j0 = slice * a.per, j1 = min(a.n, j0 + a.per);
+  // slices s0, s0 + 4, ..
+  const int s0 = (int(blockIdx.x) % a.groups) * (kVfWaves * a.each) + wid;
+  const int mine = min(a.each, (a.slices - s0 + kVfWaves - 1) / kVfWaves);
+  auto place = [&](int t) {   // of the wavefront's block t
+    const int s = s0 + kVfWaves * (t / a.blocks);
+    return (int64_t(s) * a.blocks + t % a.blocks) * kVfBlock;
+  };
+  VfRaw<T> next;
+  if (mine > 0) load_block<T>(next, x, place(0), a.n);
   fill_table(table);
-  float m = -__builtin_inff();
-  double z = 0;
+  __syncthreads();
+  VfSum s{0.0, -__builtin_inf()};
   bool bad = false;
-  for (int64_t j = j0; j < j1; j += kVfPiece) {
-    Raw8<T> raw[kVfEach / 8];
-#pragma unroll
-    for (int u = 0; u < kVfEach / 8; ++u) load_scores8<T>(raw[u], x, j + (u * kVfThreads + tid) * 8, j1);
+  for (int t = 0; t < mine * a.blocks; ++t) {
     float v[kVfEach];
-    float top = m;
+#pragma unroll
+    for (int q = 0; q < kVfEach; ++q) v[q] = float(next.v[q / 8].v[q % 8]);
+    if (t + 1 < mine * a.blocks) load_block<T>(next, x, place(t + 1), a.n);
+    float m = v[0];
 #pragma unroll
     for (int q = 0; q < kVfEach; ++q) {
-      v[q] = float(raw[q / 8].v[q % 8]);
       bad |= !(v[q] < __builtin_inff());
-      top = fmaxf(top, v[q]);
+      m = fmaxf(m, v[q]);
     }
-    if (top > m) {
-      if (m > -__builtin_inff()) z *= weight64(m, top, scale, table);
-      m = top;
-    }
-    const double ref = m == -__builtin_inff() ? 0.0 : double(m);
+    const double top = fmax(s.top, double(wave_max(m)));
+    if (a.blocks > 1) s.z *= exp256((s.top - top) * scale, table);
+    s.top = top;
 #pragma unroll
-    for (int q = 0; q < kVfEach; ++q) z += weight64(v[q], ref, scale, table);
+    for (int q = 0; q < kVfEach; ++q) s.z += weight64(v[q], top, scale, table);
+    if (a.blocks == 1 || t % a.blocks == a.blocks - 1) {
+      s.z = __ballot(bad) ? __builtin_nan("") : wave_sum64(s.z);
+      if (lane == 0) (draft ? a.dsums : a.tsums)[at * a.slices + s0 + kVfWaves * (t / a.blocks)] = s;
+      s = VfSum{0.0, -__builtin_inf()};
+      bad = false;
+    }
   }
-  if (bad) z = __builtin_nan("");
-  VfSum s = vf_join_wave(VfSum{z, m}, scale, table);
-  if ((tid & 63) == 0) parts[tid >> 6] = s;
-  __syncthreads();
-  if (tid) return;
+}
+
+// The slices' sums of a row, by a wavefront.
+__device__ __forceinline__ VfSum join_slices(const VfSum *sums, int slices, double scale, const double *table) {
+  const int lane = threadIdx.x & 63;
+  VfSum v[kVfMaxSlices / 64];
+  double top = -__builtin_inf();
 #pragma unroll
-  for (int w = 1; w < kVfThreads / 64; ++w) s = vf_join(s, parts[w], scale, table);
-  (draft ? a.dsums + at * a.slices : a.tsums + at * a.slices)[slice] = s;
+  for (int u = 0; u < kVfMaxSlices / 64; ++u) {
+    v[u] = VfSum{0.0, -__builtin_inf()};
+    if (64 * u + lane < slices) v[u] = sums[64 * u + lane];
+    top = fmax(top, v[u].top);
+  }
+  top = wave_max64(top);
+  double z = 0;
+#pragma unroll
+  for (int u = 0; u < kVfMaxSlices / 64; ++u)
+    if (64 * u < slices) z += v[u].z * exp256((v[u].top - top) * scale, table);
+  return VfSum{wave_sum64(z), top};
 }
 
 // What a sequence's drafts come to: how many stand, and of the rows that the next token is
-// drawn from their largest scores and sums.
+// drawn from their sums.
 struct Settled {
   int accepted, count;
   VfSum p, q;
@@ -173,31 +217,38 @@ __device__ __forceinline__ void settle(const VerifyArgs &a, int b, const double 
                                        Settled &out) {
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
   const int count = vf_count(a, b);
-  for (int r = wid; r < 2 * count + 1; r += kVfThreads / 64) {
+  // asked for first: two reads, one after the other
+  bool inside = false;
+  float px = 0.f, qx = 0.f, u = 0.f;
+  if (wid == 0 && lane < count) {
+    const int64_t x = a.tokens[int64_t(b) * a.k + lane];
+    u = a.uniforms[int64_t(b) * (a.k + 1) + lane];
+    inside = x >= 0 && x < a.n;
+    if (inside) {
+      px = float(target_row<T>(a, b, lane)[x]);
+      if (a.draft) qx = float(draft_row<T>(a, b, lane)[x]);
+    }
+  }
+  for (int r = wid; r < (a.draft ? 2 * count + 1 : count + 1); r += kVfWaves) {
     const bool draft = r > count;
-    if (draft && !a.draft) break;
     const int i = draft ? r - count - 1 : r;
-    const VfSum *sums = draft ? a.dsums + (int64_t(b) * a.k + i) * a.slices : a.tsums + (int64_t(b) * (a.k + 1) + i) * a.slices;
-    VfSum s{0.0, -__builtin_inff()};
-    if (lane < a.slices) s = sums[lane];
-    s = vf_join_wave(s, draft ? a.dscale : a.tscale, table);
+    const VfSum s = join_slices(draft ? a.dsums + (int64_t(b) * a.k + i) * a.slices
+                                      : a.tsums + (int64_t(b) * (a.k + 1) + i) * a.slices, a.slices,
+                                draft ? a.dscale : a.tscale, table);
     if (lane == 0) rows[draft][i] = s;
   }
   __syncthreads();
   if (wid == 0) {
     bool stands = false;
-    if (lane < count) {
-      const int64_t x = a.tokens[int64_t(b) * a.k + lane];
-      if (x >= 0 && x < a.n) {
-        const VfSum p = rows[0][lane], q = rows[1][lane];
-        const double px = weight64(float(target_row<T>(a, b, lane)[x]), p.m, a.tscale, table) / p.z;
-        const double qx = a.draft ? weight64(float(draft_row<T>(a, b, lane)[x]), q.m, a.dscale, table) / q.z : 1.0;
-        stands = double(a.uniforms[int64_t(b) * (a.k + 1) + lane]) * qx < px;
-      }
+    if (inside) {
+      const VfSum p = rows[0][lane], q = rows[1][lane];
+      const double is = weight64(px, p.top, a.tscale, table) / p.z;
+      const double was = a.draft ? weight64(qx, q.top, a.dscale, table) / q.z : 1.0;
+      stands = double(u) * was < is;
     }
-    const int accepted = __ffsll(static_cast<unsigned long long>(~__ballot(stands))) - 1;
+    const int fallen = __ffsll(static_cast<unsigned long long>(~__ballot(stands))) - 1;   // -1: none of 64
     if (lane == 0) {
-      const int n = accepted < 0 ? count : min(accepted, count);
+      const int n = fallen < 0 ? count : min(fallen, count);
       out.accepted = n;
       out.count = count;
       out.p = rows[0][n];
@@ -207,159 +258,161 @@ __device__ __forceinline__ void settle(const VerifyArgs &a, int b, const double 
   __syncthreads();
 }
 
-// r of an entry, where a draft fell: what p has over q.
+// The weight r of an entry: p, or where a draft fell what p has over q.
 struct Over {
   bool drafted;
   int64_t x;   // without the draft's scores: its token
-  double pm, pz, qm, qz, ps, qs;
-  template <int T>
-  __device__ __forceinline__ double of(const VerifyArgs &a, float v, float d, int64_t j, const double *table) const {
+  VfSum p, q;  // z: the sums' reciprocals
+  double ps, qs;
+  bool with;
+  __device__ __forceinline__ double of(float v, float d, int64_t j, const double *table) const {
 #pragma clang fp contract(off)   // of equal p and q nothing is left
-    const double p = weight64(v, pm, ps, table) * pz;
-    if (!drafted) return p;
-    if (!a.draft) return j == x ? 0.0 : p;
-    const double r = p - weight64(d, qm, qs, table) * qz;
+    const double is = weight64(v, p.top, ps, table) * p.z;
+    if (!drafted) return is;
+    if (!with) return j == x ? 0.0 : is;
+    const double r = is - weight64(d, q.top, qs, table) * q.z;
     return r > 0 ? r : 0.0;
   }
 };
 __device__ __forceinline__ Over over_of(const VerifyArgs &a, int b, const Settled &s, bool drafted) {
   Over o;
   o.drafted = drafted;
+  o.with = drafted && a.draft;
   o.x = drafted && !a.draft ? a.tokens[int64_t(b) * a.k + s.accepted] : -1;
-  o.pm = s.p.m, o.pz = 1.0 / s.p.z, o.ps = a.tscale;
-  o.qm = s.q.m, o.qz = 1.0 / s.q.z, o.qs = a.dscale;
+  o.p = VfSum{1.0 / s.p.z, s.p.top}, o.ps = a.tscale;
+  o.q = VfSum{1.0 / s.q.z, s.q.top}, o.qs = a.dscale;
   return o;
-}
-
-__device__ __forceinline__ double wave_sum64(double v) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
-  return v;
 }
 
 // Of each sequence with a draft that fell: r summed over each slice.
 template <int T>
 __global__ void __launch_bounds__(kVfThreads) k_verify_over(VerifyArgs a) {
-  __shared__ double table[64];
+  __shared__ double table[256];
   __shared__ VfSum rows[2][kVfMaxDrafts + 1];
   __shared__ Settled st;
-  __shared__ double parts[kVfThreads / 64];
-  const int tid = threadIdx.x;
-  const int slice = int(blockIdx.x) % a.slices, b = int(blockIdx.x / a.slices);
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int b = int(blockIdx.x) / a.ogroups;
   fill_table(table);
+  __syncthreads();
   settle<T>(a, b, table, rows, st);
   if (st.accepted == st.count) return;
   const Over over = over_of(a, b, st, true);
   const auto *x = target_row<T>(a, b, st.accepted);
   const auto *d = a.draft ? draft_row<T>(a, b, st.accepted) : x;
-  const int64_t j0 = slice * a.per, j1 = min(a.n, j0 + a.per);
-  double sum = 0;
-  for (int64_t j = j0; j < j1; j += kVfPiece)
+  for (int t = 0; t < a.oeach; ++t) {
+    const int s = (int(blockIdx.x) % a.ogroups) * (kVfWaves * a.oeach) + kVfWaves * t + wid;
+    if (s >= a.slices) break;
+    double sum = 0;
+    for (int64_t j = int64_t(s) * a.blocks * kVfBlock, e = j + int64_t(a.blocks) * kVfBlock; j < min(e, a.n); j += kVfBlock) {
+      VfRaw<T> rp, rq;
+      load_block<T>(rp, x, j, a.n);
+      load_block<T>(rq, d, j, a.n);
 #pragma unroll
-    for (int u = 0; u < kVfEach / 8; ++u) {
-      const int64_t at = j + (u * kVfThreads + tid) * 8;
-      Raw8<T> rp, rq;
-      load_scores8<T>(rp, x, at, j1);
-      load_scores8<T>(rq, d, at, j1);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) sum += over.of<T>(a, float(rp.v[q]), float(rq.v[q]), at + q, table);
+      for (int q = 0; q < kVfEach; ++q)
+        sum += over.of(float(rp.v[q / 8].v[q % 8]), float(rq.v[q / 8].v[q % 8]), j + (q >> 3) * 512 + 8 * lane + (q & 7), table);
     }
-  sum = wave_sum64(sum);
-  if ((tid & 63) == 0) parts[tid >> 6] = sum;
-  __syncthreads();
-  if (tid) return;
+    sum = wave_sum64(sum);
+    if (lane == 0) a.rsums[int64_t(b) * a.slices + s] = sum;
+  }
+}
+
+__device__ __forceinline__ double wave_upto64(double v) {   // the sum of lanes up to this one
+  const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int w = 1; w < kVfThreads / 64; ++w) sum += parts[w];
-  a.rsums[int64_t(b) * a.slices + slice] = sum;
+  for (int off = 1; off < 64; off <<= 1) {
+    const double o = __shfl_up(v, off, 64);
+    if (lane >= off) v += o;
+  }
+  return v;
 }
 
 // A workgroup to a sequence: the slice that the drawn token is in, then the token.
 template <int T>
 __global__ void __launch_bounds__(kVfThreads) k_verify_draw(VerifyArgs a) {
-  __shared__ double table[64];
+  __shared__ double table[256];
   __shared__ VfSum rows[2][kVfMaxDrafts + 1];
   __shared__ Settled st;
-  __shared__ double sums[kVfMaxSlices], waves[kVfThreads / 64];
+  __shared__ double waves[kVfWaves];
   __shared__ double want_s, base_s;
-  __shared__ int slice_s, drafted_s;
-  __shared__ int found_s, last_s;
+  __shared__ int slice_s, drafted_s, found_s, last_s;
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, b = blockIdx.x;
   fill_table(table);
+  __syncthreads();
   settle<T>(a, b, table, rows, st);
   const int n = st.accepted;
   if (tid == 0) found_s = 0x7fffffff, last_s = -1;
   if (wid == 0) {
-    double s = 0;
+    constexpr int each = kVfMaxSlices / 64;   // neighbouring slices of a lane
+    double r[each] = {};
     bool drafted = n < st.count;
     if (drafted) {
-      s = lane < a.slices ? a.rsums[int64_t(b) * a.slices + lane] : 0.0;
-      drafted = __ballot(s > 0) != 0;   // else p and q are the same
+#pragma unroll
+      for (int i = 0; i < each; ++i)
+        if (each * lane + i < a.slices) r[i] = a.rsums[int64_t(b) * a.slices + each * lane + i];
+      drafted = __ballot(r[0] > 0 || r[1] > 0 || r[2] > 0 || r[3] > 0) != 0;   // else p and q are the same
     }
     if (!drafted) {
-      s = 0;
-      if (lane < a.slices) {
-        const VfSum t = a.tsums[(int64_t(b) * (a.k + 1) + n) * a.slices + lane];
-        s = t.m == -__builtin_inff() ? t.z : t.z * weight64(t.m, st.p.m, a.tscale, table) / st.p.z;
+      const VfSum *t = a.tsums + (int64_t(b) * (a.k + 1) + n) * a.slices;
+#pragma unroll
+      for (int i = 0; i < each; ++i) {
+        r[i] = 0;
+        if (each * lane + i < a.slices) {
+          const VfSum v = t[each * lane + i];
+          r[i] = v.z * exp256((v.top - st.p.top) * a.tscale, table) / st.p.z;
+        }
       }
     }
-    sums[lane] = s;
-    if (lane == 0) {
-      double total = 0;
-      for (int i = 0; i < a.slices; ++i) total += sums[i];
-      const float u = a.uniforms[int64_t(b) * (a.k + 1) + a.k];
-      const double want = double(fminf(fmaxf(u, 0.f), 0x1.fffffep-1f)) * total;
-      double c = 0;
-      int at = -1, i = 0;
-      double base = 0;
-      for (; i < a.slices; ++i) {
-        if (sums[i] > 0) at = i, base = c;   // the last one with any, should rounding pass them all
-        c += sums[i];
-        if (c > want) break;
+    double mine = 0;
+#pragma unroll
+    for (int i = 0; i < each; ++i) mine += r[i];
+    const double upto = wave_upto64(mine), total = __shfl(upto, 63, 64);
+    const double want = double(fminf(fmaxf(a.uniforms[int64_t(b) * (a.k + 1) + a.k], 0.f), 0x1.fffffep-1f)) * total;
+    // the first lane past `want`, or the last one with any, should rounding pass them all
+    const uint64_t past = __ballot(upto > want && mine > 0), any = __ballot(mine > 0);
+    const int in = past ? __ffsll(static_cast<unsigned long long>(past)) - 1 : 63 - __clzll(static_cast<long long>(any));
+    if (lane == in) {
+      double c = upto - mine, base = c;
+      int at = -1;
+#pragma unroll
+      for (int i = 0; i < each; ++i) {
+        if (r[i] > 0 && (at < 0 || !(c > want))) at = each * lane + i, base = c;
+        c += r[i];
       }
-      // NaN, or nothing: no token
-      slice_s = total > 0 && total < __builtin_inf() ? at : -1;
+      slice_s = at;
       base_s = base;
       want_s = want;
       drafted_s = drafted;
     }
+    if (lane == 0 && !(total > 0 && total < __builtin_inf())) slice_s = -1;   // NaN, or nothing: no token
   }
   __syncthreads();
   int token = -1;
   if (slice_s >= 0) {
+    constexpr int E = kVfBlock / kVfThreads;   // consecutive entries of a thread
     const Over over = over_of(a, b, st, drafted_s);
     const auto *x = target_row<T>(a, b, n);
-    const auto *d = a.draft && drafted_s ? draft_row<T>(a, b, n) : x;
-    const int64_t j0 = slice_s * a.per, j1 = min(a.n, j0 + a.per);
+    const auto *d = over.with ? draft_row<T>(a, b, n) : x;
+    const int64_t j0 = int64_t(slice_s) * a.blocks * kVfBlock, j1 = min(a.n, j0 + int64_t(a.blocks) * kVfBlock);
     double base = base_s;
-    for (int64_t j = j0; j < j1; j += kVfPiece) {
-      // 16 consecutive entries of a thread
-      const int64_t at = j + tid * kVfEach;
-      double r[kVfEach];
-      double sum = 0;
+    for (int64_t j = j0; j < j1; j += kVfBlock) {
+      const int64_t at = j + tid * E;
+      float v[E], w[E];
 #pragma unroll
-      for (int u = 0; u < kVfEach / 8; ++u) {
-        Raw8<T> rp, rq;
-        load_scores8<T>(rp, x, at + 8 * u, j1);
-        load_scores8<T>(rq, d, at + 8 * u, j1);
+      for (int q = 0; q < E; ++q) v[q] = float(x[min(at + q, j1 - 1)]), w[q] = float(d[min(at + q, j1 - 1)]);
+      double r[E], sum = 0;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          r[8 * u + q] = over.of<T>(a, float(rp.v[q]), float(rq.v[q]), at + 8 * u + q, table);
-          sum += r[8 * u + q];
-        }
+      for (int q = 0; q < E; ++q) {
+        r[q] = at + q < j1 ? over.of(v[q], w[q], at + q, table) : 0.0;
+        sum += r[q];
       }
-      double upto = sum;
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const double o = __shfl_up(upto, off, 64);
-        if (lane >= off) upto += o;
-      }
+      const double upto = wave_upto64(sum);
       if (lane == 63) waves[wid] = upto;
       __syncthreads();
       double c = base + (upto - sum);
-      for (int w = 0; w < wid; ++w) c += waves[w];
+      for (int k = 0; k < wid; ++k) c += waves[k];
       int found = 0x7fffffff, last = -1;
 #pragma unroll
-      for (int q = 0; q < kVfEach; ++q) {
+      for (int q = 0; q < E; ++q) {
         c += r[q];
         if (r[q] > 0) last = int(at) + q;
         if (c > want_s && r[q] > 0 && found == 0x7fffffff) found = int(at) + q;
@@ -368,7 +421,7 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_draw(VerifyArgs a) {
       if (last >= 0) atomicMax(&last_s, last);
       __syncthreads();
       if (found_s != 0x7fffffff) break;
-      for (int w = 0; w < kVfThreads / 64; ++w) base += waves[w];
+      for (int k = 0; k < kVfWaves; ++k) base += waves[k];
       __syncthreads();
     }
     token = found_s != 0x7fffffff ? found_s : last_s;
@@ -381,7 +434,7 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_draw(VerifyArgs a) {
       double lp = 0;
       if (t >= 0) {
         const VfSum p = rows[0][i];
-        lp = (double(float(target_row<T>(a, b, i)[t])) - double(p.m)) * (a.tscale * (kLn2d / 64)) - log(p.z);
+        lp = (double(float(target_row<T>(a, b, i)[t])) - p.top) * (a.tscale * (kLn2d / 256)) - log(p.z);
       }
       a.logprob[o] = float(lp);
     }
@@ -389,30 +442,35 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_draw(VerifyArgs a) {
   if (tid == 0) a.accepted[b] = n;
 }
 
-// Workgroups to fill the GPU, a piece each at least.
-static int verify_slices(int64_t rows, int64_t n) {
-  const int64_t most = (n + kVfPiece - 1) / kVfPiece;
-  int64_t s = (4096 + rows - 1) / rows;
-  if (s > most) s = most;
-  return int(s < 1 ? 1 : s > kVfMaxSlices ? kVfMaxSlices : s);
+static int64_t verify_rows(int64_t b, int k, bool draft) { return b * (k + 1 + (draft ? k : 0)); }
+
+// Blocks of a slice, and slices of a row.
+static int verify_blocks(int64_t n) { return int((n + int64_t(kVfBlock) * kVfMaxSlices - 1) / (int64_t(kVfBlock) * kVfMaxSlices)); }
+static int verify_slices(int64_t n) {
+  const int64_t slice = int64_t(kVfBlock) * verify_blocks(n);
+  return int((n + slice - 1) / slice);
 }
-static int64_t verify_rows(int b, int k, bool draft) { return int64_t(b) * (k + 1 + (draft ? k : 0)); }
+// Slices of a wavefront: one where that is no more than 4,096 workgroups.
+static int verify_each(int64_t rows, int slices, int64_t most) {
+  const int64_t each = rows * slices / (kVfWaves * most), all = (slices + kVfWaves - 1) / kVfWaves;
+  return int(each < 1 ? 1 : each > all ? all : each);
+}
 
 static bool verify_sizes_ok(int64_t b, int k, int64_t n) {
-  return b >= 0 && k >= 0 && k <= kVfMaxDrafts && n >= 1 && n <= 0x7fffffff - 2 * kVfPiece &&
+  return b >= 0 && k >= 0 && k <= kVfMaxDrafts && n >= 1 && n <= 0x7fffffff - 2 * 4096 &&
          b * (2 * k + 1) <= 0x7fffffff / kVfThreads;   // a grid counts its threads in 32 bits
 }
 
 static size_t verify_bytes(int64_t b, int k, bool draft, int slices) {
-  return size_t(verify_rows(int(b), k, draft)) * slices * sizeof(VfSum) + size_t(b) * slices * sizeof(double);
+  return size_t(verify_rows(b, k, draft)) * slices * sizeof(VfSum) + size_t(b) * slices * sizeof(double);
 }
 
 template <int T>
 static void launch_verify(const VerifyArgs &a, hipStream_t s) {
   const dim3 threads(kVfThreads);
-  hipLaunchKernelGGL(k_verify_sums<T>, dim3(unsigned(verify_rows(a.b, a.k, a.draft != nullptr) * a.slices)), threads, 0,
+  hipLaunchKernelGGL(k_verify_sums<T>, dim3(unsigned(verify_rows(a.b, a.k, a.draft != nullptr) * a.groups)), threads, 0,
                      s, a);
-  if (a.k > 0) hipLaunchKernelGGL(k_verify_over<T>, dim3(unsigned(a.b) * a.slices), threads, 0, s, a);
+  if (a.k > 0) hipLaunchKernelGGL(k_verify_over<T>, dim3(unsigned(int64_t(a.b) * a.ogroups)), threads, 0, s, a);
   hipLaunchKernelGGL(k_verify_draw<T>, dim3(unsigned(a.b)), threads, 0, s, a);
 }
 
@@ -424,7 +482,7 @@ extern "C" {
 
 size_t rslm_verify_workspace(int64_t b, int32_t k, int64_t n, int32_t draft) {
   if (!verify_sizes_ok(b, k, n) || b == 0) return 0;
-  return verify_bytes(b, k, draft != 0, verify_slices(verify_rows(int(b), k, draft != 0), n));
+  return verify_bytes(b, k, draft != 0, verify_slices(n));
 }
 
 int rslm_verify(const void *target, int32_t dtype, int64_t b, int32_t k, int64_t n, int64_t target_seq_stride,
@@ -445,12 +503,16 @@ int rslm_verify(const void *target, int32_t dtype, int64_t b, int32_t k, int64_t
   const bool with = draft != nullptr;
   if (ws_bytes < rslm_verify_workspace(b, k, n, with)) return RSLM_ERR_WORKSPACE;
   if (!ws || !aligned_to(ws, 16)) return RSLM_ERR_INVALID_ARG;
-  const double unit = 64 * 1.442695040888963407360;
+  const double unit = 256 * 1.442695040888963407360;
   VerifyArgs a{target, draft,  target_seq_stride, target_stride,  draft_seq_stride,
                draft_stride, int(b), k, n, tokens, uniforms, counts, double(scale) * unit,
                with ? double(draft_scale) * unit : 1.0};
-  a.slices = verify_slices(verify_rows(a.b, k, with), n);
-  a.per = (n + int64_t(a.slices) * kVfPiece - 1) / (int64_t(a.slices) * kVfPiece) * kVfPiece;
+  a.slices = verify_slices(n);
+  a.blocks = verify_blocks(n);
+  a.each = verify_each(verify_rows(b, k, with), a.slices, 4096);
+  a.groups = (a.slices + kVfWaves * a.each - 1) / (kVfWaves * a.each);
+  a.oeach = verify_each(b, a.slices, 1024);
+  a.ogroups = (a.slices + kVfWaves * a.oeach - 1) / (kVfWaves * a.oeach);
   a.tsums = static_cast<VfSum *>(ws);
   a.dsums = a.tsums + size_t(b) * (k + 1) * a.slices;
   a.rsums = reinterpret_cast<double *>(a.tsums + size_t(verify_rows(a.b, k, with)) * a.slices);

@@ -1,6 +1,6 @@
 """Verification of drafted tokens on the GPU against float64: the tokens and how many
-stand are equal (the kernels' weights are within 2^-44, so that a uniform number between
-both's borders has a chance below 1e-7 here), log probabilities within half a unit of
+stand are equal (the kernels' weights are within 2^-42, so that a uniform number between
+both's borders has a chance below 1e-7 a token here), log probabilities within half a unit of
 float32 and 1e-12 of the largest score's distance.
 """
 
