@@ -75,6 +75,139 @@ __device__ __forceinline__ void put_mx8(const float (&v)[8], uint8_t *codes, uin
   if ((chunk & 3) == 0) scales[chunk >> 2] = uint8_t(s);
 }
 
+// ---- rows held in registers
+//
+// LANES lanes of a workgroup of 256 to a row, NV pieces of 8 coordinates each.  A row's last
+// coordinates are read 8 at a time too, from dim - 8 on, and moved to their places: no
+// branch keeps a thread's loads apart.
+
+// One of 8 coordinates from c on: read from `at`, the first `skip` of them another piece's.
+struct Piece {
+  int c, at, skip;
+};
+__device__ __forceinline__ Piece piece_at(int c, int dim) {
+  const int at = min(c, dim - 8);
+  return Piece{c, at, c - at};
+}
+template <int T>
+__device__ __forceinline__ void load_piece(Raw8<T> &p, const typename FloatType<T>::type *row, const Piece &e) {
+  if constexpr (T == RSLM_F32) {
+    const F32x8u a = *reinterpret_cast<const F32x8u *>(row + e.at);
+    __builtin_memcpy(&p, &a, sizeof(a));
+  } else {
+    const H16x8u a = *reinterpret_cast<const H16x8u *>(row + e.at);
+    __builtin_memcpy(&p, &a, sizeof(a));
+  }
+}
+// Coordinates c .. c + 7 of what was read, 0 past dim.
+__device__ __forceinline__ void place_piece(float (&v)[8], const Piece &e, bool odd) {
+  if (odd) {   // dim % 8, the same for all
+#pragma unroll
+    for (int by = 1; by < 8; by <<= 1)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = e.skip & by ? (i + by < 8 ? v[i + by] : 0.f) : v[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = e.skip >= 8 ? 0.f : v[i];
+}
+template <int T>
+__device__ __forceinline__ void piece_values(float (&v)[8], const Raw8<T> &p, const Piece &e, bool odd) {
+  raw_values<T>(v, p);
+  place_piece(v, e, odd);
+}
+__device__ __forceinline__ void piece_weight(float (&w)[8], const void *p, int type, const Piece &e, bool odd) {
+  if (!p) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = 1.f;
+    return;
+  }
+  if (type == RSLM_F32) {
+    Raw8<RSLM_F32> r;
+    load_piece<RSLM_F32>(r, static_cast<const float *>(p), e);
+    raw_values<RSLM_F32>(w, r);
+  } else if (type == RSLM_F16) {
+    Raw8<RSLM_F16> r;
+    load_piece<RSLM_F16>(r, static_cast<const _Float16 *>(p), e);
+    raw_values<RSLM_F16>(w, r);
+  } else {
+    Raw8<RSLM_BF16> r;
+    load_piece<RSLM_BF16>(r, static_cast<const __bf16 *>(p), e);
+    raw_values<RSLM_BF16>(w, r);
+  }
+  place_piece(w, e, odd);
+}
+
+// The sum over a row's lanes, in each of them.  `sums`: LANES 256 alone, as group_sum.
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v, float *sums) {
+  if constexpr (LANES == 256) return group_sum(v, sums);
+#pragma unroll
+  for (int off = LANES / 2; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
+  return v;
+}
+
+template <int T, int LANES, int NV>
+__global__ void __launch_bounds__(kNormThreads) k_norm(NormArgs a) {
+  constexpr int R = kNormThreads / LANES;
+  __shared__ float sums[2][kNormThreads / 64];
+  const int lane = threadIdx.x % LANES, chunks = mx4_steps(a.dim) * 16;
+  const bool odd = a.dim & 7;
+  Piece e[NV];
+#pragma unroll
+  for (int u = 0; u < NV; ++u) e[u] = piece_at(8 * (lane + LANES * u), a.dim);
+  int turn = 0;
+  for (int64_t row0 = int64_t(blockIdx.x) * R; row0 < a.n; row0 += int64_t(gridDim.x) * R, turn ^= 1) {
+    // past the last row: that one again, without writing
+    const int64_t mine = row0 + threadIdx.x / LANES, row = min(mine, a.n - 1);
+    const bool on = mine < a.n;
+    Raw8<T> rx[NV], rr[NV];
+    const auto *x = row_of<T>(a.x, row, a.xstride);
+#pragma unroll
+    for (int u = 0; u < NV; ++u) load_piece<T>(rx[u], x, e[u]);
+    if (a.residual) {
+      const auto *r = row_of<T>(a.residual, row, a.rstride);
+#pragma unroll
+      for (int u = 0; u < NV; ++u) load_piece<T>(rr[u], r, e[u]);
+    }
+    float h[NV][8], sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      piece_values<T>(h[u], rx[u], e[u], odd);
+      if (a.residual) {
+        float r[8];
+        piece_values<T>(r, rr[u], e[u], odd);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[u][i] = float(typename FloatType<T>::type(h[u][i] + r[i]));
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = fmaf(h[u][i], h[u][i], sum);
+    }
+    if (a.residual && on) {
+#pragma unroll
+      for (int u = 0; u < NV; ++u) store_float8<T>(h[u], row_of<T>(a.h, row, a.hstride), e[u].c, a.dim);
+    }
+    float w[NV][8];
+#pragma unroll
+    for (int u = 0; u < NV; ++u) piece_weight(w[u], a.weight, a.wtype, e[u], odd);
+    const float rstd = 1.f / sqrtf(lanes_sum<LANES>(sum, sums[turn]) / float(a.dim) + a.eps);
+    if (lane == 0 && on) a.rstd[row] = rstd;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h[u][i] = h[u][i] * rstd * w[u][i] + 0.f;
+      if (a.y && on) store_float8<T>(h[u], row_of<T>(a.y, row, a.ystride), e[u].c, a.dim);
+      const int k = lane + LANES * u;   // whole quads: chunks is a multiple of 16
+      if (a.codes && on && k < chunks) {
+        if (e[u].c + 8 > a.dim) {   // 0 past dim, though rstd may be no number
+#pragma unroll
+          for (int i = 0; i < 8; ++i) h[u][i] = e[u].c + i < a.dim ? h[u][i] : 0.f;
+        }
+        put_mx8(h[u], a.codes + row * chunks * 8, a.scales + row * (chunks / 4), k);
+      }
+    }
+  }
+}
+
 // A row of any length to a workgroup, which reads it twice (h, written in between,
 // the second time; from the cache).
 template <int T>
@@ -108,7 +241,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_long(NormArgs a) {
       load_float8<T>(v, h, 8 * k, a.dim);
       load_weight8(w, a.weight, a.wtype, 8 * k, a.dim);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = v[i] * rstd * w[i] + 0.f;
+      for (int i = 0; i < 8; ++i) v[i] = 8 * k + i < a.dim ? v[i] * rstd * w[i] + 0.f : 0.f;
       if (a.y) store_float8<T>(v, row_of<T>(a.y, row, a.ystride), 8 * k, a.dim);
       if (a.codes) put_mx8(v, a.codes + row * chunks * 8, a.scales + row * (chunks / 4), k);
     }
@@ -126,6 +259,97 @@ struct NormBackArgs {
   float *partial;   // strips x dim
   int64_t per;      // rows of a strip
 };
+
+// Rows of a strip by a workgroup, R at a time, which sums dweight's part in registers.
+template <int T, int LANES, int NV>
+__global__ void __launch_bounds__(kNormThreads) k_norm_backward(NormBackArgs a) {
+  constexpr int R = kNormThreads / LANES;
+  __shared__ float sums[2][kNormThreads / 64];
+  __shared__ float parts[R > 1 ? kNormThreads * NV * 8 : 1];
+  const int lane = threadIdx.x % LANES;
+  const bool odd = a.dim & 7;
+  Piece e[NV];
+  float w[NV][8], acc[NV][8] = {};
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    e[u] = piece_at(8 * (lane + LANES * u), a.dim);
+    piece_weight(w[u], a.weight, a.wtype, e[u], odd);
+  }
+  const int64_t r0 = int64_t(blockIdx.x) * a.per, r1 = min(a.n, r0 + a.per);
+  Raw8<T> rd[NV], rh[NV], re[NV];
+  float rstd = 0.f;
+  auto fetch = [&](int64_t row0) {
+    const int64_t row = min(row0 + threadIdx.x / LANES, r1 - 1);
+    const auto *d = row_of<T>(a.dy, row, a.dystride), *h = row_of<T>(a.h, row, a.hstride);
+#pragma unroll
+    for (int u = 0; u < NV; ++u) load_piece<T>(rd[u], d, e[u]);
+#pragma unroll
+    for (int u = 0; u < NV; ++u) load_piece<T>(rh[u], h, e[u]);
+    if (a.dh) {
+      const auto *f = row_of<T>(a.dh, row, a.dhstride);
+#pragma unroll
+      for (int u = 0; u < NV; ++u) load_piece<T>(re[u], f, e[u]);
+    }
+    rstd = a.rstd[row];
+  };
+  int turn = 0;
+  if (r0 < r1) fetch(r0);
+  for (int64_t row0 = r0; row0 < r1; row0 += R, turn ^= 1) {
+    const int64_t row = row0 + threadIdx.x / LANES;
+    const bool on = row < r1;
+    float g[NV][8], n[NV][8], sum = 0.f;
+    const float now = rstd;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      float d[8];
+      piece_values<T>(d, rd[u], e[u], odd);
+      piece_values<T>(n[u], rh[u], e[u], odd);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        n[u][i] *= now;
+        if (on) acc[u][i] = fmaf(d[i], n[u][i], acc[u][i]);
+        g[u][i] = d[i] * w[u][i];
+        sum = fmaf(g[u][i], n[u][i], sum);
+      }
+    }
+    if (a.dx) {
+      const float mean = lanes_sum<LANES>(sum, sums[turn]) / float(a.dim);
+#pragma unroll
+      for (int u = 0; u < NV; ++u) {
+        float f[8] = {};
+        if (a.dh) piece_values<T>(f, re[u], e[u], odd);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[u][i] = fmaf(now, fmaf(-n[u][i], mean, g[u][i]), f[i]);
+      }
+    }
+    // the next rows' loads, before this one's stores (which may be to dy, h or dh, but of
+    // rows that are done)
+    if (row0 + R < r1) fetch(row0 + R);
+    if (a.dx && on) {
+#pragma unroll
+      for (int u = 0; u < NV; ++u) store_float8<T>(g[u], row_of<T>(a.dx, row, a.dxstride), e[u].c, a.dim);
+    }
+  }
+  if (!a.partial) return;
+  float *out = a.partial + int64_t(blockIdx.x) * a.dim;
+  if constexpr (R > 1) {
+    // the R rows' parts, in their order
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) parts[(threadIdx.x / LANES) * (LANES * NV * 8) + (u * LANES + lane) * 8 + i] = acc[u][i];
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.dim; c += kNormThreads) {
+      float s = parts[c];
+#pragma unroll
+      for (int r = 1; r < R; ++r) s += parts[r * (LANES * NV * 8) + c];
+      out[c] = s;
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < NV; ++u) store_float8<RSLM_F32>(acc[u], out, e[u].c, a.dim);
+  }
+}
 
 template <int T>
 __global__ void __launch_bounds__(kNormThreads) k_norm_backward_long(NormBackArgs a) {
@@ -179,48 +403,85 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_dweight(NormBackArgs a) {
   store_float8<RSLM_F32>(acc, a.partial + int64_t(blockIdx.y) * a.dim, c, a.dim);
 }
 
-// The strips' sums of a column, eight parts of them to eight threads, in a fixed order.
-__global__ void __launch_bounds__(256) k_norm_join(const float *__restrict__ partial, int strips, int dim,
-                                                   void *__restrict__ dweight, int wtype) {
-  __shared__ float sums[8][32];
+// The strips' sums of a column, 32 parts of them to 32 threads, in a fixed order.
+__global__ void __launch_bounds__(1024) k_norm_join(const float *__restrict__ partial, int strips, int dim,
+                                                    void *__restrict__ dweight, int wtype) {
+  __shared__ float sums[32][33];
   const int col = threadIdx.x & 31, part = threadIdx.x >> 5;
   const int c = int(blockIdx.x) * 32 + col;
   float s = 0.f;
-  if (c < dim)
-    for (int i = part; i < strips; i += 8) s += partial[int64_t(i) * dim + c];
+#pragma unroll 8
+  for (int i = part; i < strips; i += 32) s += partial[int64_t(i) * dim + min(c, dim - 1)];
   sums[part][col] = s;
   __syncthreads();
   if (part || c >= dim) return;
 #pragma unroll
-  for (int i = 1; i < 8; ++i) s += sums[i][col];
+  for (int i = 1; i < 32; ++i) s += sums[i][col];
   if (wtype == RSLM_F32) store_float<RSLM_F32>(dweight, c, s);
   else if (wtype == RSLM_F16) store_float<RSLM_F16>(dweight, c, s);
   else store_float<RSLM_BF16>(dweight, c, s);
 }
 
-constexpr int kNormStrips = 512;
+constexpr int kNormStrips = 512;   // two workgroups to a CU
+constexpr int kNormHeld = 16384, kNormBackHeld = 8192;   // coordinates of a row in registers
 
 static int64_t norm_strips(int64_t n) { return n < kNormStrips ? n : kNormStrips; }
 
+// The lanes of a row and its pieces: a row of up to 128 coordinates to 16 lanes, of up to
+// 1,024 to a wavefront, of more (or of over 512 where there are few) to a workgroup.
+#define RSLM_NORM_SWITCH(DIM, N, CALL)                          \
+  if ((DIM) <= 128) CALL(16, 1)                                 \
+  else if ((DIM) <= 512) CALL(64, 1)                            \
+  else if ((DIM) <= 1024 && (N) >= 1024) CALL(64, 2)            \
+  else if ((DIM) <= 2048) CALL(256, 1)                          \
+  else if ((DIM) <= 4096) CALL(256, 2)                          \
+  else CALL(256, 4)
+
 template <int T>
 static void launch_norm(const NormArgs &a, hipStream_t s) {
-  const dim3 grid(unsigned(a.n < 65536 ? a.n : 65536));
-  hipLaunchKernelGGL(k_norm_long<T>, grid, dim3(kNormThreads), 0, s, a);
+  if (a.dim < 8 || a.dim > kNormHeld) {
+    const dim3 grid(unsigned(a.n < 65536 ? a.n : 65536));
+    hipLaunchKernelGGL(k_norm_long<T>, grid, dim3(kNormThreads), 0, s, a);
+    return;
+  }
+#define RSLM_NORM(LANES, NV)                                                                       \
+  {                                                                                                \
+    const int64_t wg = (a.n + 256 / LANES - 1) / (256 / LANES);                                    \
+    const dim3 grid(unsigned(wg < 65536 ? wg : 65536));                                            \
+    hipLaunchKernelGGL((k_norm<T, LANES, NV>), grid, dim3(kNormThreads), 0, s, a);                 \
+  }
+  if (a.dim > 8192) RSLM_NORM(256, 8)
+  else RSLM_NORM_SWITCH(a.dim, a.n, RSLM_NORM)
+#undef RSLM_NORM
 }
 
 template <int T>
 static void launch_norm_backward(const NormBackArgs &b, void *dweight, int dwtype, hipStream_t s) {
   NormBackArgs a = b;
-  const dim3 grid(unsigned(a.n < 65536 ? a.n : 65536));
-  if (a.dx) hipLaunchKernelGGL(k_norm_backward_long<T>, grid, dim3(kNormThreads), 0, s, a);
-  if (!dweight) return;
-  const int64_t strips = norm_strips(a.n);
-  a.per = strips ? (a.n + strips - 1) / strips : 0;
-  if (strips)
-    hipLaunchKernelGGL(k_norm_dweight<T>, dim3(unsigned((a.dim + 2047) / 2048), unsigned(strips)), dim3(kNormThreads),
-                       0, s, a);
-  hipLaunchKernelGGL(k_norm_join, dim3(unsigned((a.dim + 31) / 32)), dim3(256), 0, s, a.partial, int(strips), a.dim,
-                     dweight, dwtype);
+  int64_t strips = norm_strips(a.n);
+  if (a.n > 0) {
+    a.per = (a.n + strips - 1) / strips;
+    if (a.dim < 8 || a.dim > kNormBackHeld) {
+      const dim3 grid(unsigned(a.n < 65536 ? a.n : 65536));
+      if (a.dx) hipLaunchKernelGGL(k_norm_backward_long<T>, grid, dim3(kNormThreads), 0, s, a);
+      if (dweight)
+        hipLaunchKernelGGL(k_norm_dweight<T>, dim3(unsigned((a.dim + 2047) / 2048), unsigned(strips)),
+                           dim3(kNormThreads), 0, s, a);
+    } else {
+      if (!dweight) a.partial = nullptr;
+#define RSLM_NORM(LANES, NV)                                                                       \
+  {                                                                                                \
+    a.per = (a.per + 256 / LANES - 1) / (256 / LANES) * (256 / LANES);                             \
+    strips = (a.n + a.per - 1) / a.per;                                                            \
+    hipLaunchKernelGGL((k_norm_backward<T, LANES, NV>), dim3(unsigned(strips)), dim3(kNormThreads), 0, s, a); \
+  }
+      RSLM_NORM_SWITCH(a.dim, a.n, RSLM_NORM)
+#undef RSLM_NORM
+    }
+  }
+  if (dweight)
+    hipLaunchKernelGGL(k_norm_join, dim3(unsigned((a.dim + 31) / 32)), dim3(1024), 0, s, a.partial, int(strips), a.dim,
+                       dweight, dwtype);
 }
 
 static bool norm_sizes_ok(int64_t n, int dim, int dtype) {
