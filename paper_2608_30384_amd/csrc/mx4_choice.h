@@ -1,4 +1,4 @@
-// Which arrangement of the kernels a product of MX4 rows takes, by its sizes.
+// Which arrangement of the kernels a product with MX4 rows takes, by its sizes.
 // Plain C++, so that the choice can be looked at without a GPU.
 #pragma once
 
@@ -56,6 +56,35 @@ inline Mx4MatmulForm matmul_form(int64_t m, int64_t n) {
   if ((m > 16 || matmul_direct_grid(m, n, 16).x > kMostWorkgroups) && pieces(32, 32) >= 1024) return kMmDirect32;
   return kMmDirect16;
 }
+
+// ---- 8-bit by 4-bit (mx8_score.hip)
+
+// Few rows of a; LDS tiles of 256 rows of a, one workgroup to a CU; or of less (128, to
+// float32 64), two workgroups to a CU.
+enum Mx8ScoreForm { kS8Few, kS8Tile256, kS8Tile };
+
+// Tiles of 256 rows where they fill the GPU and there are enough groups of 128 coordinates
+// to make up for a tile's beginning and end, which the other CU-sharing workgroup covers
+// else.  us, m x n x dim with tiles of 256 and of 128 rows to bfloat16, and of 256, 128 and
+// 64 to float32:
+//     512 x  32,768 x 4,096    52   68    1,024 x 32,768 x 4,096   244  282  296
+//   1,024 x  32,768 x 2,048    60   62      512 x 32,768 x 2,048    63   76   71
+//   4,096 x  32,768 x 1,536   182  192    2,048 x  8,192 x 2,048    72   78   75
+//   4,096 x  32,768 x 1,024   141  137    4,096 x 32,768 x 1,024   322  381  344
+//   1,024 x  32,768 x 1,024    39   35    1,024 x 32,768 x   512    53   61   53
+//   4,096 x 131,072 x   768   518  508      255 x 100,003 x 1,024   80   93   77
+//     257 x 100,000 x 1,024    64   39      300 x 100,000 x   768  117   89   70
+//                                            64 x 100,000 x   768   53   36   20
+inline Mx8ScoreForm score8_form(int64_t m, int64_t n, int steps) {
+  if (m <= 16) return kS8Few;
+  return matmul_form(m, n) == kMmTile256 && steps >= 12 ? kS8Tile256 : kS8Tile;
+}
+
+// Few rows: whether four wavefronts share out the groups of 16 rows of b (less than 16
+// wavefronts to a CU with one each), and whether a's codes are held in LDS.
+constexpr int kFew8Lds = 65536;
+inline bool few8_split(int64_t n, int steps) { return (n + 15) / 16 < 4096 && steps >= 4; }
+inline bool few8_held(int64_t m, int steps) { return m * steps * 128 <= kFew8Lds; }
 
 // ---- float by 4-bit (mx4_score.hip)
 

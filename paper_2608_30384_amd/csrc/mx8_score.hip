@@ -4,8 +4,9 @@
 // which takes both kinds of code as they are.  Of every 8 products that it adds first it
 // drops what lies more than 13 places below the largest's leading one (each product is cut
 // toward zero): less than 2^-13 of the largest for each of the others, of Gaussian rows
-// about 6e-6 of a result.  That is far below the rounding to 16 bits, but not float32.  Float32 results therefore
-// take the bfloat16 instruction, in which every value of either row is exact.
+// about 6e-6 of a result.  That is far below the rounding to 16 bits, but not float32.
+// Float32 results therefore take the bfloat16 instruction, in which every value of either
+// row is exact.
 #include "mx4_choice.h"
 #include "mx4_dev.h"
 
@@ -46,78 +47,14 @@ __device__ __forceinline__ f32x4 mx_mfma_bf16(uint4 a, uint4 b, f32x4 c) {
                                                  0);
 }
 
-// Each wavefront: 16 MT rows of a by 16 NT rows of b, operands straight from memory.  In
-// bfloat16 (T float32) lane group g multiplies coordinates 32 g .. + 31 of both, eight at a
-// time: the order of the sum is free.
-template <int T, int MT, int NT>
-__global__ void __launch_bounds__(256) k_mx8_score(const uint8_t *__restrict__ ac, const uint8_t *__restrict__ as,
-                                                   int64_t m, const uint8_t *__restrict__ bc,
-                                                   const uint8_t *__restrict__ bs, int64_t n, int steps,
-                                                   void *__restrict__ out, int64_t stride) {
-  constexpr bool kExact = T == RSLM_F32;
-  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-  const int64_t n0 = (int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6)) * (16 * NT);
-  const int64_t m0 = int64_t(blockIdx.y) * (16 * MT);
-  if (n0 >= n) return;
-  f32x4 acc[MT][NT] = {};
-  for (int t = 0; t < steps; ++t) {
-    Mx8Frag a[MT];
-    Mx4FragB b[NT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const int64_t at = min(m0 + 16 * i + r, m - 1) * steps + t;
-      const uint8_t *p = ac + at * 128 + (kExact ? 32 : 16) * g;
-      a[i].lo = *reinterpret_cast<const i32x4 *>(p);
-      a[i].hi = *reinterpret_cast<const i32x4 *>(p + (kExact ? 16 : 64));
-      a[i].s = as[at * 4 + g];
-    }
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const int64_t at = min(n0 + 16 * j + r, n - 1) * steps + t;
-      b[j].q = *reinterpret_cast<const i32x4 *>(bc + at * 64 + 16 * g);
-      b[j].s = bs[at * 4 + g];
-    }
-    if constexpr (kExact) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint4 x[MT], y[NT];
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          const i32x4 w = q < 2 ? a[i].lo : a[i].hi;
-          x[i] = mx8_bf16x8(make_uint2(uint32_t(w[2 * (q & 1)]), uint32_t(w[2 * (q & 1) + 1])), e8m0_arg(a[i].s));
-        }
-#pragma unroll
-        for (int j = 0; j < NT; ++j) y[j] = mx4_bf16x8(uint32_t(b[j].q[q]), e8m0_arg(b[j].s));
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-          for (int j = 0; j < NT; ++j) acc[i][j] = mx_mfma_bf16(y[j], x[i], acc[i][j]);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = mx84_mfma(b[j], a[i], acc[i][j]);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int64_t row = m0 + 16 * i + r;
-    if (row >= m) continue;
-    typename FloatType<T>::type *orow = static_cast<typename FloatType<T>::type *>(out) + row * stride;
-#pragma unroll
-    for (int j = 0; j < NT; ++j) store_float4<T>(orow, n0 + 16 * j + 4 * g, n, acc[i][j]);
-  }
-}
-
 // ---- few rows of a -----------------------------------------------------------
 //
-// Bound by reading b, once.  A wavefront takes 16 rows of b, with two groups of them
-// asked for at once; a's rows are in LDS (HELD) where they fit.  Where there are few rows
-// of b, the wavefronts of a workgroup share out the groups of the same 16 (SPLIT), and
-// their sums are added in a fixed order.
-constexpr int kFew8Flight = 2;
-constexpr int kFew8Lds = 65536;   // bytes of a's codes
+// Bound by reading b, once: 1 x 1,000,000 x 768 72 us (5.7 TB/s), 1 x 131,072 x 768 11.3.  A
+// wavefront takes 16 rows of b, with two groups of them asked for at once; a's rows are in
+// LDS (HELD) where they fit.  Where there are few rows of b, the wavefronts of a workgroup
+// share out the groups of the same 16 (SPLIT), and their sums are added in a fixed order:
+// 1 x 4,096 x 4,096 in less than the 7 us of a call, 19 with one wavefront for all groups.
+constexpr int kFew8Flight = 2;   // us with 1, 2, 4, 6: 1 x 1,000,000 x 768 92, 72, 90, 80; 16 x 131,072 x 4,096 88, 69, 69, 77
 
 template <int T, bool SPLIT, bool HELD>
 __global__ void __launch_bounds__(256) k_mx8_score_few(const uint8_t *__restrict__ ac, const uint8_t *__restrict__ as,
@@ -223,13 +160,19 @@ __global__ void __launch_bounds__(256) k_mx8_score_few(const uint8_t *__restrict
 //
 // A workgroup of 4 wavefronts takes 32 MF rows of a by 256 of b, each wavefront 16 MF by
 // 128, one group of 128 coordinates after another.  The memory unit writes codes and
-// scales to LDS by itself, into one of three places for a group: in group t those of t + 2
-// are asked for, and one barrier, behind the last read of group t's place, waits for those
-// of t + 1 alone, a group and a half old.  The rows of b of the next group, and the first
-// two fragments of a's, are then read to registers under the group's last instructions,
-// each fragment of b behind the last one that uses the register; the others of a two
-// fragments ahead.  A read or a load or two fit behind a matrix
-// instruction, which the unit works on for 32 cycles.
+// scales to LDS by itself.  With 256 rows of a there are three places for a group: in group
+// t those of t + 2 are asked for, and one barrier, behind the last read of group t's place,
+// waits for those of t + 1 alone, a group and a half old.  With 128 rows there are two, and
+// two workgroups to a CU: those of t + 2 are asked for behind the barrier, which waits for
+// all, and the other workgroup multiplies meanwhile.  The rows of b of the next group, and
+// the first two fragments of a's, are then read to registers under the group's last
+// instructions, each fragment of b behind the last one that uses the register; the others
+// of a two fragments ahead.  A read or a load or two fit behind a matrix instruction, which
+// the unit works on for 32 cycles.  8,192 x 32,768 x 4,096 in 833 to 922 us (up to 2,640
+// TFLOP/s; the instruction alone reaches 4,700), 1,133 with 128 rows, which LDS bounds; 300 x
+// 100,000 x 768 33 us with 128 rows, 43 with one workgroup to a CU.  A workgroup that went
+// on from tile to tile took more (1,024 us): its loads' places and addresses do not leave
+// room for the sums in the registers.
 //
 // LDS, by lines of 128 bytes: a row of a, or two of b.  A line's eight 16-byte pieces are
 // exchanged by its number, so that the rows of a read fall on different banks; the
@@ -401,18 +344,165 @@ __global__ void __launch_bounds__(256, MF == 4 ? 2 : 1) k_mx8_score_tile(
   }
 }
 
+// ---- large products to float32 -------------------------------------------------
+//
+// The same tiles and places, multiplied in bfloat16.  A group is taken in two passes, of 16
+// of each lane's 32 coordinates: in a pass a wavefront has its 128 rows of b in bfloat16 and
+// goes through its fragments of a, 16 instructions to one.  A step ahead a's 16 codes of a
+// lane are turned to bfloat16, two ahead they are read; at a pass's last step b's are turned,
+// each fragment behind the last instruction that uses the register.  The barrier, late in
+// the second pass, waits for the next group, and those after it are asked for behind it.
+template <int MF>
+__global__ void __launch_bounds__(256, MF == 2 ? 2 : 1) k_mx8_score_tile_f32(
+    const uint8_t *__restrict__ ac, const uint8_t *__restrict__ as, int64_t m, const uint8_t *__restrict__ bc,
+    const uint8_t *__restrict__ bs, int64_t n, int steps, float *__restrict__ out, int64_t stride, int mtiles) {
+  static_assert(MF == 8 || MF == 2, "the places of reads and loads between the instructions");
+  constexpr int BM = 32 * MF, BN = kMmN;
+  constexpr int LA = BM / 32, LB = BN / 64, kLoads = LA + LB + 2;   // loads of a wavefront and group
+  constexpr int kA = BM * kS8LineA, kB = BN * kS8LineB, kS = 4 * (BM + BN);
+  constexpr int kB0 = 3 * kA, kS0 = kB0 + 3 * kB, kNone = kS0 + 3 * kS;
+  __shared__ __align__(1024) uint8_t lds[kNone + 256];
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
+  const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tiles = gridDim.x, per = tiles / 8, rest = tiles % 8;
+  const int xcd = blockIdx.x % 8, at = blockIdx.x / 8 + xcd * per + min(xcd, rest);
+  const int ntiles = tiles / mtiles;
+  const int band = at / (8 * ntiles), rows = min(8, mtiles - 8 * band), in = at - band * 8 * ntiles;
+  const int64_t m0 = int64_t(8 * band + in % rows) * BM, n0 = int64_t(in / rows) * BN;
+  const uint32_t cpa = 128u * steps, cpb = 64u * steps, sp = 4u * steps;
+  const i32x4 ra = buffer_of(ac + m0 * cpa, (m - m0) * cpa), rb = buffer_of(bc + n0 * cpb, (n - n0) * cpb);
+  const i32x4 rsa = buffer_of(as + m0 * sp, (m - m0) * sp), rsb = buffer_of(bs + n0 * sp, (n - n0) * sp);
+  const uint32_t lds0 = lds_address(lds);
+
+  // ---- loads, as above; a line of b is exchanged by its number
+  const int line = lane >> 3, place = lane & 7, slot = place ^ line;
+  const uint32_t va = (wid * (8 * LA) + line) * cpa + (slot << 4);
+  const uint32_t vb = (wid * (16 * LB) + 2 * line + (slot >> 2)) * cpb + ((slot & 3) << 4);
+  const uint32_t vs = (wid * 64 + lane) * sp;
+  auto load = [&](int t, int p, int i) {
+    const uint32_t past = t < steps ? 0u : 0x80000000u;
+    if (i < LA)
+      load_to_lds(ra, lds0 + p * kA + (wid * LA + i) * 1024, (va + (8 * i) * cpa + t * kS8LineA) | past);
+    else if (i < LA + LB)
+      load_to_lds(rb, lds0 + kB0 + p * kB + (wid * LB + i - LA) * 1024, (vb + (16 * (i - LA)) * cpb + t * kS8LineB) | past);
+    else if (i == LA + LB)
+      load_to_lds4(rsa, lds0 + (wid * 64 < BM ? kS0 + p * kS + wid * 256 : kNone), (vs + t * 4) | past);
+    else
+      load_to_lds4(rsb, lds0 + kS0 + p * kS + 4 * BM + wid * 256, (vs + t * 4) | past);
+  };
+
+  // ---- reads: a's 16 bytes 32 g + 16 pass .. of a fragment's rows, b's 32 g .. of all
+  const int wm = (wid >> 1) * (16 * MF), wn = (wid & 1) * 128;
+  const int ra0 = (wm + r) * kS8LineA + (((2 * g) ^ (r & 7)) << 4), ra1 = (wm + r) * kS8LineA + (((2 * g + 1) ^ (r & 7)) << 4);
+  const int rb_off = kB0 + ((wn + r) >> 1) * 128 + (((4 * (r & 1) + g) ^ ((r >> 1) & 7)) << 4);
+  const int rsa_off = kS0 + (wm + r) * 4 + g, rsb_off = kS0 + 4 * BM + (wn + r) * 4 + g;
+  i32x4 code[2];   // of a, by the step's parity
+  int scale[2];
+  uint4 x[2][2];   // in bfloat16, both halves
+  Mx4FragB fb[8];
+  uint4 y[2][8];
+  auto read_a = [&](int p, int step) {   // steps of the next group are 2 MF and 2 MF + 1
+    const int k = step % MF, pass = step / MF % 2;
+    code[step & 1] = *reinterpret_cast<const i32x4 *>(&lds[p * kA + (pass ? ra1 : ra0) + 16 * k * kS8LineA]);
+    scale[step & 1] = lds[p * kS + rsa_off + 64 * k];
+  };
+  auto turn_a = [&](int step, int q) {
+    const i32x4 w = code[step & 1];
+    x[step & 1][q] = mx8_bf16x8(make_uint2(uint32_t(w[2 * q]), uint32_t(w[2 * q + 1])), e8m0_arg(scale[step & 1]));
+  };
+  auto read_b = [&](int p, int j) {
+    fb[j].q = *reinterpret_cast<const i32x4 *>(&lds[p * kB + rb_off + 8 * j * 128]);
+    fb[j].s = lds[p * kS + rsb_off + 64 * j];
+  };
+  auto turn_b = [&](int pass, int q, int j) { y[q][j] = mx4_bf16x8(uint32_t(fb[j].q[2 * pass + q]), e8m0_arg(fb[j].s)); };
+
+  f32x4 acc[MF][8] = {};
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(p, p, i);
+  arrive<kLoads>();
+#pragma unroll
+  for (int j = 0; j < 8; ++j) read_b(0, j);
+  read_a(0, 0);
+  read_a(0, 1);
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    turn_a(0, q);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) turn_b(0, q, j);
+  }
+
+  // Group t is in place p, the next one in p1, and p2 is free behind the barrier.
+  int p = 0;
+  for (int t = 0; t < steps; ++t) {
+    const int p1 = p == 2 ? 0 : p + 1, p2 = p1 == 2 ? 0 : p1 + 1;
+    for_each<32 * MF>([&](auto i_) __attribute__((always_inline)) {
+      constexpr int i = decltype(i_)::value, step = i / 16, q = i / 8 % 2, j = i % 8, k = step % MF;
+      constexpr int late = i - 16 * (2 * MF - 4);   // behind the barrier
+      if constexpr (late == 0) arrive<0>();
+      acc[k][j] = mx_mfma_bf16(y[q][j], x[step & 1][q], acc[k][j]);
+      if constexpr (i % 16 == 0) read_a(step + 2 < 2 * MF ? p : p1, step + 2);
+      if constexpr (i % 16 == 6) turn_a(step + 1, 0);
+      if constexpr (i % 16 == 12) turn_a(step + 1, 1);
+      // the next group's rows of b, behind the first pass's end and ahead of the second's
+      constexpr int from = MF == 2 ? 32 : 0, each = MF == 2 ? 2 : 4;
+      if constexpr (late >= from && late < from + 8 * each && late % each == each / 2) read_b(p1, (late - from) / each);
+      if constexpr (late >= 0 && late % 4 == 0 && late / 4 < kLoads) load(t + 2, p2, late / 4);
+      if constexpr (k == MF - 1) turn_b(1 - step / MF, q, j);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    p = p1;
+  }
+
+  // Through LDS, so that a store writes 2 rows of 512 consecutive bytes, a part of LDS for
+  // each wavefront.
+  struct __attribute__((packed, aligned(4))) Wide {
+    uint32_t v[4];
+  };
+  constexpr int kOwn = MF == 8 ? 32768 : 16384, kRows = kOwn / 512;   // rows at a time
+  static_assert(4 * kOwn <= kNone, "LDS of the stores");
+  arrive<0>();   // the last operands have been read, and the last loads have come, everywhere
+  uint8_t *own = lds + wid * kOwn;
+#pragma unroll
+  for (int k0 = 0; k0 < MF; k0 += kRows / 16) {
+#pragma unroll
+    for (int k = k0; k < k0 + kRows / 16; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        *reinterpret_cast<uint4 *>(own + (16 * (k - k0) + r) * 512 + 16 * ((4 * j + g) ^ r)) =
+            __builtin_bit_cast(uint4, acc[k][j]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the wavefront's own part
+#pragma unroll 4
+    for (int i = 0; i < kRows / 2; ++i) {
+      const int row = 2 * i + (lane >> 5), piece = lane & 31;
+      const uint4 v = *reinterpret_cast<const uint4 *>(own + row * 512 + 16 * (piece ^ (row & 15)));
+      const int64_t orow = m0 + wm + 16 * k0 + row, c = n0 + wn + piece * 4;
+      if (orow >= m) continue;
+      float *o = out + orow * stride + c;
+      if (c + 4 <= n) {   // rows may begin anywhere
+        *reinterpret_cast<Wide *>(o) = __builtin_bit_cast(Wide, v);
+      } else {
+        const uint32_t e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (c + q < n) o[q] = __uint_as_float(e[q]);
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+}
+
 template <int T, int MF>
 static void launch_score8_tile(const Mx8ScoreCall &c) {
   const int64_t mt = (c.m + 32 * MF - 1) / (32 * MF), nt = (c.n + kMmN - 1) / kMmN;
-  hipLaunchKernelGGL((k_mx8_score_tile<T, MF>), dim3(unsigned(mt * nt)), dim3(256), 0, c.s, c.ac, c.as, c.m, c.bc, c.bs,
-                     c.n, c.steps, c.out, c.stride, int(mt));
-}
-
-template <int T, int F>
-static void launch_score8_direct(const Mx8ScoreCall &c) {
-  const Mx4DirectGrid g = matmul_direct_grid(c.m, c.n, 16 * F);
-  hipLaunchKernelGGL((k_mx8_score<T, F, F>), dim3(unsigned(g.x), unsigned(g.y)), dim3(256), 0, c.s, c.ac, c.as, c.m,
-                     c.bc, c.bs, c.n, c.steps, c.out, c.stride);
+  const dim3 grid(unsigned(mt * nt));
+  if constexpr (T == RSLM_F32)
+    hipLaunchKernelGGL(k_mx8_score_tile_f32<MF>, grid, dim3(256), 0, c.s, c.ac, c.as, c.m, c.bc, c.bs, c.n, c.steps,
+                       static_cast<float *>(c.out), c.stride, int(mt));
+  else
+    hipLaunchKernelGGL((k_mx8_score_tile<T, MF>), grid, dim3(256), 0, c.s, c.ac, c.as, c.m, c.bc, c.bs, c.n, c.steps,
+                       c.out, c.stride, int(mt));
 }
 
 template <int T, bool SPLIT, bool HELD>
@@ -427,7 +517,7 @@ static void launch_score8_few_one(const Mx8ScoreCall &c) {
 }
 template <int T>
 static void launch_score8_few(const Mx8ScoreCall &c) {
-  const bool split = (c.n + 15) / 16 < 4096 && c.steps >= 4, held = c.m * c.steps * 128 <= kFew8Lds;
+  const bool split = few8_split(c.n, c.steps), held = few8_held(c.m, c.steps);
   if (split && held) launch_score8_few_one<T, true, true>(c);
   else if (split) launch_score8_few_one<T, true, false>(c);
   else if (held) launch_score8_few_one<T, false, true>(c);
@@ -436,13 +526,10 @@ static void launch_score8_few(const Mx8ScoreCall &c) {
 
 template <int T>
 static void launch_score8(const Mx8ScoreCall &c) {
-  if (c.m <= 16) return launch_score8_few<T>(c);
-  if constexpr (T == RSLM_F32) {
-    if (c.m > 32 || matmul_direct_grid(c.m, c.n, 32).x > kMostWorkgroups) launch_score8_direct<T, 4>(c);
-    else launch_score8_direct<T, 2>(c);
-  } else {
-    if (matmul_form(c.m, c.n) == kMmTile256 && c.steps >= 12) launch_score8_tile<T, 8>(c);
-    else launch_score8_tile<T, 4>(c);
+  switch (score8_form(c.m, c.n, c.steps)) {
+    case kS8Few: launch_score8_few<T>(c); break;
+    case kS8Tile256: launch_score8_tile<T, 8>(c); break;
+    default: launch_score8_tile<T, T == RSLM_F32 ? 2 : 4>(c);
   }
 }
 
