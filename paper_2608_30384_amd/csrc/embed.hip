@@ -80,8 +80,9 @@ __global__ void __launch_bounds__(256) k_embed(EmbedArgs a) {
 
 // ---- the sort
 //
-// Of 65,536 entries 4 kernels of a few us each, bound by their chains of reads, barriers
-// and votes; the table is filled with zeros beside them, by workgroups of their own.
+// Of 65,536 entries two passes, each a kernel of 5 us that counts and one of 11 that moves,
+// bound by their chains of reads, barriers and votes; beside the latter the table is filled
+// with zeros, by workgroups of their own.  Up to 2,048 entries take one kernel.
 
 // A token of the sort: its id (the number of rows: none) and its place.
 typedef uint2 Entry;   // x: id, y: place
@@ -137,7 +138,6 @@ __device__ __forceinline__ Entry sort_entry(const SortArgs &a, int64_t i) { retu
 
 // How many entries of a workgroup's run have each digit.
 __global__ void __launch_bounds__(kSortThreads) k_sort_count(SortArgs a) {
-  if (int(blockIdx.x) >= a.tiles) return fill_rows(a.fill);
   __shared__ uint32_t bins[kSortMaxBins];
   const int nb = 1 << a.bits;
   for (int b = threadIdx.x; b < nb; b += kSortThreads) bins[b] = 0u;
@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_move(SortArgs a) {
   uint32_t total[2] = {}, before[2] = {};
   if (tid * each < nb) {
     const uint32_t *c = a.counts + tid * each;
-    constexpr int U = 16;   // tiles' counts asked for at once
+    constexpr int U = 32;   // tiles' counts asked for at once
     for (int t0 = 0; t0 < a.tiles; t0 += U) {
       uint32_t v[U][2];
 #pragma unroll
@@ -345,8 +345,8 @@ constexpr int kSumFlight = 4;   // rows asked for at once, twice
 
 // A lane's 8 columns of a row: those from `at` on, of which the first `skip` are another
 // lane's.  So a row's last columns too are read and written 8 at a time, and no branch
-// keeps a wavefront's loads apart (of 65,536 x 768 bfloat16, with a branch for the last
-// columns 72 us; so and twice as many chunks ?).  Rows of less than 8: WIDE false.
+// keeps a wavefront's loads apart (65,536 x 768 bfloat16 33 us, 3.0 TB/s of dout alone; 72
+// with a branch for the last columns).  Rows of less than 8: WIDE false.
 struct SumLane {
   int at, skip;
 };
@@ -459,9 +459,10 @@ __global__ void __launch_bounds__(256) k_embed_sum(EmbedSumArgs a) {
 
 // Runs over several chunks: the tail of the one that they begin in, and the heads after
 // it, every fourth of them to a wavefront.
+constexpr int kJoinWaves = 4;
 template <int TO, bool WIDE>
-__global__ void __launch_bounds__(256) k_embed_join(EmbedSumArgs a) {
-  __shared__ float sums[3][kSumCols];
+__global__ void __launch_bounds__(64 * kJoinWaves) k_embed_join(EmbedSumArgs a) {
+  __shared__ float sums[kJoinWaves - 1][kSumCols];
   __shared__ int ends;
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
   const int64_t chunk = blockIdx.x, e0 = chunk * a.chunk, e1 = e0 + a.chunk;
@@ -470,15 +471,15 @@ __global__ void __launch_bounds__(256) k_embed_join(EmbedSumArgs a) {
   if (id == a.rows || behind != id || ahead == id) return;   // ends here, or began before
   // the last head: that of the first chunk whose end is not the run's
   int64_t last = chunk + 1;
-  for (;; last += 256) {
-    if (tid == 0) ends = 256;
+  for (;; last += 64 * kJoinWaves) {
+    if (tid == 0) ends = 64 * kJoinWaves;
     __syncthreads();
     const int64_t end = (last + tid + 1) * a.chunk;
     if (end >= a.n || a.sorted[end].x != id) atomicMin(&ends, tid);
     __syncthreads();
     const int first = ends;
     __syncthreads();
-    if (first < 256) {
+    if (first < 64 * kJoinWaves) {
       last += first;
       break;
     }
@@ -492,16 +493,16 @@ __global__ void __launch_bounds__(256) k_embed_join(EmbedSumArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] = v.v[i];
   }
-  constexpr int U = 4;
-  for (int64_t j = chunk + 1 + wid; j <= last; j += 4 * U) {
+  constexpr int U = 4;   // heads asked for at once
+  for (int64_t j = chunk + 1 + wid; j <= last; j += kJoinWaves * U) {
     Raw8<RSLM_F32> v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      sum_load<RSLM_F32, WIDE>(v[u], a.head + min(j + 4 * u, last) * a.dim, l, a.dim);
+      sum_load<RSLM_F32, WIDE>(v[u], a.head + min(j + kJoinWaves * u, last) * a.dim, l, a.dim);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[i] += j + 4 * u <= last ? v[u].v[i] : 0.f;
+      for (int i = 0; i < 8; ++i) acc[i] += j + kJoinWaves * u <= last ? v[u].v[i] : 0.f;
   }
   if (wid > 0) {
 #pragma unroll
@@ -510,7 +511,7 @@ __global__ void __launch_bounds__(256) k_embed_join(EmbedSumArgs a) {
   __syncthreads();
   if (wid > 0) return;
 #pragma unroll
-  for (int w = 0; w < 3; ++w)
+  for (int w = 0; w < kJoinWaves - 1; ++w)
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i] += sums[w][8 * lane + i];
   put_row<TO, WIDE>(a, id, l, acc);
@@ -535,10 +536,10 @@ static EmbedPlan embed_plan(int64_t n, int64_t rows, int dim) {
   const int64_t rounds = (n + kSortRound - 1) / kSortRound;
   p.per = (rounds + kSortMaxTiles - 1) / kSortMaxTiles * kSortRound;
   p.tiles = p.per ? int((n + p.per - 1) / p.per) : 0;
-  // 16 wavefronts to a CU, chunks of 8 to 512 entries
+  // 8 wavefronts to a CU, chunks of 8 to 512 entries
   const int64_t cols = (dim + kSumCols - 1) / kSumCols;
   p.chunk = 8;
-  while (p.chunk < 512 && (n + p.chunk - 1) / p.chunk * cols > 4096) p.chunk *= 2;
+  while (p.chunk < 512 && (n + p.chunk - 1) / p.chunk * cols > 2048) p.chunk *= 2;
   p.chunks = (n + p.chunk - 1) / p.chunk;
   p.entries = rounded(size_t(n) * sizeof(Entry));
   p.counts = rounded(size_t(p.tiles) * (size_t(1) << p.bits) * 4);
@@ -553,7 +554,8 @@ static void launch_sums_one(const EmbedSumArgs &a, hipStream_t s) {
   hipLaunchKernelGGL((k_embed_sum<T, TO, WIDE>), grid, dim3(256), 0, s, a);
   // the last chunk has none after it
   if (a.chunks > 1)
-    hipLaunchKernelGGL((k_embed_join<TO, WIDE>), dim3(unsigned(a.chunks - 1), grid.y), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_embed_join<TO, WIDE>), dim3(unsigned(a.chunks - 1), grid.y),
+                       dim3(64 * kJoinWaves), 0, s, a);
 }
 template <int T, int TO>
 static void launch_sums(const EmbedSumArgs &a, hipStream_t s) {
@@ -590,10 +592,11 @@ static int embed_call(EmbedArgs a, int stype, int out_dtype, void *stream) {
   return check_launch();
 }
 
-// Workgroups that fill rows with zeros, 8 values a thread.
+// Workgroups that fill rows with zeros, 8 values a thread: with more of them the sort's
+// reads beside wait longer (65,536 x 768 with the lookup: 138 us, 144 with 2,048, 146 with 256).
 static unsigned fill_groups(int64_t rows, int dim) {
   const int64_t wg = (rows * ((dim + 7) / 8) + 255) / 256;
-  return unsigned(wg < 2048 ? wg : 2048);
+  return unsigned(wg < 512 ? wg : 512);
 }
 
 static bool ids_ok(const void *ids, int id_bytes) { return ids && aligned_to(ids, id_bytes); }
@@ -661,8 +664,8 @@ int rslm_embed_backward(const void *dout, int32_t dtype, int64_t n, int32_t dim,
   Entry *in = reinterpret_cast<Entry *>(w), *out = reinterpret_cast<Entry *>(w + p.entries);
   SortArgs a{ids, id_bytes == 8, rows, in, out, n, p.per, 0, p.bits, p.tiles,
              reinterpret_cast<uint32_t *>(w + 2 * p.entries)};
-  // a part of the table's rows is filled beside each kernel of the sort
-  const int64_t parts = p.tiles == 1 ? 1 : 2 * p.passes;
+  // a part of the table's rows is filled beside each pass's longer kernel
+  const int64_t parts = p.tiles == 1 ? 1 : p.passes;
   int64_t part = 0;
   auto grid = [&] {
     const int64_t row0 = rows * part / parts, row1 = rows * (part + 1) / parts;
@@ -676,8 +679,7 @@ int rslm_embed_backward(const void *dout, int32_t dtype, int64_t n, int32_t dim,
     a.in = a.out;
   } else {
     for (int pass = 0; pass < p.passes; ++pass) {
-      const dim3 g0 = grid();
-      hipLaunchKernelGGL(k_sort_count, g0, dim3(kSortThreads), 0, s, a);
+      hipLaunchKernelGGL(k_sort_count, dim3(unsigned(p.tiles)), dim3(kSortThreads), 0, s, a);
       const dim3 g1 = grid();
       hipLaunchKernelGGL(k_sort_move, g1, dim3(kSortThreads), 0, s, a);
       a.ids = nullptr;
