@@ -210,18 +210,29 @@ struct Settled {
   int accepted, count;
   VfSum p, q;
 };
+// A drafted token and its score, by the lane of the first wavefront that has it.
+struct Drafted {
+  int64_t x;
+  float score;
+};
+
+// Log probability of an entry.
+__device__ __forceinline__ float log_of(float v, const VfSum &p, double scale) {
+  return float((double(v) - p.top) * (scale * (kLn2d / 256)) - log(p.z));
+}
 
 // By all threads of a workgroup: a wavefront joins a row's slices.
 template <int T>
-__device__ __forceinline__ void settle(const VerifyArgs &a, int b, const double *table, VfSum (*rows)[kVfMaxDrafts + 1],
-                                       Settled &out) {
+__device__ __forceinline__ Drafted settle(const VerifyArgs &a, int b, const double *table,
+                                          VfSum (*rows)[kVfMaxDrafts + 1], Settled &out) {
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
   const int count = vf_count(a, b);
   // asked for first: two reads, one after the other
   bool inside = false;
+  int64_t x = -1;
   float px = 0.f, qx = 0.f, u = 0.f;
   if (wid == 0 && lane < count) {
-    const int64_t x = a.tokens[int64_t(b) * a.k + lane];
+    x = a.tokens[int64_t(b) * a.k + lane];
     u = a.uniforms[int64_t(b) * (a.k + 1) + lane];
     inside = x >= 0 && x < a.n;
     if (inside) {
@@ -256,6 +267,7 @@ __device__ __forceinline__ void settle(const VerifyArgs &a, int b, const double 
     }
   }
   __syncthreads();
+  return Drafted{x, px};
 }
 
 // The weight r of an entry: p, or where a draft fell what p has over q.
@@ -335,11 +347,24 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_draw(VerifyArgs a) {
   __shared__ double waves[kVfWaves];
   __shared__ double want_s, base_s;
   __shared__ int slice_s, drafted_s, found_s, last_s;
+  __shared__ float score_s;
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, b = blockIdx.x;
+  const float u = a.uniforms[int64_t(b) * (a.k + 1) + a.k];
   fill_table(table);
   __syncthreads();
-  settle<T>(a, b, table, rows, st);
+  const Drafted drafts = settle<T>(a, b, table, rows, st);
   const int n = st.accepted;
+  // all but the drawn token
+  if (wid == 1) {
+    for (int i = lane; i <= a.k; i += 64)
+      if (i > n) {
+        a.out[int64_t(b) * (a.k + 1) + i] = -1;
+        if (a.logprob) a.logprob[int64_t(b) * (a.k + 1) + i] = 0.f;
+      }
+  } else if (wid == 0 && lane < n) {
+    a.out[int64_t(b) * (a.k + 1) + lane] = drafts.x;
+    if (a.logprob) a.logprob[int64_t(b) * (a.k + 1) + lane] = log_of(drafts.score, rows[0][lane], a.tscale);
+  }
   if (tid == 0) found_s = 0x7fffffff, last_s = -1;
   if (wid == 0) {
     constexpr int each = kVfMaxSlices / 64;   // neighbouring slices of a lane
@@ -366,7 +391,7 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_draw(VerifyArgs a) {
 #pragma unroll
     for (int i = 0; i < each; ++i) mine += r[i];
     const double upto = wave_upto64(mine), total = __shfl(upto, 63, 64);
-    const double want = double(fminf(fmaxf(a.uniforms[int64_t(b) * (a.k + 1) + a.k], 0.f), 0x1.fffffep-1f)) * total;
+    const double want = double(fminf(fmaxf(u, 0.f), 0x1.fffffep-1f)) * total;
     // the first lane past `want`, or the last one with any, should rounding pass them all
     const uint64_t past = __ballot(upto > want && mine > 0), any = __ballot(mine > 0);
     const int in = past ? __ffsll(static_cast<unsigned long long>(past)) - 1 : 63 - __clzll(static_cast<long long>(any));
@@ -420,26 +445,21 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_draw(VerifyArgs a) {
       if (found != 0x7fffffff) atomicMin(&found_s, found);
       if (last >= 0) atomicMax(&last_s, last);
       __syncthreads();
+      // the token so far, and its score
+      token = found_s != 0x7fffffff ? found_s : last_s;
+#pragma unroll
+      for (int q = 0; q < E; ++q)
+        if (at + q == token) score_s = v[q];
       if (found_s != 0x7fffffff) break;
       for (int k = 0; k < kVfWaves; ++k) base += waves[k];
       __syncthreads();
     }
-    token = found_s != 0x7fffffff ? found_s : last_s;
+    __syncthreads();
   }
-  for (int i = tid; i <= a.k; i += kVfThreads) {
-    const int64_t o = int64_t(b) * (a.k + 1) + i;
-    const int64_t t = i < n ? a.tokens[int64_t(b) * a.k + i] : i == n ? int64_t(token) : -1;
-    a.out[o] = t;
-    if (a.logprob) {
-      double lp = 0;
-      if (t >= 0) {
-        const VfSum p = rows[0][i];
-        lp = (double(float(target_row<T>(a, b, i)[t])) - p.top) * (a.tscale * (kLn2d / 256)) - log(p.z);
-      }
-      a.logprob[o] = float(lp);
-    }
-  }
-  if (tid == 0) a.accepted[b] = n;
+  if (tid) return;
+  a.out[int64_t(b) * (a.k + 1) + n] = token;
+  if (a.logprob) a.logprob[int64_t(b) * (a.k + 1) + n] = token < 0 ? 0.f : log_of(score_s, st.p, a.tscale);
+  a.accepted[b] = n;
 }
 
 static int64_t verify_rows(int64_t b, int k, bool draft) { return b * (k + 1 + (draft ? k : 0)); }
