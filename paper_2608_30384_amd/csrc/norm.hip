@@ -6,6 +6,10 @@
 //
 // Bound by memory: x and the residual are read, h and y (or 1.03 bytes a coordinate of
 // codes and scales) are written, once each; backward h, dy and dh are read and dx written.
+// us, 8,192 x 4,096 bfloat16: forward 55 (4.9 TB/s), backward with the weight's gradient 46
+// (5.8 TB/s, some of it from the last-level cache) and 5; 20,001 x 2,049 float32 to 8 bits
+// 120 (4.5 TB/s).  Reading rows twice, and the weight's gradient by a kernel of its own,
+// took 82, 162 and 143.
 #include "mx4_dev.h"
 #include "rows_dev.h"
 
@@ -208,8 +212,10 @@ __global__ void __launch_bounds__(kNormThreads) k_norm(NormArgs a) {
   }
 }
 
-// A row of any length to a workgroup, which reads it twice (h, written in between,
-// the second time; from the cache).
+// ---- rows too long for that, or of less than 8 coordinates
+//
+// A row to a workgroup, which reads it twice (h, written in between, the second time; from
+// the cache).
 template <int T>
 __global__ void __launch_bounds__(kNormThreads) k_norm_long(NormArgs a) {
   __shared__ float sums[2][kNormThreads / 64];
@@ -463,10 +469,11 @@ static void launch_norm_backward(const NormBackArgs &b, void *dweight, int dwtyp
     a.per = (a.n + strips - 1) / strips;
     if (a.dim < 8 || a.dim > kNormBackHeld) {
       const dim3 grid(unsigned(a.n < 65536 ? a.n : 65536));
-      if (a.dx) hipLaunchKernelGGL(k_norm_backward_long<T>, grid, dim3(kNormThreads), 0, s, a);
+      // the weight's gradient first: dx may be dy or h
       if (dweight)
         hipLaunchKernelGGL(k_norm_dweight<T>, dim3(unsigned((a.dim + 2047) / 2048), unsigned(strips)),
                            dim3(kNormThreads), 0, s, a);
+      if (a.dx) hipLaunchKernelGGL(k_norm_backward_long<T>, grid, dim3(kNormThreads), 0, s, a);
     } else {
       if (!dweight) a.partial = nullptr;
 #define RSLM_NORM(LANES, NV)                                                                       \

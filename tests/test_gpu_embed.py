@@ -162,6 +162,14 @@ def test_gradient_of_nothing(R):
     assert R.rslm_embed_backward(torch.ones((3, 12), device="cuda"), torch.zeros((3,), dtype=torch.int64, device="cuda"), 0).shape == (0, 12)
 
 
+def test_gradient_of_rows_that_are_one(R):
+    """dout of one row for all tokens, as the gradient of a sum over them is."""
+    ids = torch.tensor([3, 1, 3, 3, -1, 0] * 500, device="cuda")
+    one = torch.arange(40, device="cuda", dtype=torch.float32)
+    got = R.rslm_embed_backward(one.expand(3000, 40), ids, 5)
+    assert torch.equal(got, torch.stack([500 * one, 500 * one, 0 * one, 1500 * one, 0 * one]))
+
+
 def test_other_stream(R):
     table, ids = torch.randn((300, 96), device="cuda"), torch.randint(-1, 300, (5000,), device="cuda")
     want = R.rslm_embed(table, ids)

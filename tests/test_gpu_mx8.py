@@ -130,10 +130,14 @@ def sides(m, n, dim, seed, spread=3):
 
 
 def product(a, b, dim):
-    """The product in float64, the sum of the terms' magnitudes, and of the largest of each eight."""
+    """The product in float64, the sum of the terms' magnitudes, and of the largest of each eight
+    (of large products that sum again, which is more)."""
     x, y = mx8.values(*a, dim), mx4.values(*b, dim)
     pad = -dim % 8
     xs, ys = np.pad(np.abs(x), ((0, 0), (0, pad))), np.pad(np.abs(y), ((0, 0), (0, pad)))
+    if x.shape[0] * y.shape[0] * dim > 1 << 28:
+        terms = np.abs(x) @ np.abs(y).T
+        return x @ y.T, terms, terms
     top = np.zeros((x.shape[0], y.shape[0]))
     for o in range(0, dim, 8):
         top += (xs[:, None, o:o + 8] * ys[None, :, o:o + 8]).max(-1)
@@ -154,7 +158,8 @@ def check_product(got, want, terms, top, dim, dt):
 @pytest.mark.parametrize("m,n,dim", [
     (1, 1, 1), (1, 3, 31), (2, 17, 32), (3, 16, 33), (1, 300, 96), (15, 64, 100), (16, 255, 128), (17, 257, 129),
     (5, 1000, 768), (32, 65, 200), (33, 70, 300), (64, 129, 256), (65, 300, 129), (100, 513, 260), (128, 256, 384),
-    (130, 1030, 500), (257, 700, 96), (300, 2049, 640), (1, 5000, 2049), (9, 33, 4096)])
+    (130, 1030, 500), (257, 700, 96), (300, 2049, 640), (1, 5000, 2049), (9, 33, 4096), (16, 100, 4096),
+    (16, 70000, 200), (15, 50, 4200), (70, 300, 2000), (260, 70001, 1500), (250, 66001, 1541), (1000, 17000, 1536)])
 def test_score(R, dt, m, n, dim):
     a, b = sides(m, n, dim, m + 7 * n + dim, spread=1 if dt == "f16" else 3)
     if dt == "f16":

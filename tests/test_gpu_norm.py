@@ -127,7 +127,7 @@ def test_many_rows(R, n, dim):
     assert torch.equal(dx, again[0]) and torch.equal(dw, again[1])
 
 
-@pytest.mark.parametrize("dim", [40, 768, 4096, 16392])
+@pytest.mark.parametrize("dim", [5, 40, 768, 4096, 8200, 16392])
 def test_in_place(R, dim):
     g = torch.Generator().manual_seed(dim)
     x, residual = wide(g, 6, dim, 0, "bf16"), wide(g, 6, dim, 0, "bf16")
@@ -137,11 +137,14 @@ def test_in_place(R, dim):
         got = R.rslm_rmsnorm(both[0], residual=both[1], rows=True, h=both[into])
         assert got.h is both[into] and torch.equal(got.h, want.h) and torch.equal(got.y, want.y)
         assert torch.equal(got.rows.codes, want.rows.codes) and torch.equal(got.rstd, want.rstd)
-    dy = wide(g, 6, dim, 0, "bf16")
-    dx, _ = R.rslm_rmsnorm_backward(dy, want, dh=x)
-    for into in range(2):
-        both = [dy.clone(), x.clone()]
-        assert torch.equal(R.rslm_rmsnorm_backward(both[0], want, dh=both[1], out=both[into])[0], dx)
+    # the gradient into dy, dh or h, whose other readers (the weight's gradient) come first
+    dy, weight = wide(g, 6, dim, 0, "bf16"), torch.rand((dim,), generator=g).cuda()
+    dx, dw = R.rslm_rmsnorm_backward(dy, want, weight, dh=x)
+    for into in range(3):
+        all3 = [dy.clone(), x.clone(), want.h.clone()]
+        again = type(want)(all3[2], None, None, want.rstd)
+        got = R.rslm_rmsnorm_backward(all3[0], again, weight, dh=all3[1], out=all3[into])
+        assert got[0] is all3[into] and torch.equal(got[0], dx) and torch.equal(got[1], dw)
 
 
 def test_rows_of_zeros_and_of_no_numbers(R):
