@@ -6,13 +6,14 @@
 //
 // All of it is in float64: at 131,072 entries an error of 1e-7 in the sums would draw
 // another token once in some hundred.  An exponential is then a table of 256 entries, a
-// polynomial of degree 3 and a scaling, some 18 instructions, which bound the first kernel
+// polynomial of degree 3 and a scaling, some 16 instructions, which bound the first kernel
 // where there are many rows.
 //
 // Three kernels.  The first sums the exponentials of every row, a slice of 1,024 entries
-// (more where a row has over 262,144) to a wavefront.  The second settles which drafts
-// stand, each workgroup for itself, and where one falls sums r over the slices.  The third
-// settles the same and draws: the slice, then the token.
+// (more where a row has over 262,144) at a time to a wavefront.  The second settles which
+// drafts stand, each workgroup for itself, and where one falls sums r over the slices.  The
+// third draws: the slice, then the token.  64 sequences of 4 drafts by 131,072 bfloat16
+// scores: 40, 16 and 10 us; one, of float32: 4.7, 5.4 and 8.3, chains of dependent reads.
 #include "mx4_dev.h"
 
 namespace rslm {
@@ -48,6 +49,13 @@ struct VfSum {
   double z, top;
 };
 
+// What a sequence's drafts come to: how many stand, and of the rows that the next token is
+// drawn from their sums.
+struct Settled {
+  int accepted, count;
+  VfSum p, q;
+};
+
 struct VerifyArgs {
   const void *target, *draft;
   int64_t tseq, trow, dseq, drow;   // strides, in elements
@@ -62,24 +70,30 @@ struct VerifyArgs {
   int oeach, ogroups;               // and of a sequence in the second
   VfSum *tsums, *dsums;             // b x (k + 1) x slices, b x k x slices
   double *rsums;                    // b x slices
+  Settled *settled;                 // b
   int64_t *out;
   int32_t *accepted;
   float *logprob;
 };
 
-// 2^(y / 256), y <= 0.  y = i + f with |f| <= 1/2: the table has 2^((i mod 256) / 256), and
-// 2^(f / 256) is its Taylor polynomial of degree 3, off by 1.4e-13 of itself.  0 for -infinity
-// (and NaN).
-__device__ __forceinline__ double exp256(double y, const double *table) {
+// 2^(y / 256), y <= 0, as a product.  y = i + f with |f| <= 1/2: the table has
+// 2^((i mod 256) / 256), and 2^(f / 256) is its Taylor polynomial of degree 3, off by 1.4e-13
+// of itself.  0 for -infinity (and NaN).
+struct Factors {
+  double e, q;
+};
+__device__ __forceinline__ Factors factors256(double y, const double *table) {
   constexpr double l = kLn2d / 256;
   constexpr double big = 6755399441055744.0;   // 1.5 2^52: adding it rounds to a whole number
   y = fmax(y, -320000.0);                      // 2^-1250: zero
   const double t = y + big;
   const double f = y - (t - big);
   const int i = int(uint32_t(__builtin_bit_cast(uint64_t, t)));
-  const double p = fma(f, fma(f, l * l * l / 6, l * l / 2), l);
-  const double e = table[i & 255];
-  return ldexp(fma(e, f * p, e), i >> 8);
+  return Factors{ldexp(table[i & 255], i >> 8), fma(f, fma(f, fma(f, l * l * l / 6, l * l / 2), l), 1.0)};
+}
+__device__ __forceinline__ double exp256(double y, const double *table) {
+  const Factors p = factors256(y, table);
+  return p.e * p.q;
 }
 __device__ __forceinline__ double weight64(float v, double top, double scale, const double *table) {
   return exp256((double(v) - top) * scale, table);
@@ -87,10 +101,33 @@ __device__ __forceinline__ double weight64(float v, double top, double scale, co
 // Without a barrier: that is the caller's.
 __device__ __forceinline__ void fill_table(double *table) { table[threadIdx.x] = kVfTable.v[threadIdx.x]; }
 
+// v of the lane R behind, round each 16 lanes.
+template <int R>
+__device__ __forceinline__ float row_turn(float v) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x120 + R, 0xf, 0xf, true));   // row_ror
+}
+template <int R>
+__device__ __forceinline__ double row_turn(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __builtin_amdgcn_mov_dpp(int(uint32_t(u)), 0x120 + R, 0xf, 0xf, true);
+  const uint32_t hi = __builtin_amdgcn_mov_dpp(int(uint32_t(u >> 32)), 0x120 + R, 0xf, 0xf, true);
+  return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
 __device__ __forceinline__ double wave_sum64(double v) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
-  return v;
+  v += row_turn<8>(v);
+  v += row_turn<4>(v);
+  v += row_turn<2>(v);
+  v += row_turn<1>(v);
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
+}
+__device__ __forceinline__ float wave_max32(float v) {
+  v = fmaxf(v, row_turn<8>(v));
+  v = fmaxf(v, row_turn<4>(v));
+  v = fmaxf(v, row_turn<2>(v));
+  v = fmaxf(v, row_turn<1>(v));
+  v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
 }
 __device__ __forceinline__ double wave_max64(double v) {
 #pragma unroll
@@ -163,7 +200,10 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_sums(VerifyArgs a) {
   for (int t = 0; t < mine * a.blocks; ++t) {
     float v[kVfEach];
 #pragma unroll
-    for (int q = 0; q < kVfEach; ++q) v[q] = float(next.v[q / 8].v[q % 8]);
+    for (int q = 0; q < kVfEach; ++q) {
+      v[q] = float(next.v[q / 8].v[q % 8]);
+      asm("" : "+v"(v[q]));   // else the maxima are rounded to 16 bits one by one
+    }
     if (t + 1 < mine * a.blocks) load_block<T>(next, x, place(t + 1), a.n);
     float m = v[0];
 #pragma unroll
@@ -171,11 +211,18 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_sums(VerifyArgs a) {
       bad |= !(v[q] < __builtin_inff());
       m = fmaxf(m, v[q]);
     }
-    const double top = fmax(s.top, double(wave_max(m)));
+    const double top = fmax(s.top, double(wave_max32(m)));
     if (a.blocks > 1) s.z *= exp256((s.top - top) * scale, table);
     s.top = top;
 #pragma unroll
-    for (int q = 0; q < kVfEach; ++q) s.z += weight64(v[q], top, scale, table);
+    for (int q = 0; q < kVfEach; ++q) {
+      const Factors p = factors256((double(v[q]) - top) * scale, table);
+      s.z = fma(p.e, p.q, s.z);
+      if (q % 2 == 1) {   // two at a time: all at once take 138 registers and not 91, 54 us and not 45
+        asm volatile("" : "+v"(s.z));
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
     if (a.blocks == 1 || t % a.blocks == a.blocks - 1) {
       s.z = __ballot(bad) ? __builtin_nan("") : wave_sum64(s.z);
       if (lane == 0) (draft ? a.dsums : a.tsums)[at * a.slices + s0 + kVfWaves * (t / a.blocks)] = s;
@@ -204,12 +251,6 @@ __device__ __forceinline__ VfSum join_slices(const VfSum *sums, int slices, doub
   return VfSum{wave_sum64(z), top};
 }
 
-// What a sequence's drafts come to: how many stand, and of the rows that the next token is
-// drawn from their sums.
-struct Settled {
-  int accepted, count;
-  VfSum p, q;
-};
 // A drafted token and its score, by the lane of the first wavefront that has it.
 struct Drafted {
   int64_t x;
@@ -306,7 +347,22 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_over(VerifyArgs a) {
   const int b = int(blockIdx.x) / a.ogroups;
   fill_table(table);
   __syncthreads();
-  settle<T>(a, b, table, rows, st);
+  const Drafted drafts = settle<T>(a, b, table, rows, st);
+  // all but the drawn token, by the first workgroup
+  if (int(blockIdx.x) % a.ogroups == 0) {
+    const int n = st.accepted, i = threadIdx.x;
+    if (i < n) {
+      a.out[int64_t(b) * (a.k + 1) + i] = drafts.x;
+      if (a.logprob) a.logprob[int64_t(b) * (a.k + 1) + i] = log_of(drafts.score, rows[0][i], a.tscale);
+    } else if (i > n && i <= a.k) {
+      a.out[int64_t(b) * (a.k + 1) + i] = -1;
+      if (a.logprob) a.logprob[int64_t(b) * (a.k + 1) + i] = 0.f;
+    }
+    if (i == 0) {
+      a.settled[b] = st;
+      a.accepted[b] = n;
+    }
+  }
   if (st.accepted == st.count) return;
   const Over over = over_of(a, b, st, true);
   const auto *x = target_row<T>(a, b, st.accepted);
@@ -350,21 +406,11 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_draw(VerifyArgs a) {
   __shared__ float score_s;
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, b = blockIdx.x;
   const float u = a.uniforms[int64_t(b) * (a.k + 1) + a.k];
+  if (a.k > 0 && tid == 0) st = a.settled[b];
   fill_table(table);
   __syncthreads();
-  const Drafted drafts = settle<T>(a, b, table, rows, st);
+  if (a.k == 0) settle<T>(a, b, table, rows, st);   // no kernel before this one has
   const int n = st.accepted;
-  // all but the drawn token
-  if (wid == 1) {
-    for (int i = lane; i <= a.k; i += 64)
-      if (i > n) {
-        a.out[int64_t(b) * (a.k + 1) + i] = -1;
-        if (a.logprob) a.logprob[int64_t(b) * (a.k + 1) + i] = 0.f;
-      }
-  } else if (wid == 0 && lane < n) {
-    a.out[int64_t(b) * (a.k + 1) + lane] = drafts.x;
-    if (a.logprob) a.logprob[int64_t(b) * (a.k + 1) + lane] = log_of(drafts.score, rows[0][lane], a.tscale);
-  }
   if (tid == 0) found_s = 0x7fffffff, last_s = -1;
   if (wid == 0) {
     constexpr int each = kVfMaxSlices / 64;   // neighbouring slices of a lane
@@ -459,7 +505,7 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_draw(VerifyArgs a) {
   if (tid) return;
   a.out[int64_t(b) * (a.k + 1) + n] = token;
   if (a.logprob) a.logprob[int64_t(b) * (a.k + 1) + n] = token < 0 ? 0.f : log_of(score_s, st.p, a.tscale);
-  a.accepted[b] = n;
+  if (a.k == 0) a.accepted[b] = 0;
 }
 
 static int64_t verify_rows(int64_t b, int k, bool draft) { return b * (k + 1 + (draft ? k : 0)); }
@@ -470,7 +516,9 @@ static int verify_slices(int64_t n) {
   const int64_t slice = int64_t(kVfBlock) * verify_blocks(n);
   return int((n + slice - 1) / slice);
 }
-// Slices of a wavefront: one where that is no more than 4,096 workgroups.
+// Slices of a wavefront: one where that is no more than `most` workgroups (of the sums of 64
+// sequences with 6,144 of them 40 us, 43 with 4,096 or 8,192; of the second kernel with 1,024
+// 17, 19 with 2,048, as each settles first).
 static int verify_each(int64_t rows, int slices, int64_t most) {
   const int64_t each = rows * slices / (kVfWaves * most), all = (slices + kVfWaves - 1) / kVfWaves;
   return int(each < 1 ? 1 : each > all ? all : each);
@@ -482,7 +530,8 @@ static bool verify_sizes_ok(int64_t b, int k, int64_t n) {
 }
 
 static size_t verify_bytes(int64_t b, int k, bool draft, int slices) {
-  return size_t(verify_rows(b, k, draft)) * slices * sizeof(VfSum) + size_t(b) * slices * sizeof(double);
+  return size_t(verify_rows(b, k, draft)) * slices * sizeof(VfSum) +
+         size_t(b) * (slices * sizeof(double) + sizeof(Settled));
 }
 
 template <int T>
@@ -529,13 +578,14 @@ int rslm_verify(const void *target, int32_t dtype, int64_t b, int32_t k, int64_t
                with ? double(draft_scale) * unit : 1.0};
   a.slices = verify_slices(n);
   a.blocks = verify_blocks(n);
-  a.each = verify_each(verify_rows(b, k, with), a.slices, 4096);
+  a.each = verify_each(verify_rows(b, k, with), a.slices, 6144);
   a.groups = (a.slices + kVfWaves * a.each - 1) / (kVfWaves * a.each);
   a.oeach = verify_each(b, a.slices, 1024);
   a.ogroups = (a.slices + kVfWaves * a.oeach - 1) / (kVfWaves * a.oeach);
   a.tsums = static_cast<VfSum *>(ws);
   a.dsums = a.tsums + size_t(b) * (k + 1) * a.slices;
   a.rsums = reinterpret_cast<double *>(a.tsums + size_t(verify_rows(a.b, k, with)) * a.slices);
+  a.settled = reinterpret_cast<Settled *>(a.rsums + size_t(b) * a.slices);
   a.out = out_tokens;
   a.accepted = accepted;
   a.logprob = logprob;
