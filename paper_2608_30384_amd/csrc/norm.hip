@@ -6,9 +6,9 @@
 //
 // Bound by memory: x and the residual are read, h and y (or 1.03 bytes a coordinate of
 // codes and scales) are written, once each; backward h, dy and dh are read and dx written.
-// us, 8,192 x 4,096 bfloat16: forward 55 (4.9 TB/s), backward with the weight's gradient 46
-// (5.8 TB/s, some of it from the last-level cache) and 5; 20,001 x 2,049 float32 to 8 bits
-// 120 (4.5 TB/s).  Reading rows twice, and the weight's gradient by a kernel of its own,
+// us, 8,192 x 4,096 bfloat16: forward 51 (5.2 TB/s), backward with the weight's gradient 45
+// (6.0 TB/s, some of it from the last-level cache) and 5; 20,001 x 2,049 float32 to 8 bits
+// 107 (5.0 TB/s).  Reading rows twice, and the weight's gradient by a kernel of its own,
 // took 82, 162 and 143.
 #include "mx4_dev.h"
 #include "rows_dev.h"
@@ -52,15 +52,21 @@ __device__ __forceinline__ void load_weight8(float (&w)[8], const void *p, int t
   }
 }
 
+constexpr int kNormMost = 1024;   // threads of a workgroup
+
 // The sum of the workgroup's v, in every thread; `sums` has a place for each
 // wavefront, and is free again after the caller's next barrier.
 __device__ __forceinline__ float group_sum(float v, float *sums) {
+  const int waves = blockDim.x / 64;
   v = wave_sum(v);
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = v;
+  if (threadIdx.x >= waves && threadIdx.x < kNormMost / 64) sums[threadIdx.x] = 0.f;   // sums of four are added
   __syncthreads();
-  float s = sums[0];
-#pragma unroll
-  for (int i = 1; i < kNormThreads / 64; ++i) s += sums[i];
+  float s = 0.f;
+  for (int i = 0; i < waves; i += 4) {
+    const float4 v4 = *reinterpret_cast<const float4 *>(sums + i);
+    s += (v4.x + v4.y) + (v4.z + v4.w);
+  }
   return s;
 }
 
@@ -81,9 +87,9 @@ __device__ __forceinline__ void put_mx8(const float (&v)[8], uint8_t *codes, uin
 
 // ---- rows held in registers
 //
-// LANES lanes of a workgroup of 256 to a row, NV pieces of 8 coordinates each.  A row's last
-// coordinates are read 8 at a time too, from dim - 8 on, and moved to their places: no
-// branch keeps a thread's loads apart.
+// LANES lanes of a workgroup of 256 to a row, or a workgroup (LANES 0), NV pieces of 8
+// coordinates each.  A row's last coordinates are read 8 at a time too, from dim - 8 on, and
+// moved to their places: no branch keeps a thread's loads apart.
 
 // One of 8 coordinates from c on: read from `at`, the first `skip` of them another piece's.
 struct Piece {
@@ -141,28 +147,37 @@ __device__ __forceinline__ void piece_weight(float (&w)[8], const void *p, int t
   place_piece(w, e, odd);
 }
 
-// The sum over a row's lanes, in each of them.  `sums`: LANES 256 alone, as group_sum.
+constexpr int norm_rows(int lanes) { return lanes ? kNormThreads / lanes : 1; }          // of a workgroup
+constexpr int norm_bound(int lanes) { return lanes ? kNormThreads : kNormMost; }         // its threads
+template <int LANES>
+__device__ __forceinline__ int norm_lanes() {
+  return LANES ? LANES : int(blockDim.x);
+}
+
+// The sum over a row's lanes, in each of them.  `sums`: LANES 0 alone, as group_sum.
 template <int LANES>
 __device__ __forceinline__ float lanes_sum(float v, float *sums) {
-  if constexpr (LANES == 256) return group_sum(v, sums);
+  if constexpr (LANES == 0) return group_sum(v, sums);
 #pragma unroll
   for (int off = LANES / 2; off >= 1; off >>= 1) v += __shfl_xor(v, off, 64);
   return v;
 }
 
 template <int T, int LANES, int NV>
-__global__ void __launch_bounds__(kNormThreads) k_norm(NormArgs a) {
-  constexpr int R = kNormThreads / LANES;
-  __shared__ float sums[2][kNormThreads / 64];
-  const int lane = threadIdx.x % LANES, chunks = mx4_steps(a.dim) * 16;
+__global__ void __launch_bounds__(norm_bound(LANES)) k_norm(NormArgs a) {
+  constexpr int R = norm_rows(LANES);
+  __shared__ __align__(16) float sums[2][kNormMost / 64];
+  const int lanes = norm_lanes<LANES>(), lane = R == 1 ? threadIdx.x : threadIdx.x % lanes;
+  const int mine0 = R == 1 ? 0 : threadIdx.x / lanes;
+  const int chunks = mx4_steps(a.dim) * 16;
   const bool odd = a.dim & 7;
   Piece e[NV];
 #pragma unroll
-  for (int u = 0; u < NV; ++u) e[u] = piece_at(8 * (lane + LANES * u), a.dim);
+  for (int u = 0; u < NV; ++u) e[u] = piece_at(8 * (lane + lanes * u), a.dim);
   int turn = 0;
   for (int64_t row0 = int64_t(blockIdx.x) * R; row0 < a.n; row0 += int64_t(gridDim.x) * R, turn ^= 1) {
     // past the last row: that one again, without writing
-    const int64_t mine = row0 + threadIdx.x / LANES, row = min(mine, a.n - 1);
+    const int64_t mine = row0 + mine0, row = min(mine, a.n - 1);
     const bool on = mine < a.n;
     Raw8<T> rx[NV], rr[NV];
     const auto *x = row_of<T>(a.x, row, a.xstride);
@@ -200,7 +215,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm(NormArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[u][i] = h[u][i] * rstd * w[u][i] + 0.f;
       if (a.y && on) store_float8<T>(h[u], row_of<T>(a.y, row, a.ystride), e[u].c, a.dim);
-      const int k = lane + LANES * u;   // whole quads: chunks is a multiple of 16
+      const int k = lane + lanes * u;   // whole quads: chunks is a multiple of 16
       if (a.codes && on && k < chunks) {
         if (e[u].c + 8 > a.dim) {   // 0 past dim, though rstd may be no number
 #pragma unroll
@@ -217,14 +232,14 @@ __global__ void __launch_bounds__(kNormThreads) k_norm(NormArgs a) {
 // A row to a workgroup, which reads it twice (h, written in between, the second time; from
 // the cache).
 template <int T>
-__global__ void __launch_bounds__(kNormThreads) k_norm_long(NormArgs a) {
-  __shared__ float sums[2][kNormThreads / 64];
-  const int tid = threadIdx.x, chunks = mx4_steps(a.dim) * 16;
+__global__ void __launch_bounds__(kNormMost) k_norm_long(NormArgs a) {
+  __shared__ __align__(16) float sums[2][kNormMost / 64];
+  const int tid = threadIdx.x, lanes = blockDim.x, chunks = mx4_steps(a.dim) * 16;
   int turn = 0;
   for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x, turn ^= 1) {
     const auto *x = row_of<T>(a.x, row, a.xstride);
     float sum = 0.f;
-    for (int c = 8 * tid; c < a.dim; c += 8 * kNormThreads) {
+    for (int c = 8 * tid; c < a.dim; c += 8 * lanes) {
       float v[8];
       load_float8<T>(v, x, c, a.dim);
       if (a.residual) {
@@ -242,7 +257,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_long(NormArgs a) {
     if (!a.y && !a.codes) continue;
     // a thread reads back what it wrote itself
     const auto *h = a.residual ? row_of<T>(static_cast<const void *>(a.h), row, a.hstride) : x;
-    for (int k = tid; k < chunks; k += kNormThreads) {
+    for (int k = tid; k < chunks; k += lanes) {
       float v[8], w[8];
       load_float8<T>(v, h, 8 * k, a.dim);
       load_weight8(w, a.weight, a.wtype, 8 * k, a.dim);
@@ -268,24 +283,28 @@ struct NormBackArgs {
 
 // Rows of a strip by a workgroup, R at a time, which sums dweight's part in registers.
 template <int T, int LANES, int NV>
-__global__ void __launch_bounds__(kNormThreads) k_norm_backward(NormBackArgs a) {
-  constexpr int R = kNormThreads / LANES;
-  __shared__ float sums[2][kNormThreads / 64];
+__global__ void __launch_bounds__(norm_bound(LANES)) k_norm_backward(NormBackArgs a) {
+  constexpr int R = norm_rows(LANES);
+  // rows of over 8,192, 16 wavefronts, which have 128 registers each: the weight is read for
+  // each row and no row ahead (16,384 bfloat16: 4.2 TB/s; with both 3.0)
+  constexpr bool HELD = LANES || NV == 1;
+  __shared__ __align__(16) float sums[2][kNormMost / 64];
   __shared__ float parts[R > 1 ? kNormThreads * NV * 8 : 1];
-  const int lane = threadIdx.x % LANES;
+  const int lanes = norm_lanes<LANES>(), lane = R == 1 ? threadIdx.x : threadIdx.x % lanes;
+  const int mine0 = R == 1 ? 0 : threadIdx.x / lanes;
   const bool odd = a.dim & 7;
   Piece e[NV];
   float w[NV][8], acc[NV][8] = {};
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
-    e[u] = piece_at(8 * (lane + LANES * u), a.dim);
-    piece_weight(w[u], a.weight, a.wtype, e[u], odd);
+    e[u] = piece_at(8 * (lane + lanes * u), a.dim);
+    if constexpr (HELD) piece_weight(w[u], a.weight, a.wtype, e[u], odd);
   }
   const int64_t r0 = int64_t(blockIdx.x) * a.per, r1 = min(a.n, r0 + a.per);
   Raw8<T> rd[NV], rh[NV], re[NV];
   float rstd = 0.f;
   auto fetch = [&](int64_t row0) {
-    const int64_t row = min(row0 + threadIdx.x / LANES, r1 - 1);
+    const int64_t row = min(row0 + mine0, r1 - 1);
     const auto *d = row_of<T>(a.dy, row, a.dystride), *h = row_of<T>(a.h, row, a.hstride);
 #pragma unroll
     for (int u = 0; u < NV; ++u) load_piece<T>(rd[u], d, e[u]);
@@ -299,10 +318,11 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_backward(NormBackArgs a) 
     rstd = a.rstd[row];
   };
   int turn = 0;
-  if (r0 < r1) fetch(r0);
+  if (HELD && r0 < r1) fetch(r0);
   for (int64_t row0 = r0; row0 < r1; row0 += R, turn ^= 1) {
-    const int64_t row = row0 + threadIdx.x / LANES;
+    const int64_t row = row0 + mine0;
     const bool on = row < r1;
+    if (!HELD) fetch(row0);
     float g[NV][8], n[NV][8], sum = 0.f;
     const float now = rstd;
 #pragma unroll
@@ -310,6 +330,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_backward(NormBackArgs a) 
       float d[8];
       piece_values<T>(d, rd[u], e[u], odd);
       piece_values<T>(n[u], rh[u], e[u], odd);
+      if constexpr (!HELD) piece_weight(w[u], a.weight, a.wtype, e[u], odd);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         n[u][i] *= now;
@@ -330,7 +351,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_backward(NormBackArgs a) 
     }
     // the next rows' loads, before this one's stores (which may be to dy, h or dh, but of
     // rows that are done)
-    if (row0 + R < r1) fetch(row0 + R);
+    if (HELD && row0 + R < r1) fetch(row0 + R);
     if (a.dx && on) {
 #pragma unroll
       for (int u = 0; u < NV; ++u) store_float8<T>(g[u], row_of<T>(a.dx, row, a.dxstride), e[u].c, a.dim);
@@ -343,7 +364,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_backward(NormBackArgs a) 
 #pragma unroll
     for (int u = 0; u < NV; ++u)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) parts[(threadIdx.x / LANES) * (LANES * NV * 8) + (u * LANES + lane) * 8 + i] = acc[u][i];
+      for (int i = 0; i < 8; ++i) parts[mine0 * (LANES * NV * 8) + (u * LANES + lane) * 8 + i] = acc[u][i];
     __syncthreads();
     for (int c = threadIdx.x; c < a.dim; c += kNormThreads) {
       float s = parts[c];
@@ -358,15 +379,15 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_backward(NormBackArgs a) 
 }
 
 template <int T>
-__global__ void __launch_bounds__(kNormThreads) k_norm_backward_long(NormBackArgs a) {
-  __shared__ float sums[2][kNormThreads / 64];
-  const int tid = threadIdx.x;
+__global__ void __launch_bounds__(kNormMost) k_norm_backward_long(NormBackArgs a) {
+  __shared__ __align__(16) float sums[2][kNormMost / 64];
+  const int tid = threadIdx.x, lanes = blockDim.x;
   int turn = 0;
   for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x, turn ^= 1) {
     const auto *dy = row_of<T>(a.dy, row, a.dystride), *h = row_of<T>(a.h, row, a.hstride);
     const float rstd = a.rstd[row];
     float sum = 0.f;
-    for (int c = 8 * tid; c < a.dim; c += 8 * kNormThreads) {
+    for (int c = 8 * tid; c < a.dim; c += 8 * lanes) {
       float d[8], v[8], w[8];
       load_float8<T>(d, dy, c, a.dim);
       load_float8<T>(v, h, c, a.dim);
@@ -375,7 +396,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_backward_long(NormBackArg
       for (int i = 0; i < 8; ++i) sum = fmaf(d[i] * w[i], v[i] * rstd, sum);
     }
     const float mean = group_sum(sum, sums[turn]) / float(a.dim);
-    for (int c = 8 * tid; c < a.dim; c += 8 * kNormThreads) {
+    for (int c = 8 * tid; c < a.dim; c += 8 * lanes) {
       float d[8], v[8], w[8], e[8];
       load_float8<T>(d, dy, c, a.dim);
       load_float8<T>(v, h, c, a.dim);
@@ -428,61 +449,75 @@ __global__ void __launch_bounds__(1024) k_norm_join(const float *__restrict__ pa
   else store_float<RSLM_BF16>(dweight, c, s);
 }
 
-constexpr int kNormStrips = 512;   // two workgroups to a CU
-constexpr int kNormHeld = 16384, kNormBackHeld = 8192;   // coordinates of a row in registers
+constexpr int kNormHeld = 16384;                       // coordinates of a row in registers
+constexpr int kNormOne = 4096, kNormBackOne = 8192;    // of one in single pieces
 
-static int64_t norm_strips(int64_t n) { return n < kNormStrips ? n : kNormStrips; }
+// Strips of the backward pass: as many of its workgroups as 16 wavefronts to a CU make,
+// which is what all types' registers allow.  (bfloat16, dx and the weight's gradient: rows of
+// 2,049, 5 wavefronts each, 4.0 TB/s with 768 of them, 3.5 with 1,024; of 768 4.4, with half
+// as many 4.2.)
+static int64_t norm_strips(int64_t n, int dim) {
+  const int waves = dim < 8 || dim > kNormHeld ? 8 : dim <= 1024 ? 4 : dim <= kNormBackOne ? (dim + 511) / 512 : (dim + 1023) / 1024;
+  const int64_t most = 256 * (16 / waves);
+  return n < most ? n : most;
+}
 
 // The lanes of a row and its pieces: a row of up to 128 coordinates to 16 lanes, of up to
-// 1,024 to a wavefront, of more (or of over 512 where there are few) to a workgroup.
-#define RSLM_NORM_SWITCH(DIM, N, CALL)                          \
+// 1,024 to a wavefront, of more (or of over 512 where there are few) to a workgroup, of as
+// many wavefronts as it fills: of one piece to a lane up to ONE coordinates, else two.
+// (Forward, 5,120 bfloat16: 5.5 TB/s; 256 lanes of four pieces 3.2, 640 of one 3.5.)
+#define RSLM_NORM_SWITCH(DIM, N, ONE, CALL)                     \
   if ((DIM) <= 128) CALL(16, 1)                                 \
   else if ((DIM) <= 512) CALL(64, 1)                            \
   else if ((DIM) <= 1024 && (N) >= 1024) CALL(64, 2)            \
-  else if ((DIM) <= 2048) CALL(256, 1)                          \
-  else if ((DIM) <= 4096) CALL(256, 2)                          \
-  else CALL(256, 4)
+  else if ((DIM) <= ONE) CALL(0, 1)                             \
+  else CALL(0, 2)
+// The threads of a workgroup with NV pieces of 8 coordinates each.
+static unsigned norm_group(int lanes, int nv, int dim) {
+  return lanes ? kNormThreads : unsigned((dim + 8 * nv - 1) / (8 * nv) + 63) / 64 * 64;
+}
+static unsigned norm_long_group(int dim) { return dim < 8 ? 64u : unsigned(kNormMost); }
 
 template <int T>
 static void launch_norm(const NormArgs &a, hipStream_t s) {
   if (a.dim < 8 || a.dim > kNormHeld) {
     const dim3 grid(unsigned(a.n < 65536 ? a.n : 65536));
-    hipLaunchKernelGGL(k_norm_long<T>, grid, dim3(kNormThreads), 0, s, a);
+    hipLaunchKernelGGL(k_norm_long<T>, grid, dim3(norm_long_group(a.dim)), 0, s, a);
     return;
   }
 #define RSLM_NORM(LANES, NV)                                                                       \
   {                                                                                                \
-    const int64_t wg = (a.n + 256 / LANES - 1) / (256 / LANES);                                    \
+    const int64_t wg = (a.n + norm_rows(LANES) - 1) / norm_rows(LANES);                            \
     const dim3 grid(unsigned(wg < 65536 ? wg : 65536));                                            \
-    hipLaunchKernelGGL((k_norm<T, LANES, NV>), grid, dim3(kNormThreads), 0, s, a);                 \
+    hipLaunchKernelGGL((k_norm<T, LANES, NV>), grid, dim3(norm_group(LANES, NV, a.dim)), 0, s, a); \
   }
-  if (a.dim > 8192) RSLM_NORM(256, 8)
-  else RSLM_NORM_SWITCH(a.dim, a.n, RSLM_NORM)
+  RSLM_NORM_SWITCH(a.dim, a.n, kNormOne, RSLM_NORM)
 #undef RSLM_NORM
 }
 
 template <int T>
 static void launch_norm_backward(const NormBackArgs &b, void *dweight, int dwtype, hipStream_t s) {
   NormBackArgs a = b;
-  int64_t strips = norm_strips(a.n);
+  int64_t strips = norm_strips(a.n, a.dim);
   if (a.n > 0) {
     a.per = (a.n + strips - 1) / strips;
-    if (a.dim < 8 || a.dim > kNormBackHeld) {
+    if (a.dim < 8 || a.dim > kNormHeld) {
       const dim3 grid(unsigned(a.n < 65536 ? a.n : 65536));
       // the weight's gradient first: dx may be dy or h
       if (dweight)
         hipLaunchKernelGGL(k_norm_dweight<T>, dim3(unsigned((a.dim + 2047) / 2048), unsigned(strips)),
                            dim3(kNormThreads), 0, s, a);
-      if (a.dx) hipLaunchKernelGGL(k_norm_backward_long<T>, grid, dim3(kNormThreads), 0, s, a);
+      if (a.dx) hipLaunchKernelGGL(k_norm_backward_long<T>, grid, dim3(norm_long_group(a.dim)), 0, s, a);
     } else {
       if (!dweight) a.partial = nullptr;
 #define RSLM_NORM(LANES, NV)                                                                       \
   {                                                                                                \
-    a.per = (a.per + 256 / LANES - 1) / (256 / LANES) * (256 / LANES);                             \
+    a.per = (a.per + norm_rows(LANES) - 1) / norm_rows(LANES) * norm_rows(LANES);                  \
     strips = (a.n + a.per - 1) / a.per;                                                            \
-    hipLaunchKernelGGL((k_norm_backward<T, LANES, NV>), dim3(unsigned(strips)), dim3(kNormThreads), 0, s, a); \
+    hipLaunchKernelGGL((k_norm_backward<T, LANES, NV>), dim3(unsigned(strips)),                    \
+                       dim3(norm_group(LANES, NV, a.dim)), 0, s, a);                               \
   }
-      RSLM_NORM_SWITCH(a.dim, a.n, RSLM_NORM)
+      RSLM_NORM_SWITCH(a.dim, a.n, kNormBackOne, RSLM_NORM)
 #undef RSLM_NORM
     }
   }
@@ -526,7 +561,7 @@ int rslm_rmsnorm(const void *x, int32_t dtype, int64_t n, int32_t dim, int64_t x
 
 size_t rslm_rmsnorm_backward_workspace(int64_t n, int32_t dim) {
   if (!norm_sizes_ok(n, dim, RSLM_F32)) return 0;
-  return size_t(norm_strips(n)) * dim * sizeof(float);
+  return size_t(norm_strips(n, dim)) * dim * sizeof(float);
 }
 
 int rslm_rmsnorm_backward(const void *dy, int32_t dtype, int64_t n, int32_t dim, int64_t dy_stride, const void *h,

@@ -66,7 +66,7 @@ def check_forward(r, x, residual, weight, dt, eps, rows):
 
 SIZES = [(1, 1, 0), (2, 7, 1), (5, 8, 0), (3, 33, 2), (40, 96, 0), (17, 128, 0), (9, 129, 7), (4, 512, 0), (33, 768, 1),
          (1, 1024, 0), (300, 2049, 15), (2, 2048, 0), (1, 4096, 0), (3, 4100, 3), (2, 8192, 0), (1, 8200, 0), (2, 16384, 0),
-         (1, 16392, 1), (1, 20001, 0), (1, 65536, 0)]
+         (1, 16392, 1), (1, 20001, 0), (1, 65536, 0), (3, 1100, 0), (2, 5120, 1), (2, 9000, 3), (1, 12288, 0), (1100, 640, 1)]
 
 
 @pytest.mark.parametrize("dt,wt", [("f32", "f32"), ("f16", "f16"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "f16")])
@@ -107,7 +107,7 @@ def test_forward_and_gradient(R, dt, wt, n, dim, extra):
     assert np.abs(f64(dx) - dx64).max() <= 2 * HALF[dt] * np.abs(dx64).max() + 1e-5 * np.abs(dx64).max()
 
 
-@pytest.mark.parametrize("n,dim", [(700, 64), (5000, 96), (2000, 300), (1500, 1024), (1030, 2049), (600, 4096)])
+@pytest.mark.parametrize("n,dim", [(700, 64), (5000, 96), (2000, 300), (1500, 1024), (1030, 2049), (600, 4096), (1300, 1100), (300, 5120), (270, 9000)])
 def test_many_rows(R, n, dim):
     """More rows than workgroups: every row and every row's part of dweight, in bfloat16
     whose 8-bit rows are those of the float32 norm."""
