@@ -75,16 +75,23 @@ enum Mx8ScoreForm { kS8Few, kS8Tile256, kS8Tile };
 //   4,096 x 131,072 x   768   518  508      255 x 100,003 x 1,024   80   93   77
 //     257 x 100,000 x 1,024    64   39      300 x 100,000 x   768  117   89   70
 //                                            64 x 100,000 x   768   53   36   20
-inline Mx8ScoreForm score8_form(int64_t m, int64_t n, int steps) {
-  if (m <= 16) return kS8Few;
+//
+// Few rows, or few blocks of 16 by 16, each of which then takes a workgroup's time and no
+// more while a tile takes all groups one after the other.  us, few and tile, float32 / 16 bits:
+//     64 x  1,000 x 4,096     8 / 8    34 / 23     256 blocks
+//    128 x  4,000 x   768     8 / 8    11 / 9    2,000
+//     64 x  8,000 x 4,096    25 / 25   34 / 24   2,000
+//     64 x 16,000 x 1,536    18 / 18   16 / 12   4,000
+inline Mx8ScoreForm score8_form(int64_t m, int64_t n, int steps, bool exact) {
+  if (m <= 16 || (m + 15) / 16 * ((n + 15) / 16) <= (exact ? 3500 : 2000)) return kS8Few;
   return matmul_form(m, n) == kMmTile256 && steps >= 12 ? kS8Tile256 : kS8Tile;
 }
 
 // Few rows: whether four wavefronts share out the groups of 16 rows of b (less than 16
-// wavefronts to a CU with one each), and whether a's codes are held in LDS.
+// wavefronts to a CU with one each), and whether 16 rows of a's codes are held in LDS.
 constexpr int kFew8Lds = 65536;
 inline bool few8_split(int64_t n, int steps) { return (n + 15) / 16 < 4096 && steps >= 4; }
-inline bool few8_held(int64_t m, int steps) { return m * steps * 128 <= kFew8Lds; }
+inline bool few8_held(int64_t m, int steps) { return (m < 16 ? m : 16) * steps * 128 <= kFew8Lds; }
 
 // ---- float by 4-bit (mx4_score.hip)
 

@@ -49,16 +49,17 @@ __device__ __forceinline__ f32x4 mx_mfma_bf16(uint4 a, uint4 b, f32x4 c) {
 
 // ---- few rows of a -----------------------------------------------------------
 //
-// Bound by reading b, once: 1 x 1,000,000 x 768 72 us (5.7 TB/s), 1 x 131,072 x 768 11.3.  A
-// wavefront takes 16 rows of b, with two groups of them asked for at once; a's rows are in
-// LDS (HELD) where they fit.  Where there are few rows of b, the wavefronts of a workgroup
-// share out the groups of the same 16 (SPLIT), and their sums are added in a fixed order:
-// 1 x 4,096 x 4,096 in less than the 7 us of a call, 19 with one wavefront for all groups.
+// Up to 16 rows of a to a workgroup.  Bound by reading b, once for these: 1 x 1,000,000 x
+// 768 72 us (5.7 TB/s), 1 x 131,072 x 768 11.3.  A wavefront takes 16 rows of b, with two
+// groups of them asked for at once; a's rows are in LDS (HELD) where they fit.  Where there
+// are few rows of b, the wavefronts of a workgroup share out the groups of the same 16
+// (SPLIT), and their sums are added in a fixed order: 1 x 4,096 x 4,096 in less than the 7 us
+// of a call, 19 with one wavefront for all groups.
 constexpr int kFew8Flight = 2;   // us with 1, 2, 4, 6: 1 x 1,000,000 x 768 92, 72, 90, 80; 16 x 131,072 x 4,096 88, 69, 69, 77
 
 template <int T, bool SPLIT, bool HELD>
 __global__ void __launch_bounds__(256) k_mx8_score_few(const uint8_t *__restrict__ ac, const uint8_t *__restrict__ as,
-                                                       int m, const uint8_t *__restrict__ bc,
+                                                       int64_t rows, const uint8_t *__restrict__ bc,
                                                        const uint8_t *__restrict__ bs, int64_t n, int steps,
                                                        void *__restrict__ out, int64_t stride, int64_t tiles) {
   constexpr bool kExact = T == RSLM_F32;
@@ -67,6 +68,11 @@ __global__ void __launch_bounds__(256) k_mx8_score_few(const uint8_t *__restrict
   __shared__ f32x4 sums[SPLIT ? 256 : 1];
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // rows 16 y .. 16 y + m - 1
+  const int64_t row0 = 16 * int64_t(blockIdx.y);
+  ac += row0 * steps * 128, as += row0 * steps * 4;
+  out = static_cast<typename FloatType<T>::type *>(out) + row0 * stride;
+  const int m = int(min(rows - row0, int64_t(16)));
   uint32_t *held_scales = reinterpret_cast<uint32_t *>(few8_lds + m * steps * 8);
   const int64_t each = SPLIT ? int64_t(gridDim.x) : int64_t(gridDim.x) * 4;
   int64_t tile = SPLIT ? int64_t(blockIdx.x) : int64_t(blockIdx.x) * 4 + wid;
@@ -507,13 +513,14 @@ static void launch_score8_tile(const Mx8ScoreCall &c) {
 
 template <int T, bool SPLIT, bool HELD>
 static void launch_score8_few_one(const Mx8ScoreCall &c) {
-  const int64_t tiles = (c.n + 15) / 16, wg = SPLIT ? tiles : (tiles + 3) / 4;
-  const size_t lds = HELD ? size_t(c.m) * c.steps * 132 : 0;
+  const int64_t tiles = (c.n + 15) / 16, wg = SPLIT ? tiles : (tiles + 3) / 4, groups = (c.m + 15) / 16;
+  const size_t lds = HELD ? size_t(c.m < 16 ? c.m : 16) * c.steps * 132 : 0;
   // no more workgroups than the GPU holds at once, so that each fills its LDS once, and the
   // same number of tiles to each
-  const int64_t most = 256 * (lds > 40960 ? 2 : lds > 20480 ? 3 : 4), rounds = (wg + most - 1) / most;
-  hipLaunchKernelGGL((k_mx8_score_few<T, SPLIT, HELD>), dim3(unsigned((wg + rounds - 1) / rounds)), dim3(256), lds, c.s, c.ac,
-                     c.as, int(c.m), c.bc, c.bs, c.n, c.steps, c.out, c.stride, tiles);
+  const int64_t all = 256 * (lds > 40960 ? 2 : lds > 20480 ? 3 : 4), most = all > groups ? all / groups : 1;
+  const int64_t rounds = (wg + most - 1) / most;
+  hipLaunchKernelGGL((k_mx8_score_few<T, SPLIT, HELD>), dim3(unsigned((wg + rounds - 1) / rounds), unsigned(groups)), dim3(256),
+                     lds, c.s, c.ac, c.as, c.m, c.bc, c.bs, c.n, c.steps, c.out, c.stride, tiles);
 }
 template <int T>
 static void launch_score8_few(const Mx8ScoreCall &c) {
@@ -526,7 +533,7 @@ static void launch_score8_few(const Mx8ScoreCall &c) {
 
 template <int T>
 static void launch_score8(const Mx8ScoreCall &c) {
-  switch (score8_form(c.m, c.n, c.steps)) {
+  switch (score8_form(c.m, c.n, c.steps, T == RSLM_F32)) {
     case kS8Few: launch_score8_few<T>(c); break;
     case kS8Tile256: launch_score8_tile<T, 8>(c); break;
     default: launch_score8_tile<T, T == RSLM_F32 ? 2 : 4>(c);

@@ -159,7 +159,8 @@ def check_product(got, want, terms, top, dim, dt):
     (1, 1, 1), (1, 3, 31), (2, 17, 32), (3, 16, 33), (1, 300, 96), (15, 64, 100), (16, 255, 128), (17, 257, 129),
     (5, 1000, 768), (32, 65, 200), (33, 70, 300), (64, 129, 256), (65, 300, 129), (100, 513, 260), (128, 256, 384),
     (130, 1030, 500), (257, 700, 96), (300, 2049, 640), (1, 5000, 2049), (9, 33, 4096), (16, 100, 4096),
-    (16, 70000, 200), (15, 50, 4200), (70, 300, 2000), (260, 70001, 1500), (250, 66001, 1541), (1000, 17000, 1536)])
+    (16, 70000, 200), (15, 50, 4200), (70, 300, 2000), (260, 70001, 1500), (250, 66001, 1541), (1000, 17000, 1536),
+    (17, 60000, 31), (33, 40001, 129), (65, 30003, 300), (129, 9001, 96), (257, 4001, 260), (40, 19000, 2049)])
 def test_score(R, dt, m, n, dim):
     a, b = sides(m, n, dim, m + 7 * n + dim, spread=1 if dt == "f16" else 3)
     if dt == "f16":
@@ -171,7 +172,7 @@ def test_score(R, dt, m, n, dim):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("m,n,dim", [(1, 40, 64), (16, 40, 300), (40, 300, 300), (256, 4096, 128), (256, 8192, 768)])
+@pytest.mark.parametrize("m,n,dim", [(1, 40, 64), (16, 40, 300), (40, 300, 300), (256, 4096, 128), (256, 8192, 768), (64, 16000, 100)])
 def test_score_at_the_ends_of_the_scales(R, dt, m, n, dim):
     """Scales of 0 and 254 on either side with the other's making up for it, and NaN scales
     and codes, whose rows and columns are NaN and no others."""
