@@ -90,7 +90,8 @@ def whole(rng, n, dim):
 @pytest.mark.parametrize("kind", ["zipf", "one", "none", "sorted", "falling", "outside", "few"])
 @pytest.mark.parametrize("n,rows,dim", [(1, 1, 1), (2, 5, 8), (63, 4, 7), (64, 700, 96), (65, 511, 33), (1000, 512, 130),
                                         (4095, 513, 64), (4096, 70000, 8), (4097, 262143, 4), (10007, 262144, 3),
-                                        (9000, 100, 520), (30000, 1000, 40)])
+                                        (9000, 100, 520), (30000, 1000, 40), (2049, 600, 20), (8192, 262144, 3),
+                                        (8191, 5, 64), (8193, 70000, 12)])
 def test_gradient_is_exact_for_whole_numbers(R, kind, n, rows, dim):
     rng = np.random.default_rng(n + rows)
     dout, ids = whole(rng, n, dim), some_ids(kind, n, rows, n)
