@@ -262,14 +262,18 @@ __device__ __forceinline__ i32x4 buffer_of(const uint8_t *p, int64_t bytes) {
   r[3] = 0x00020000;   // raw, 32-bit; reads past the end give 0
   return r;
 }
-// 64 lanes x 16 bytes from the buffer to LDS, lane l's at lds + 16 l.  The LDS
+// 64 lanes x 16 (or 4) bytes from the buffer to LDS, lane l's at lds + 16 (4) l.  The LDS
 // address goes in m0, which the compiler writes, as it may hold a value of its own
 // there; one instruction has to come between (it may be the s_nop).
 // The whole offset is the lane's, which the end of the buffer is checked against.
+template <int BYTES = 16>
 __device__ __forceinline__ void load_to_lds(i32x4 buf, uint32_t lds, uint32_t offset) {
-  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+  static_assert(BYTES == 16 || BYTES == 4);
+  asm volatile("s_nop 0\n\t"
+               ".if %3 == 16\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds\n\t"
+               ".else\n\tbuffer_load_dword %1, %2, 0 offen lds\n\t.endif"
                :
-               : "{m0}"(lds), "v"(offset), "s"(buf)
+               : "{m0}"(lds), "v"(offset), "s"(buf), "n"(BYTES)
                : "memory");
 }
 // The same from 64 addresses, one of each lane.

@@ -198,14 +198,6 @@ __device__ __forceinline__ void for_each(F &&f) {
   for_each_of(std::make_integer_sequence<int, N>{}, f);
 }
 
-// 64 lanes x 4 bytes from the buffer to LDS (load_to_lds of 16).
-__device__ __forceinline__ void load_to_lds4(i32x4 buf, uint32_t lds, uint32_t offset) {
-  asm volatile("s_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
-               :
-               : "{m0}"(lds), "v"(offset), "s"(buf)
-               : "memory");
-}
-
 template <int T, int MF>
 __global__ void __launch_bounds__(256, MF == 4 ? 2 : 1) k_mx8_score_tile(
     const uint8_t *__restrict__ ac, const uint8_t *__restrict__ as, int64_t m, const uint8_t *__restrict__ bc,
@@ -252,9 +244,9 @@ __global__ void __launch_bounds__(256, MF == 4 ? 2 : 1) k_mx8_score_tile(
       load_to_lds(rb, lds0 + kB0 + p * kB + (wid * LB + i - LA) * 1024,
                   (vb[(i - LA) & 1] + (32 * ((i - LA) >> 1)) * cpb + t * kS8LineB) | past);
     else if (i == LA + LB)
-      load_to_lds4(rsa, lds0 + (wid * 64 < BM ? kS0 + p * kS + wid * 256 : kNone), (vs + t * 4) | past);
+      load_to_lds<4>(rsa, lds0 + (wid * 64 < BM ? kS0 + p * kS + wid * 256 : kNone), (vs + t * 4) | past);
     else
-      load_to_lds4(rsb, lds0 + kS0 + p * kS + 4 * BM + wid * 256, (vs + t * 4) | past);
+      load_to_lds<4>(rsb, lds0 + kS0 + p * kS + 4 * BM + wid * 256, (vs + t * 4) | past);
   };
 
   // ---- reads
@@ -392,9 +384,9 @@ __global__ void __launch_bounds__(256, MF == 2 ? 2 : 1) k_mx8_score_tile_f32(
     else if (i < LA + LB)
       load_to_lds(rb, lds0 + kB0 + p * kB + (wid * LB + i - LA) * 1024, (vb + (16 * (i - LA)) * cpb + t * kS8LineB) | past);
     else if (i == LA + LB)
-      load_to_lds4(rsa, lds0 + (wid * 64 < BM ? kS0 + p * kS + wid * 256 : kNone), (vs + t * 4) | past);
+      load_to_lds<4>(rsa, lds0 + (wid * 64 < BM ? kS0 + p * kS + wid * 256 : kNone), (vs + t * 4) | past);
     else
-      load_to_lds4(rsb, lds0 + kS0 + p * kS + 4 * BM + wid * 256, (vs + t * 4) | past);
+      load_to_lds<4>(rsb, lds0 + kS0 + p * kS + 4 * BM + wid * 256, (vs + t * 4) | past);
   };
 
   // ---- reads: a's 16 bytes 32 g + 16 pass .. of a fragment's rows, b's 32 g .. of all
