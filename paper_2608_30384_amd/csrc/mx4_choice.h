@@ -65,16 +65,16 @@ enum Mx8ScoreForm { kS8Few, kS8Tile256, kS8Tile };
 
 // Tiles of 256 rows where they fill the GPU and there are enough groups of 128 coordinates
 // to make up for a tile's beginning and end, which the other CU-sharing workgroup covers
-// else.  us, m x n x dim with tiles of 256 and of 128 rows to bfloat16, and of 256, 128 and
-// 64 to float32:
-//     512 x  32,768 x 4,096    52   68    1,024 x 32,768 x 4,096   244  282  296
-//   1,024 x  32,768 x 2,048    60   62      512 x 32,768 x 2,048    63   76   71
-//   4,096 x  32,768 x 1,536   182  192    2,048 x  8,192 x 2,048    72   78   75
-//   4,096 x  32,768 x 1,024   141  137    4,096 x 32,768 x 1,024   322  381  344
-//   1,024 x  32,768 x 1,024    39   35    1,024 x 32,768 x   512    53   61   53
-//   4,096 x 131,072 x   768   518  508      255 x 100,003 x 1,024   80   93   77
-//     257 x 100,000 x 1,024    64   39      300 x 100,000 x   768  117   89   70
-//                                            64 x 100,000 x   768   53   36   20
+// else.  us, m x n x dim with tiles of 256 and of 128 rows to bfloat16, and of 256 and 64 to
+// float32:
+//     512 x  32,768 x 4,096    52   68      1,024 x 32,768 x 4,096   215  271
+//   1,024 x  32,768 x 2,048    60   62        512 x 32,768 x 2,048    60   66
+//   4,096 x  32,768 x 1,536   182  192      4,096 x 32,768 x 1,536   395  405
+//   4,096 x  32,768 x 1,024   141  137      4,096 x 32,768 x 1,024   309  287
+//   1,024 x  32,768 x 1,024    39   35      1,024 x 32,768 x   512    51   46
+//   4,096 x 131,072 x   768   518  508
+//     257 x 100,000 x 1,024    64   39
+// Tiles of 128 rows to float32, on the GPU one at a time, were the slowest of the three.
 //
 // Few rows, or few blocks of 16 by 16, each of which then takes a workgroup's time and no
 // more while a tile takes all groups one after the other.  us, few and tile, float32 / 16 bits:

@@ -454,10 +454,13 @@ __global__ void __launch_bounds__(256, MF == 2 ? 2 : 1) k_mx8_score_tile_f32(
   }
 
   // Through LDS, so that a store writes 2 rows of 512 consecutive bytes, a part of LDS for
-  // each wavefront.
-  struct __attribute__((packed, aligned(4))) Wide {
-    uint32_t v[4];
-  };
+  // each wavefront.  Of small tiles past the caches' order: us, with and without, and with the
+  // log probabilities that read the scores behind them
+  //     255 x 100,003 x 1,024   67   71    89   92    2,048 x 131,072 x 768   464  570   723  806
+  //   1,000 x  50,000 x    96   46   50    87   85
+  // Large tiles gain less and the readers lose it: 2,048 x 32,768 x 4,096 440, 453, then 510, 482;
+  // 16-bit results of 2,048 x 131,072 x 768 217, 265, then 403, 399.
+  typedef uint32_t Wide __attribute__((ext_vector_type(4), aligned(4)));
   constexpr int kOwn = MF == 8 ? 32768 : 16384, kRows = kOwn / 512;   // rows at a time
   static_assert(4 * kOwn <= kNone, "LDS of the stores");
   arrive<0>();   // the last operands have been read, and the last loads have come, everywhere
@@ -479,7 +482,8 @@ __global__ void __launch_bounds__(256, MF == 2 ? 2 : 1) k_mx8_score_tile_f32(
       if (orow >= m) continue;
       float *o = out + orow * stride + c;
       if (c + 4 <= n) {   // rows may begin anywhere
-        *reinterpret_cast<Wide *>(o) = __builtin_bit_cast(Wide, v);
+        if constexpr (MF == 2) __builtin_nontemporal_store(__builtin_bit_cast(Wide, v), reinterpret_cast<Wide *>(o));
+        else *reinterpret_cast<Wide *>(o) = __builtin_bit_cast(Wide, v);
       } else {
         const uint32_t e[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
