@@ -9,11 +9,12 @@
 // polynomial of degree 3 and a scaling, some 16 instructions, which bound the first kernel
 // where there are many rows.
 //
-// Three kernels.  The first sums the exponentials of every row, a slice of 1,024 entries
-// (more where a row has over 262,144) at a time to a wavefront.  The second settles which
-// drafts stand, each workgroup for itself, and where one falls sums r over the slices.  The
-// third draws: the slice, then the token.  64 sequences of 4 drafts by 131,072 bfloat16
-// scores: 40, 16 and 10 us; one, of float32: 4.7, 5.4 and 8.3, chains of dependent reads.
+// Two kernels.  The first sums the exponentials of every row, a slice of 1,024 entries (more
+// where a row has over 262,144) at a time to a wavefront.  In the second each workgroup of a
+// sequence settles which drafts stand, and where one falls sums r over its slices; the last
+// one to have done so draws.  64 sequences of 4 drafts by 131,072 bfloat16 scores: 39 and 26
+// us (a kernel of its own for the draw: 17 and 9); one, of float32: 4.8 and 11.6 (5.4 and 8.3,
+// and a launch), chains of dependent reads.
 #include "mx4_dev.h"
 
 namespace rslm {
@@ -70,7 +71,7 @@ struct VerifyArgs {
   int oeach, ogroups;               // and of a sequence in the second
   VfSum *tsums, *dsums;             // b x (k + 1) x slices, b x k x slices
   double *rsums;                    // b x slices
-  Settled *settled;                 // b
+  int *done;                        // b: workgroups that have written their rsums
   int64_t *out;
   int32_t *accepted;
   float *logprob;
@@ -180,6 +181,7 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_sums(VerifyArgs a) {
   const bool draft = row >= trows;
   const int64_t at = draft ? row - trows : row;
   const int b = int(at / (draft ? a.k : a.k + 1)), i = int(at - int64_t(b) * (draft ? a.k : a.k + 1));
+  if (at == int64_t(b) * (a.k + 1) && !draft && int(blockIdx.x) % a.groups == 0 && threadIdx.x == 0) a.done[b] = 0;
   // rows past the sequence's last draft are not read
   if (i >= vf_count(a, b) + (draft ? 0 : 1)) return;
   const auto *x = draft ? draft_row<T>(a, b, i) : target_row<T>(a, b, i);
@@ -337,38 +339,15 @@ __device__ __forceinline__ Over over_of(const VerifyArgs &a, int b, const Settle
   return o;
 }
 
-// Of each sequence with a draft that fell: r summed over each slice.
+// r summed over the slices of a workgroup, one at a time to a wavefront.
 template <int T>
-__global__ void __launch_bounds__(kVfThreads) k_verify_over(VerifyArgs a) {
-  __shared__ double table[256];
-  __shared__ VfSum rows[2][kVfMaxDrafts + 1];
-  __shared__ Settled st;
+__device__ __forceinline__ void sum_over(const VerifyArgs &a, int b, int group, const Settled &st, const double *table) {
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int b = int(blockIdx.x) / a.ogroups;
-  fill_table(table);
-  __syncthreads();
-  const Drafted drafts = settle<T>(a, b, table, rows, st);
-  // all but the drawn token, by the first workgroup
-  if (int(blockIdx.x) % a.ogroups == 0) {
-    const int n = st.accepted, i = threadIdx.x;
-    if (i < n) {
-      a.out[int64_t(b) * (a.k + 1) + i] = drafts.x;
-      if (a.logprob) a.logprob[int64_t(b) * (a.k + 1) + i] = log_of(drafts.score, rows[0][i], a.tscale);
-    } else if (i > n && i <= a.k) {
-      a.out[int64_t(b) * (a.k + 1) + i] = -1;
-      if (a.logprob) a.logprob[int64_t(b) * (a.k + 1) + i] = 0.f;
-    }
-    if (i == 0) {
-      a.settled[b] = st;
-      a.accepted[b] = n;
-    }
-  }
-  if (st.accepted == st.count) return;
   const Over over = over_of(a, b, st, true);
   const auto *x = target_row<T>(a, b, st.accepted);
   const auto *d = a.draft ? draft_row<T>(a, b, st.accepted) : x;
   for (int t = 0; t < a.oeach; ++t) {
-    const int s = (int(blockIdx.x) % a.ogroups) * (kVfWaves * a.oeach) + kVfWaves * t + wid;
+    const int s = group * (kVfWaves * a.oeach) + kVfWaves * t + wid;
     if (s >= a.slices) break;
     double sum = 0;
     for (int64_t j = int64_t(s) * a.blocks * kVfBlock, e = j + int64_t(a.blocks) * kVfBlock; j < min(e, a.n); j += kVfBlock) {
@@ -380,7 +359,7 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_over(VerifyArgs a) {
         sum += over.of(float(rp.v[q / 8].v[q % 8]), float(rq.v[q / 8].v[q % 8]), j + (q >> 3) * 512 + 8 * lane + (q & 7), table);
     }
     sum = wave_sum64(sum);
-    if (lane == 0) a.rsums[int64_t(b) * a.slices + s] = sum;
+    if (lane == 0) __hip_atomic_store(&a.rsums[int64_t(b) * a.slices + s], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
 }
 
@@ -394,7 +373,9 @@ __device__ __forceinline__ double wave_upto64(double v) {   // the sum of lanes 
   return v;
 }
 
-// A workgroup to a sequence: the slice that the drawn token is in, then the token.
+// Of each sequence: which drafts stand, by each of its workgroups; where one fell, r summed
+// over each slice; then, by the last workgroup to do so (else the first), the drawn token: the
+// slice that it is in, then the token.
 template <int T>
 __global__ void __launch_bounds__(kVfThreads) k_verify_draw(VerifyArgs a) {
   __shared__ double table[256];
@@ -402,15 +383,39 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_draw(VerifyArgs a) {
   __shared__ Settled st;
   __shared__ double waves[kVfWaves];
   __shared__ double want_s, base_s;
-  __shared__ int slice_s, drafted_s, found_s, last_s;
+  __shared__ int slice_s, drafted_s, found_s, last_s, draws_s;
   __shared__ float score_s;
-  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6, b = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int b = int(blockIdx.x) / a.ogroups, group = int(blockIdx.x) % a.ogroups;
   const float u = a.uniforms[int64_t(b) * (a.k + 1) + a.k];
-  if (a.k > 0 && tid == 0) st = a.settled[b];
   fill_table(table);
   __syncthreads();
-  if (a.k == 0) settle<T>(a, b, table, rows, st);   // no kernel before this one has
+  const Drafted drafts = settle<T>(a, b, table, rows, st);
   const int n = st.accepted;
+  if (group == 0) {   // all but the drawn token
+    if (tid < n) {
+      a.out[int64_t(b) * (a.k + 1) + tid] = drafts.x;
+      if (a.logprob) a.logprob[int64_t(b) * (a.k + 1) + tid] = log_of(drafts.score, rows[0][tid], a.tscale);
+    } else if (tid > n && tid <= a.k) {
+      a.out[int64_t(b) * (a.k + 1) + tid] = -1;
+      if (a.logprob) a.logprob[int64_t(b) * (a.k + 1) + tid] = 0.f;
+    }
+    if (tid == 0) a.accepted[b] = n;
+  }
+  if (n < st.count) {
+    // The sums are written and read past the caches that other workgroups do not share, and
+    // have arrived before the workgroup counts itself: the last one reads all of them.  (With
+    // fences, which write back and empty those caches, 64 sequences took 44 us and not 26.)
+    sum_over<T>(a, b, group, st, table);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0)
+      draws_s = __hip_atomic_fetch_add(&a.done[b], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.ogroups - 1;
+    __syncthreads();
+    if (!draws_s) return;
+  } else if (group > 0) {
+    return;
+  }
   if (tid == 0) found_s = 0x7fffffff, last_s = -1;
   if (wid == 0) {
     constexpr int each = kVfMaxSlices / 64;   // neighbouring slices of a lane
@@ -419,7 +424,8 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_draw(VerifyArgs a) {
     if (drafted) {
 #pragma unroll
       for (int i = 0; i < each; ++i)
-        if (each * lane + i < a.slices) r[i] = a.rsums[int64_t(b) * a.slices + each * lane + i];
+        if (each * lane + i < a.slices)
+          r[i] = __hip_atomic_load(&a.rsums[int64_t(b) * a.slices + each * lane + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       drafted = __ballot(r[0] > 0 || r[1] > 0 || r[2] > 0 || r[3] > 0) != 0;   // else p and q are the same
     }
     if (!drafted) {
@@ -505,7 +511,6 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_draw(VerifyArgs a) {
   if (tid) return;
   a.out[int64_t(b) * (a.k + 1) + n] = token;
   if (a.logprob) a.logprob[int64_t(b) * (a.k + 1) + n] = token < 0 ? 0.f : log_of(score_s, st.p, a.tscale);
-  if (a.k == 0) a.accepted[b] = 0;
 }
 
 static int64_t verify_rows(int64_t b, int k, bool draft) { return b * (k + 1 + (draft ? k : 0)); }
@@ -531,7 +536,7 @@ static bool verify_sizes_ok(int64_t b, int k, int64_t n) {
 
 static size_t verify_bytes(int64_t b, int k, bool draft, int slices) {
   return size_t(verify_rows(b, k, draft)) * slices * sizeof(VfSum) +
-         size_t(b) * (slices * sizeof(double) + sizeof(Settled));
+         size_t(b) * (slices * sizeof(double) + sizeof(int));
 }
 
 template <int T>
@@ -539,8 +544,7 @@ static void launch_verify(const VerifyArgs &a, hipStream_t s) {
   const dim3 threads(kVfThreads);
   hipLaunchKernelGGL(k_verify_sums<T>, dim3(unsigned(verify_rows(a.b, a.k, a.draft != nullptr) * a.groups)), threads, 0,
                      s, a);
-  if (a.k > 0) hipLaunchKernelGGL(k_verify_over<T>, dim3(unsigned(int64_t(a.b) * a.ogroups)), threads, 0, s, a);
-  hipLaunchKernelGGL(k_verify_draw<T>, dim3(unsigned(a.b)), threads, 0, s, a);
+  hipLaunchKernelGGL(k_verify_draw<T>, dim3(unsigned(int64_t(a.b) * a.ogroups)), threads, 0, s, a);
 }
 
 }  // namespace rslm
@@ -581,11 +585,11 @@ int rslm_verify(const void *target, int32_t dtype, int64_t b, int32_t k, int64_t
   a.each = verify_each(verify_rows(b, k, with), a.slices, 6144);
   a.groups = (a.slices + kVfWaves * a.each - 1) / (kVfWaves * a.each);
   a.oeach = verify_each(b, a.slices, 1024);
-  a.ogroups = (a.slices + kVfWaves * a.oeach - 1) / (kVfWaves * a.oeach);
+  a.ogroups = k > 0 ? (a.slices + kVfWaves * a.oeach - 1) / (kVfWaves * a.oeach) : 1;
   a.tsums = static_cast<VfSum *>(ws);
   a.dsums = a.tsums + size_t(b) * (k + 1) * a.slices;
   a.rsums = reinterpret_cast<double *>(a.tsums + size_t(verify_rows(a.b, k, with)) * a.slices);
-  a.settled = reinterpret_cast<Settled *>(a.rsums + size_t(b) * a.slices);
+  a.done = reinterpret_cast<int *>(a.rsums + size_t(b) * a.slices);
   a.out = out_tokens;
   a.accepted = accepted;
   a.logprob = logprob;

@@ -200,3 +200,20 @@ def test_other_stream_and_captured(R):
         R.rslm_verify(z[:1], tokens[:1], u[:1])
         torch.cuda.synchronize()
         assert torch.equal(got[0], e.tokens) and torch.equal(got[1], e.accepted) and torch.equal(got[2], e.logprob)
+
+
+@pytest.mark.parametrize("b,k,n", [(1, 4, 131072), (24, 3, 40000), (70, 2, 9000)])
+def test_calls_one_after_another(R, b, k, n):
+    """Two inputs in turn, whose sums are written to the same memory: each call draws from its
+    own, whichever workgroup of a sequence comes last."""
+    calls = []
+    for seed in (1, 2):
+        z, d, tokens, u = make(b, k, n, "f32", seed)
+        r = check(R, z, d, tokens, u)
+        calls.append(([t.cuda() for t in (z, tokens, u)], d.cuda(), r))
+    for i in range(60):
+        (z, tokens, u), d, want = calls[i % 2]
+        r = R.rslm_verify(z, tokens, u, draft=d)
+        assert torch.equal(r.tokens, want.tokens) and torch.equal(r.accepted, want.accepted)
+        assert torch.equal(r.logprob, want.logprob)
+        del r
