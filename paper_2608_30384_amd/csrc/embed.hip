@@ -543,9 +543,10 @@ static EmbedPlan embed_plan(int64_t n, int64_t rows, int dim) {
   p.per = (rounds + kSortMaxTiles - 1) / kSortMaxTiles * kSortRound;
   p.tiles = p.per ? int((n + p.per - 1) / p.per) : 0;
   if (n <= kSortSmall) p.tiles = 1;
-  // 8 wavefronts to a CU, chunks of 8 to 512 entries
+  // 8 wavefronts to a CU, chunks of 8 to 512 entries; up to 16 in one, which has nothing to
+  // join (11 of 12,000 x 512: 13.2 us, 16.4 in two; 32 of 12,000 x 64: 19.3 in one, 16.3)
   const int64_t cols = (dim + kSumCols - 1) / kSumCols;
-  p.chunk = 8;
+  p.chunk = n <= 16 ? 16 : 8;
   while (p.chunk < 512 && (n + p.chunk - 1) / p.chunk * cols > 2048) p.chunk *= 2;
   p.chunks = (n + p.chunk - 1) / p.chunk;
   p.entries = rounded(size_t(n) * sizeof(Entry));

@@ -91,7 +91,7 @@ def whole(rng, n, dim):
 @pytest.mark.parametrize("n,rows,dim", [(1, 1, 1), (2, 5, 8), (63, 4, 7), (64, 700, 96), (65, 511, 33), (1000, 512, 130),
                                         (4095, 513, 64), (4096, 70000, 8), (4097, 262143, 4), (10007, 262144, 3),
                                         (9000, 100, 520), (30000, 1000, 40), (2049, 600, 20), (8192, 262144, 3),
-                                        (8191, 5, 64), (8193, 70000, 12)])
+                                        (8191, 5, 64), (8193, 70000, 12), (9, 4, 96), (16, 40, 96), (17, 3, 96)])
 def test_gradient_is_exact_for_whole_numbers(R, kind, n, rows, dim):
     rng = np.random.default_rng(n + rows)
     dout, ids = whole(rng, n, dim), some_ids(kind, n, rows, n)
