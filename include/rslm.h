@@ -563,8 +563,9 @@ int rslm_mx8_score(const uint8_t *a_codes, const uint8_t *a_scales, int64_t m, c
  *   is a residual; it may be x or residual (the same stride).  y, codes and
  *   scales: NULL where not asked for.  weight: dim values of type weight_dtype.
  *   rstd: n float32.  eps > 0, finite.  The mean of squares has to be within
- *   float32 (|h| up to about 10^19): past it rstd is 0.  A row with a NaN gives
- *   NaN, one with an infinity NaN where that stands (in 8 bits in its 32
+ *   float32 (|h| up to about 10^19, whatever dim): past it rstd is 0.  Squares
+ *   below 2^-126 lose bits, which an eps of that size would show.  A row with a
+ *   NaN gives NaN, one with an infinity NaN where that stands (in 8 bits in its 32
  *   coordinates) and 0 elsewhere.
  *
  * rslm_rmsnorm_backward: the gradients from those of y (dy) and of h (dh, that of

@@ -163,6 +163,16 @@ __device__ __forceinline__ float lanes_sum(float v, float *sums) {
   return v;
 }
 
+// 1 / sqrt of the mean of squares and eps, of their sum.  The sum of up to 65,536 = 2^16 of them
+// may pass float32 where their mean does not: `again` then gives that of the values' 2^-8ths.
+template <class Again>
+__device__ __forceinline__ float norm_rstd(float sum, int dim, float eps, Again &&again) {
+  float mean = sum / float(dim);
+  if (sum == INFINITY) mean = again() / float(dim) * 0x1p16f;   // the same for all of a row's lanes
+  return 1.f / sqrtf(mean + eps);
+}
+constexpr float kNormLess = 0x1p-8f;
+
 template <int T, int LANES, int NV>
 __global__ void __launch_bounds__(norm_bound(LANES)) k_norm(NormArgs a) {
   constexpr int R = norm_rows(LANES);
@@ -208,7 +218,16 @@ __global__ void __launch_bounds__(norm_bound(LANES)) k_norm(NormArgs a) {
     float w[NV][8];
 #pragma unroll
     for (int u = 0; u < NV; ++u) piece_weight(w[u], a.weight, a.wtype, e[u], odd);
-    const float rstd = 1.f / sqrtf(lanes_sum<LANES>(sum, sums[turn]) / float(a.dim) + a.eps);
+    const float rstd = norm_rstd(lanes_sum<LANES>(sum, sums[turn]), a.dim, a.eps, [&] {
+      float less = 0.f;
+#pragma unroll
+      for (int u = 0; u < NV; ++u)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) less = fmaf(h[u][i] * kNormLess, h[u][i] * kNormLess, less);
+      less = lanes_sum<LANES>(less, sums[turn ^ 1]);
+      if (LANES == 0) __syncthreads();   // the next row's sums go there
+      return less;
+    });
     if (lane == 0 && on) a.rstd[row] = rstd;
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
@@ -252,11 +271,22 @@ __global__ void __launch_bounds__(kNormMost) k_norm_long(NormArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum = fmaf(v[i], v[i], sum);
     }
-    const float rstd = 1.f / sqrtf(group_sum(sum, sums[turn]) / float(a.dim) + a.eps);
-    if (tid == 0) a.rstd[row] = rstd;
-    if (!a.y && !a.codes) continue;
     // a thread reads back what it wrote itself
     const auto *h = a.residual ? row_of<T>(static_cast<const void *>(a.h), row, a.hstride) : x;
+    const float rstd = norm_rstd(group_sum(sum, sums[turn]), a.dim, a.eps, [&] {
+      float less = 0.f;
+      for (int c = 8 * tid; c < a.dim; c += 8 * lanes) {
+        float v[8];
+        load_float8<T>(v, h, c, a.dim);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) less = fmaf(v[i] * kNormLess, v[i] * kNormLess, less);
+      }
+      less = group_sum(less, sums[turn ^ 1]);
+      __syncthreads();   // the next row's sums go there
+      return less;
+    });
+    if (tid == 0) a.rstd[row] = rstd;
+    if (!a.y && !a.codes) continue;
     for (int k = tid; k < chunks; k += lanes) {
       float v[8], w[8];
       load_float8<T>(v, h, 8 * k, a.dim);
