@@ -531,7 +531,7 @@ static int verify_each(int64_t rows, int slices, int64_t most) {
 
 static bool verify_sizes_ok(int64_t b, int k, int64_t n) {
   return b >= 0 && k >= 0 && k <= kVfMaxDrafts && n >= 1 && n <= 0x7fffffff - 2 * 4096 &&
-         b * (2 * k + 1) <= 0x7fffffff / kVfThreads;   // a grid counts its threads in 32 bits
+         b <= 0x7fffffff / kVfThreads / (2 * k + 1);   // a grid counts its threads in 32 bits
 }
 
 static size_t verify_bytes(int64_t b, int k, bool draft, int slices) {
