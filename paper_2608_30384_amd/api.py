@@ -11,6 +11,7 @@ import functools
 
 import numpy as np
 import torch
+from torch.autograd.graph import increment_version
 
 from . import _lib as L
 
@@ -41,6 +42,14 @@ def _need(t, dtype, name):
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+
+
+def _written(*tensors):
+    """Tells autograd that the kernels wrote these tensors of the caller's (None: none):
+    a gradient that needs what they held before is then an error, and not wrong."""
+    for t in tensors:
+        if t is not None:
+            increment_version(t)
 
 
 class _Workspace:
@@ -130,6 +139,7 @@ def rslm_fwht(plan, x, y=None, inverse=False, stream=None):
     _need(y, torch.float32, "y")
     L.check("rslm_fwht", L.lib().rslm_fwht(plan.handle, _ptr(x), _ptr(y), n, int(inverse),
                                            _stream(stream)))
+    _written(y)
     return y
 
 
@@ -155,6 +165,7 @@ def rslm_encode(plan, x, codes, scales, n_records=None, src_row=None, rec_list=N
         plan.handle, _ptr(x), n_rows, _ptr(src_row), _ptr(rec_list), n_records,
         _ptr(centroids), _ptr(centroids_rot), nlist, _ptr(codes), _ptr(scales),
         _ptr(resid_rot), _stream(stream)))
+    _written(codes, scales, resid_rot)
 
 
 def rslm_encode_two_stage(plan, plan2, x, codes, scales, codes2, scales2, n_records=None,
@@ -184,6 +195,7 @@ def rslm_encode_two_stage(plan, plan2, x, codes, scales, codes2, scales2, n_reco
         plan.handle, plan2.handle, _ptr(x), n_rows, _ptr(src_row), _ptr(rec_list), n_records,
         _ptr(centroids), _ptr(centroids_rot), nlist, _ptr(codes), _ptr(scales), _ptr(codes2),
         _ptr(scales2), _stream(stream)))
+    _written(codes, scales, codes2, scales2)
 
 
 def rslm_encode_sq8(plan, x, codes, scales, lo, hi, codes2, n_records=None, src_row=None,
@@ -212,6 +224,7 @@ def rslm_encode_sq8(plan, x, codes, scales, lo, hi, codes2, n_records=None, src_
         plan.handle, _ptr(x), n_rows, _ptr(src_row), _ptr(rec_list), n_records,
         _ptr(centroids), _ptr(centroids_rot), nlist, _ptr(codes), _ptr(scales), _ptr(lo),
         _ptr(hi), _ptr(codes2), _stream(stream)))
+    _written(codes, scales, codes2)
 
 
 def rslm_pack_codes(plan, canon, n, stream=None):
@@ -235,6 +248,7 @@ def rslm_decode(plan, codes, scales, n, rec_list=None, centroids=None, out=None,
     L.check("rslm_decode", L.lib().rslm_decode(plan.handle, _ptr(codes), _ptr(scales), n,
                                                _ptr(rec_list), _ptr(centroids), nlist, _ptr(out),
                                                _stream(stream)))
+    _written(out)
     return out
 
 
@@ -263,6 +277,7 @@ def rslm_score(plan, records, q_rot, ids=None, n=None, out=None, stream=None):
     _need(out, torch.float32, "out")
     L.check("rslm_score", L.lib().rslm_score(plan.handle, _ptr(records), n_pool, _ptr(ids), n,
                                              _ptr(q_rot), Q, _ptr(out), _stream(stream)))
+    _written(out)
     return out
 
 
@@ -290,6 +305,7 @@ def ivf_assign_probe(x, centroids, nprobe=1, mode=L.IVF_ASSIGN_L2, out_ids=None,
     L.check("ivf_assign_probe", L.lib().ivf_assign_probe(
         _ptr(x), n, dim, _ptr(centroids), nlist, nprobe, mode, _ptr(out_ids),
         _ptr(out_scores), _ptr(ws), ws.numel(), _stream(stream)))
+    _written(out_ids, out_scores)
     return out_ids, out_scores
 
 
@@ -304,6 +320,7 @@ def ivf_assign_probe_noalloc(x, centroids, nprobe, mode, out_ids, out_scores, st
     L.check("ivf_assign_probe_noalloc", L.lib().ivf_assign_probe_noalloc(
         _ptr(x), n, dim, _ptr(centroids), centroids.shape[0], nprobe, mode, _ptr(out_ids),
         _ptr(out_scores), _stream(stream)))
+    _written(out_ids, out_scores)
     return out_ids, out_scores
 
 
@@ -322,6 +339,7 @@ def ivf_kmeans_update(x, assign, centroids, stream=None):
     L.check("ivf_kmeans_update", L.lib().ivf_kmeans_update(
         _ptr(x), n, dim, _ptr(assign), nlist, _ptr(centroids), _ptr(ws), ws.numel(),
         _stream(stream)))
+    _written(centroids)
     return centroids
 
 
@@ -367,6 +385,7 @@ def rslm_scan_topk(plan, index, q_rot, probe_ids, probe_dots, k, out_scores=None
     L.check("rslm_scan_topk", L.lib().rslm_scan_topk(
         plan.handle, C.byref(cs), _ptr(q_rot), Q, _ptr(probe_ids), _ptr(probe_dots), nprobe, k,
         _ptr(out_scores), _ptr(out_ids), _ptr(ws), ws.numel(), _stream(stream)))
+    _written(out_scores, out_ids)
     return out_scores, out_ids
 
 
@@ -379,6 +398,7 @@ def rslm_sq8_fit(v, lo=None, hi=None, accumulate=False, stream=None):
         hi = torch.empty(dim, dtype=torch.float32, device=v.device)
     L.check("rslm_sq8_fit", L.lib().rslm_sq8_fit(_ptr(v), n, dim, _ptr(lo), _ptr(hi),
                                                  int(accumulate), _stream(stream)))
+    _written(lo, hi)
     return lo, hi
 
 
@@ -393,6 +413,7 @@ def rslm_sq8_encode(v, lo, hi, codes=None, dest_row=None, stream=None):
     L.check("rslm_sq8_encode", L.lib().rslm_sq8_encode(_ptr(v), n, dim, _ptr(lo), _ptr(hi),
                                                        _ptr(dest_row), n_dest, _ptr(codes),
                                                        _stream(stream)))
+    _written(codes)
     return codes
 
 
@@ -414,6 +435,7 @@ def rslm_rescore(codes2, lo, hi, q_rot, cand_scores, cand_ids, k_out, out_scores
                                                  _ptr(cand_scores), _ptr(cand_ids), k_in, k_out,
                                                  _ptr(out_scores), _ptr(out_ids),
                                                  _stream(stream)))
+    _written(out_scores, out_ids)
     return out_scores, out_ids
 
 
@@ -440,6 +462,7 @@ def rslm_rescore_rslm(plan2, codes2, scales2, q_rot, cand_scores, cand_ids, k_ou
                                                  _ptr(cand_scores), _ptr(cand_ids), k_in, k_out,
                                                  _ptr(out_scores), _ptr(out_ids),
                                                  _stream(stream)))
+    _written(out_scores, out_ids)
     return out_scores, out_ids
 
 
@@ -510,6 +533,11 @@ def _out_rows(out, shape, dtype, device, stream, name="out"):
     code, stride = _need_rows(out, name, shape)
     if out.device != device:
         raise ValueError(f"{name} must be on {device}, got {out.device}")
+    if out.requires_grad and torch.is_grad_enabled():
+        base = out if out._base is None else out._base
+        if not base.is_leaf:
+            raise ValueError(f"{name} is computed from tensors that require a gradient, which what is written over it does "
+                             f"not have: call under torch.no_grad() or pass {name}.detach()")
     return out, code, stride
 
 
@@ -591,6 +619,7 @@ def _quantize(fn, kind, x, plan, rows, stream):
             raise ValueError("x must have the plan's dimension")
         if plan.device != device:
             raise ValueError(f"x must be on the plan's device ({plan.device}), got {device}")
+    given = rows
     if rows is None:
         rows = kind.empty(n, dim, device, stream)
     else:
@@ -601,16 +630,19 @@ def _quantize(fn, kind, x, plan, rows, stream):
     L.check(fn, getattr(L.lib(), fn)(
         plan.handle if plan is not None else None, x.data_ptr(), code, n, dim, stride, rows.codes.data_ptr(),
         rows.scales.data_ptr(), _launch_stream(stream, device)))
+    if given is not None:
+        _written(rows.codes, rows.scales)
     return rows
 
 
 def _dequantize(fn, kind, rows, dtype, out, stream):
     _need_mx(rows, kind, "rows")
-    out, code, stride = _out_rows(out, (rows.n, rows.dim), dtype, rows.device, stream)
+    into, code, stride = _out_rows(out, (rows.n, rows.dim), dtype, rows.device, stream)
     L.check(fn, getattr(L.lib(), fn)(
-        rows.codes.data_ptr(), rows.scales.data_ptr(), rows.n, rows.dim, out.data_ptr(), code, stride,
-        _launch_stream(stream, out.device)))
-    return out
+        rows.codes.data_ptr(), rows.scales.data_ptr(), rows.n, rows.dim, into.data_ptr(), code, stride,
+        _launch_stream(stream, into.device)))
+    _written(out)
+    return into
 
 
 def rslm_mx4_quantize(x, plan=None, rows=None, stream=None):
@@ -631,11 +663,12 @@ def rslm_mx4_matmul(a, b, dtype=torch.float32, out=None, stream=None):
     if a.dim != b.dim:
         raise ValueError("a and b must have the same dimension")
     _same_device(a, b, "b")
-    out, code, stride = _out_rows(out, (a.n, b.n), dtype, a.device, stream)
+    into, code, stride = _out_rows(out, (a.n, b.n), dtype, a.device, stream)
     L.check("rslm_mx4_matmul", L.lib().rslm_mx4_matmul(
-        a.codes.data_ptr(), a.scales.data_ptr(), a.n, b.codes.data_ptr(), b.scales.data_ptr(), b.n, a.dim, out.data_ptr(),
-        code, stride, _launch_stream(stream, out.device)))
-    return out
+        a.codes.data_ptr(), a.scales.data_ptr(), a.n, b.codes.data_ptr(), b.scales.data_ptr(), b.n, a.dim, into.data_ptr(),
+        code, stride, _launch_stream(stream, into.device)))
+    _written(out)
+    return into
 
 
 def rslm_mx4_score(x, b, dtype=torch.float32, out=None, stream=None):
@@ -647,13 +680,14 @@ def rslm_mx4_score(x, b, dtype=torch.float32, out=None, stream=None):
     if x.shape[1] != b.dim:
         raise ValueError("x must have b's dimension")
     _same_device(x, b, "b")
-    out, ocode, ostride = _out_rows(out, (x.shape[0], b.n), dtype, x.device, stream)
+    into, ocode, ostride = _out_rows(out, (x.shape[0], b.n), dtype, x.device, stream)
     nb = L.lib().rslm_mx4_score_workspace(x.shape[0], b.n, b.dim, code)
     ws = _WS.get(nb, x.device, "mx4_score", stream) if nb else None
     L.check("rslm_mx4_score", L.lib().rslm_mx4_score(
-        x.data_ptr(), code, x.shape[0], stride, b.codes.data_ptr(), b.scales.data_ptr(), b.n, b.dim, out.data_ptr(),
-        ocode, ostride, _at(ws), nb, _launch_stream(stream, out.device)))
-    return out
+        x.data_ptr(), code, x.shape[0], stride, b.codes.data_ptr(), b.scales.data_ptr(), b.n, b.dim, into.data_ptr(),
+        ocode, ostride, _at(ws), nb, _launch_stream(stream, into.device)))
+    _written(out)
+    return into
 
 
 def rslm_mx4_score_backward(dout, b, dtype=None, out=None, stream=None):
@@ -666,13 +700,14 @@ def rslm_mx4_score_backward(dout, b, dtype=None, out=None, stream=None):
         raise ValueError("dout must have a column for every row of b")
     _same_device(dout, b, "b")
     m = dout.shape[0]
-    out, ocode, ostride = _out_rows(out, (m, b.dim), dout.dtype if dtype is None else dtype, dout.device, stream)
+    into, ocode, ostride = _out_rows(out, (m, b.dim), dout.dtype if dtype is None else dtype, dout.device, stream)
     nb = L.lib().rslm_mx4_score_backward_workspace(m, b.n, b.dim, code)
     ws = _WS.get(nb, dout.device, "mx4_backward", stream) if nb else None
     L.check("rslm_mx4_score_backward", L.lib().rslm_mx4_score_backward(
-        dout.data_ptr(), code, m, stride, b.codes.data_ptr(), b.scales.data_ptr(), b.n, b.dim, out.data_ptr(), ocode,
-        ostride, _at(ws), nb, _launch_stream(stream, out.device)))
-    return out
+        dout.data_ptr(), code, m, stride, b.codes.data_ptr(), b.scales.data_ptr(), b.n, b.dim, into.data_ptr(), ocode,
+        ostride, _at(ws), nb, _launch_stream(stream, into.device)))
+    _written(out)
+    return into
 
 
 # ------------------------------------------------------------------ 8-bit (MX8) rows
@@ -696,11 +731,12 @@ def rslm_mx8_score(a, b, dtype=torch.float32, out=None, stream=None):
     if a.dim != b.dim:
         raise ValueError("a and b must have the same dimension")
     _same_device(a, b, "b")
-    out, code, stride = _out_rows(out, (a.n, b.n), dtype, a.device, stream)
+    into, code, stride = _out_rows(out, (a.n, b.n), dtype, a.device, stream)
     L.check("rslm_mx8_score", L.lib().rslm_mx8_score(
-        a.codes.data_ptr(), a.scales.data_ptr(), a.n, b.codes.data_ptr(), b.scales.data_ptr(), b.n, a.dim, out.data_ptr(),
-        code, stride, _launch_stream(stream, out.device)))
-    return out
+        a.codes.data_ptr(), a.scales.data_ptr(), a.n, b.codes.data_ptr(), b.scales.data_ptr(), b.n, a.dim, into.data_ptr(),
+        code, stride, _launch_stream(stream, into.device)))
+    _written(out)
+    return into
 
 
 # ------------------------------------------------------------------ norms
@@ -751,18 +787,20 @@ def rslm_rmsnorm(x, weight=None, residual=None, eps=1e-6, y=True, rows=False, h=
     n, dim = x.shape
     wcode = _need_weight(weight, dim, x)
     rstride = hstride = 0
+    total = None
     if residual is not None:
         rstride = _like_rows(residual, x, "residual")
-        h, _, hstride = _out_rows(h, (n, dim), x.dtype, x.device, stream, "h")
+        total, _, hstride = _out_rows(h, (n, dim), x.dtype, x.device, stream, "h")
     elif h is not None:
         raise ValueError("h is written with a residual only")
-    r = RmsNorm(h if residual is not None else x, _empty((n, dim), x.dtype, x.device, stream) if y else None,
+    r = RmsNorm(x if total is None else total, _empty((n, dim), x.dtype, x.device, stream) if y else None,
                 Mx8Rows.empty(n, dim, x.device, stream) if rows else None,
                 _empty((n,), torch.float32, x.device, stream))
     L.check("rslm_rmsnorm", L.lib().rslm_rmsnorm(
-        x.data_ptr(), code, n, dim, stride, _at(residual), rstride, _at(weight), wcode, eps, _at(h), hstride, _at(r.y), dim,
+        x.data_ptr(), code, n, dim, stride, _at(residual), rstride, _at(weight), wcode, eps, _at(total), hstride, _at(r.y), dim,
         r.rows.codes.data_ptr() if rows else None, r.rows.scales.data_ptr() if rows else None, r.rstd.data_ptr(),
         _launch_stream(stream, x.device)))
+    _written(h)
     return r
 
 
@@ -784,7 +822,7 @@ def rslm_rmsnorm_backward(dy, result, weight=None, dh=None, dweight=True, out=No
     _same_device(dy, rstd, "result.rstd")
     wcode = _need_weight(weight, dim, dy)
     dhstride = _like_rows(dh, dy, "dh") if dh is not None else 0
-    out, _, ostride = _out_rows(out, (n, dim), dy.dtype, dy.device, stream)
+    into, _, ostride = _out_rows(out, (n, dim), dy.dtype, dy.device, stream)
     dw = ws = None
     nb = 0
     if dweight and weight is not None:
@@ -793,8 +831,9 @@ def rslm_rmsnorm_backward(dy, result, weight=None, dh=None, dweight=True, out=No
         ws = _scratch(nb, dy.device, stream)
     L.check("rslm_rmsnorm_backward", L.lib().rslm_rmsnorm_backward(
         dy.data_ptr(), code, n, dim, stride, h.data_ptr(), hstride, rstd.data_ptr(), _at(weight), wcode, _at(dh), dhstride,
-        out.data_ptr(), ostride, _at(dw), _at(ws), nb, _launch_stream(stream, dy.device)))
-    return out, dw
+        into.data_ptr(), ostride, _at(dw), _at(ws), nb, _launch_stream(stream, dy.device)))
+    _written(out)
+    return into, dw
 
 
 def _scratch(nbytes, device, stream):
@@ -824,20 +863,22 @@ def rslm_embed(table, ids, scale=1.0, dtype=None, out=None, stream=None):
     if isinstance(table, _MxRows):
         _need_mx(table, Mx4Rows, "table")
         _same_device(table, ids, "ids")
-        out, ocode, ostride = _out_rows(out, (n, table.dim), torch.float32 if dtype is None else dtype, table.device, stream)
+        into, ocode, ostride = _out_rows(out, (n, table.dim), torch.float32 if dtype is None else dtype, table.device, stream)
         L.check("rslm_mx4_embed", L.lib().rslm_mx4_embed(
             table.codes.data_ptr(), table.scales.data_ptr(), table.n, table.dim, ids.data_ptr(), id_bytes, n, scale,
-            out.data_ptr(), ocode, ostride, _launch_stream(stream, out.device)))
-        return out
+            into.data_ptr(), ocode, ostride, _launch_stream(stream, into.device)))
+        _written(out)
+        return into
     _no_history(table, "table")
     code, stride = _need_rows(table, "table")
     _need_dim(table, "table")
     _same_device(table, ids, "ids")
-    out, ocode, ostride = _out_rows(out, (n, table.shape[1]), table.dtype if dtype is None else dtype, table.device, stream)
+    into, ocode, ostride = _out_rows(out, (n, table.shape[1]), table.dtype if dtype is None else dtype, table.device, stream)
     L.check("rslm_embed", L.lib().rslm_embed(
-        table.data_ptr(), code, table.shape[0], table.shape[1], stride, ids.data_ptr(), id_bytes, n, scale, out.data_ptr(),
-        ocode, ostride, _launch_stream(stream, out.device)))
-    return out
+        table.data_ptr(), code, table.shape[0], table.shape[1], stride, ids.data_ptr(), id_bytes, n, scale, into.data_ptr(),
+        ocode, ostride, _launch_stream(stream, into.device)))
+    _written(out)
+    return into
 
 
 def rslm_embed_backward(dout, ids, rows, scale=1.0, dtype=None, out=None, accumulate=False, stream=None):
@@ -856,13 +897,14 @@ def rslm_embed_backward(dout, ids, rows, scale=1.0, dtype=None, out=None, accumu
     _same_device(dout, ids, "ids")
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
-    out, ocode, ostride = _out_rows(out, (rows, dim), dout.dtype if dtype is None else dtype, dout.device, stream)
+    into, ocode, ostride = _out_rows(out, (rows, dim), dout.dtype if dtype is None else dtype, dout.device, stream)
     nb = L.lib().rslm_embed_backward_workspace(n, rows, dim)
     ws = _scratch(nb, dout.device, stream)
     L.check("rslm_embed_backward", L.lib().rslm_embed_backward(
-        dout.data_ptr(), code, n, dim, stride, ids.data_ptr(), id_bytes, rows, scale, int(accumulate), out.data_ptr(), ocode,
-        ostride, _at(ws), nb, _launch_stream(stream, out.device)))
-    return out
+        dout.data_ptr(), code, n, dim, stride, ids.data_ptr(), id_bytes, rows, scale, int(accumulate), into.data_ptr(), ocode,
+        ostride, _at(ws), nb, _launch_stream(stream, into.device)))
+    _written(out)
+    return into
 
 
 # ------------------------------------------------------------------ log probabilities
@@ -926,11 +968,12 @@ def rslm_logprob_backward(scores, target, result, dlogprob=None, dentropy=None, 
             if t.shape != (m,):
                 raise ValueError(f"{name} must have an entry for every row of scores")
             _same_device(scores, t, name)
-    out, _, ostride = _out_rows(out, (m, n), scores.dtype, scores.device, stream)
+    into, _, ostride = _out_rows(out, (m, n), scores.dtype, scores.device, stream)
     L.check("rslm_logprob_backward", L.lib().rslm_logprob_backward(
         scores.data_ptr(), code, m, n, stride, result.scale, _at(target), result.stats.data_ptr(), result.entropy.data_ptr(),
-        _at(dlogprob), _at(dentropy), out.data_ptr(), ostride, _launch_stream(stream, out.device)))
-    return out
+        _at(dlogprob), _at(dentropy), into.data_ptr(), ostride, _launch_stream(stream, into.device)))
+    _written(out)
+    return into
 
 
 # ------------------------------------------------------------------ drafted tokens
