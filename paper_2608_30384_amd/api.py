@@ -11,6 +11,7 @@ import functools
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.graph import increment_version
 
 from . import _lib as L
@@ -505,9 +506,18 @@ def _need_rows(t, name, shape=None):
 def _no_history(t, name):
     """Refuses a tensor that autograd would follow: the results have no history, and a
     gradient through them would be lost without an error."""
-    if t is not None and t.requires_grad and torch.is_grad_enabled():
+    if t is None:
+        return
+    if t.requires_grad and torch.is_grad_enabled():
         raise ValueError(f"{name} requires a gradient, which these calls do not record: take it from the "
                          f"_backward function, and call under torch.no_grad() or pass {name}.detach()")
+    _no_tangent(t, name)
+
+
+def _no_tangent(t, name):
+    if forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None:
+        raise ValueError(f"{name} has a forward-mode tangent, which these calls do not carry on: pass its primal, or call "
+                         f"inside a torch.autograd.Function with a jvp of its own")
 
 
 def _empty(shape, dtype, device, stream):
@@ -538,6 +548,7 @@ def _out_rows(out, shape, dtype, device, stream, name="out"):
         if not base.is_leaf:
             raise ValueError(f"{name} is computed from tensors that require a gradient, which what is written over it does "
                              f"not have: call under torch.no_grad() or pass {name}.detach()")
+    _no_tangent(out, name)
     return out, code, stride
 
 
