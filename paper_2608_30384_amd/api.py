@@ -617,8 +617,15 @@ class Mx8Rows(_MxRows):
 
 
 def _need_mx(rows, kind, name):
-    if not isinstance(rows, kind):
+    """Refuses rows of the other kind, which would be read past their end.  An object of
+    another class, with what the calls read of rows, is one of this kind if it holds enough."""
+    if isinstance(rows, kind):
+        return
+    if isinstance(rows, _MxRows) or not all(hasattr(rows, a) for a in ("codes", "scales", "n", "dim", "device")):
         raise TypeError(f"{name} must be {kind.__name__}, got {type(rows).__name__}")
+    groups = rows.n * ((rows.dim + 127) // 128)
+    if rows.codes.nbytes < groups * kind._bytes or rows.scales.nbytes < 4 * groups:
+        raise ValueError(f"{name}'s codes / scales must hold {groups * kind._bytes} and {4 * groups} bytes")
 
 
 def _quantize(fn, kind, x, plan, rows, stream):
