@@ -538,7 +538,8 @@ int rslm_mx4_score_backward(const void *dout, int32_t dtype, int64_t m, int64_t 
  *   is rounded to, both have infinity).
  * rslm_mx8_score: their products with MX4 rows,
  *   out[i][j] = sum_d a_i[d] b_j[d],  out: m rows of n, type dtype,
- *   row i at i * stride elements (stride >= n).  m <= 4,194,240.
+ *   row i at i * stride elements (stride >= n).  m <= 4,194,240.  Both sides' rows
+ *   rotated by the same plan, or neither's (rslm_rmsnorm's are not).
  *   Float32 results have the error of a float32 sum of exact products (values of
  *   a below 2^-130 apart).  For float16 and bfloat16 results the matrix cores drop,
  *   of each product of coordinates 8 i .. 8 i + 7, what lies more than 13 places

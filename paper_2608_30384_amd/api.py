@@ -741,9 +741,10 @@ def rslm_mx8_dequantize(rows, dtype=torch.float32, out=None, stream=None):
 
 
 def rslm_mx8_score(a, b, dtype=torch.float32, out=None, stream=None):
-    """a b^T of MX8 rows a and MX4 rows b (a.n x b.n).  For float32 results products
-    are exact; for 16-bit ones the matrix cores drop what lies far below their
-    rounding (``include/rslm.h``), at twice the rate."""
+    """a b^T of MX8 rows a and MX4 rows b (a.n x b.n), both rotated by the same plan or
+    neither.  For float32 results products are exact; for 16-bit ones the matrix cores
+    drop what lies far below the largest products (``include/rslm.h``), at twice the
+    rate."""
     _need_mx(a, Mx8Rows, "a")
     _need_mx(b, Mx4Rows, "b")
     if a.dim != b.dim:
@@ -796,8 +797,10 @@ def rslm_rmsnorm(x, weight=None, residual=None, eps=1e-6, y=True, rows=False, h=
     """h = x + residual and its root-mean-square norm times weight (None: ones), as
     floats of x's type (y), as MX8 rows (rows), or both.  x and residual: float32,
     float16 or bfloat16, any row stride; weight: any of these types; h: where to
-    write the sum (may be x or residual).  The gradients are
-    ``rslm_rmsnorm_backward``'s: autograd does not follow the call."""
+    write the sum (may be x or residual).  The MX8 rows are not rotated: Mx4Rows made
+    without a plan belong to them, and to rotated ones ``rslm_mx8_quantize`` of y with
+    their plan.  The gradients are ``rslm_rmsnorm_backward``'s: autograd does not follow
+    the call."""
     for t, name in ((x, "x"), (weight, "weight"), (residual, "residual")):
         _no_history(t, name)
     code, stride = _need_rows(x, "x")
