@@ -69,3 +69,18 @@ def test_past_the_mean_of_float32(R, dim):
     assert r.rstd[2] == 0 and r.y[2, dim - 1].isnan() and (r.y[2, :dim - 1] == 0).all()
     assert r.y[3].isnan().all()
     assert (r.y[4] == 0).all() and abs(float(r.rstd[4]) - 1e3) < 1e-3
+
+
+@pytest.mark.parametrize("n,dim", [(200_000, 1030), (140_000, 5)])
+def test_large_rows_among_many(R, n, dim):
+    """More rows than workgroups, large and ordinary ones in turns that differ from workgroup to
+    workgroup: each has its own sum."""
+    g = torch.Generator(device="cuda").manual_seed(dim)
+    x = torch.randn((n, dim), generator=g, device="cuda")
+    large = torch.rand((n,), generator=g, device="cuda") < 0.5
+    x[large] = 1.2e19 * (0.5 + 0.5 * torch.rand((int(large.sum()), dim), generator=g, device="cuda"))
+    r = R.rslm_rmsnorm(x, y=False, rows=True)
+    rstd = 1 / torch.sqrt(x.double().square().mean(1) + 1e-6)
+    assert ((r.rstd.double() - rstd).abs() <= (44 + dim / 256) * U * rstd).all()
+    assert torch.equal(R.rslm_rmsnorm(x[:70], y=False, rows=True).rows.codes, r.rows.codes[:70])
+    assert torch.equal(R.rslm_rmsnorm(x[-70:], y=False, rows=True).rows.codes, r.rows.codes[-70:])
