@@ -544,7 +544,9 @@ int rslm_mx4_score_backward(const void *dout, int32_t dtype, int64_t m, int64_t 
  *   a below 2^-130 apart).  For float16 and bfloat16 results the matrix cores drop,
  *   of each product of coordinates 8 i .. 8 i + 7, what lies more than 13 places
  *   below the leading place of the largest of them: less than 2^-13 of the largest
- *   for each of the others, mostly some 2^-17 of a result in all.
+ *   for each of the others.  Of rows with random signs that is some 2^-17 of a
+ *   result in all; where large products of a group cancel it is relative to them,
+ *   and not to the result.
  * ------------------------------------------------------------------------ */
 int rslm_mx8_quantize(const rslm_plan *plan, const void *x, int32_t dtype, int64_t n, int32_t dim,
                       int64_t stride, uint8_t *codes, uint8_t *scales, void *stream);
