@@ -351,7 +351,7 @@ constexpr int kSumFlight = 4;   // rows asked for at once, twice
 
 // A lane's 8 columns of a row: those from `at` on, of which the first `skip` are another
 // lane's.  So a row's last columns too are read and written 8 at a time, and no branch
-// keeps a wavefront's loads apart (65,536 x 768 bfloat16 33 us, 3.0 TB/s of dout alone; 72
+// keeps a wavefront's loads apart (65,536 x 768 bfloat16 45 us, 2.2 TB/s of dout alone; 68
 // with a branch for the last columns).  Rows of less than 8: WIDE false.
 struct SumLane {
   int at, skip;

@@ -7,7 +7,7 @@
 // coordinates, 8 consecutive ones each: one 16- or 32-byte load, one 4-byte
 // word of codes (8-byte for MX8), and the 32 coordinates of a scale are those of four adjacent
 // lanes, whose largest magnitude is found by two exchanges inside the quad.  65,536 x 768
-// float32, rotated: 67 us to MX4, 64 to MX8 (4.0 TB/s, VALU 83 % busy); from MX8 to bfloat16 24.
+// float32, rotated: 67 us to MX4, 58 to 64 to MX8 (4.0 TB/s and more, VALU 83 to 85 % busy); from MX8 to bfloat16 24.
 #include "mx4_dev.h"
 #include "rows_dev.h"
 

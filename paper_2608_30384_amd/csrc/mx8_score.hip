@@ -235,7 +235,8 @@ __global__ void __launch_bounds__(256, MF == 4 ? 2 : 1) k_mx8_score_tile(
     vb[j] = (wid * (16 * LB) + 16 * j + 2 * line + (slot >> 2)) * cpb + ((slot & 3) << 4);
   }
   const uint32_t vs = (wid * 64 + lane) * sp;
-  // load i of group t, to place p; past the last group from past the end, which gives zeros
+  // load i of group t, to place p.  Past the last group the loads keep their number, from past
+  // the end or, of buffers of over 2 GiB, from other rows: what they bring is not multiplied.
   auto load = [&](int t, int p, int i) {
     const uint32_t past = t < steps ? 0u : 0x80000000u;
     if (i < LA)
@@ -350,6 +351,9 @@ __global__ void __launch_bounds__(256, MF == 4 ? 2 : 1) k_mx8_score_tile(
 // lane are turned to bfloat16, two ahead they are read; at a pass's last step b's are turned,
 // each fragment behind the last instruction that uses the register.  The barrier, late in
 // the second pass, waits for the next group, and those after it are asked for behind it.
+// Two workgroups to a CU (MF 2) leave 256 registers, which are 5 too few: 24 bytes a lane go to
+// scratch memory, and one of these, an address, is read back in each group behind the barrier,
+// where all but the first matrix instruction wait for it.
 template <int MF>
 __global__ void __launch_bounds__(256, MF == 2 ? 2 : 1) k_mx8_score_tile_f32(
     const uint8_t *__restrict__ ac, const uint8_t *__restrict__ as, int64_t m, const uint8_t *__restrict__ bc,

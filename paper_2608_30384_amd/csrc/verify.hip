@@ -12,7 +12,7 @@
 // Two kernels.  The first sums the exponentials of every row, a slice of 1,024 entries (more
 // where a row has over 262,144) at a time to a wavefront.  In the second each workgroup of a
 // sequence settles which drafts stand, and where one falls sums r over its slices; the last
-// one to have done so draws.  64 sequences of 4 drafts by 131,072 bfloat16 scores: 39 and 26
+// one to have done so draws.  64 sequences of 4 drafts by 131,072 bfloat16 scores: 35 and 26
 // us (a kernel of its own for the draw: 17 and 9); one, of float32: 4.8 and 11.6 (5.4 and 8.3,
 // and a launch), chains of dependent reads.
 #include "mx4_dev.h"
@@ -406,6 +406,9 @@ __global__ void __launch_bounds__(kVfThreads) k_verify_draw(VerifyArgs a) {
     // The sums are written and read past the caches that other workgroups do not share, and
     // have arrived before the workgroup counts itself: the last one reads all of them.  (With
     // fences, which write back and empty those caches, 64 sequences took 44 us and not 26.)
+    // All these accesses are relaxed: their order is gfx950's and not the language's.  There
+    // stores and loads of agent scope go to memory that all XCDs see, the wait ends when a
+    // wavefront's stores are there, and the barrier comes behind every wavefront's.
     sum_over<T>(a, b, group, st, table);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
