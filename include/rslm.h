@@ -577,9 +577,9 @@ int rslm_mx8_score(const uint8_t *a_codes, const uint8_t *a_scales, int64_t m, c
  *   dx      = rstd * (g - u * mean_d(g u)) + dh  (x's and the residual's)
  *   dweight = sum over rows of dy * u  (dim values of type weight_dtype)
  *   dx or dweight NULL: not computed.  dx may be dy, h or dh (the same stride).
- *   Gradients go past the rounding to 8 bits as if it were not there.  Sums (here
- *   those themselves have to be within float32) are taken in a fixed order.  ws (for
- *   dweight): 16-byte aligned.
+ *   Gradients go past the rounding to 8 bits as if it were not there.  Sums are
+ *   float32 in a fixed order; here they themselves, and not only their means, have
+ *   to be within it.  ws (for dweight): 16-byte aligned.
  * n <= 2^31 - 256, 1 <= dim <= 65,536.
  * ------------------------------------------------------------------------ */
 int rslm_rmsnorm(const void *x, int32_t dtype, int64_t n, int32_t dim, int64_t x_stride, const void *residual,
